@@ -205,6 +205,96 @@ atb_status atb_bfp16_quantize(const float *A_f32_dev, int64_t lda, void *A_bfp_d
 atb_status atb_bfp16_decode(const void *A_bfp_dev, void *A_bf16_dev, int64_t M, int64_t K,
                             void *hip_stream);
 
+/* ------------------------------------- a feed-forward sublayer's operators
+ *
+ * What a transformer's feed-forward sublayer needs around its matrix products: layer norm, the gated block in bf16 with
+ * its gradients, and the same block's products with 4-bit weights for few tokens.  All matrices are row-major, a row's
+ * elements next to each other; ld* is the distance between rows in elements, at least a row's length.  Sums and
+ * statistics are held in fp32.  M == 0 (no tokens) is a valid call: gradients of parameters are then written as zero.
+ * Non-finite inputs give what the formulas give; they reach no row or column that does not depend on them. */
+
+typedef enum atb_type { ATB_TYPE_BF16 = 0, ATB_TYPE_F32 = 1 } atb_type;
+typedef enum atb_activation {
+    ATB_ACT_SILU = 0,      /* g / (1 + exp(-g)) */
+    ATB_ACT_GELU = 1,      /* g (1 + erf(g / sqrt 2)) / 2 */
+    ATB_ACT_GELU_TANH = 2  /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+} atb_activation;
+
+/* Layer norm of the M rows of x (D elements of `type`, DEVICE):
+ *     mu = sum(x) / D,  r = 1 / sqrt(sum((x - mu)^2) / D + eps),  y = (x - mu) r weight + bias.
+ * weight, bias: DEVICE, D elements of `param_type`, or NULL for 1 and 0.  y: DEVICE, type `type`; may be x itself.
+ * mean, rstd: DEVICE, M floats each, or NULL: mu and r, which the backward pass takes.  1 <= D <= 2^24; every pointer
+ * at least aligned to its elements.  Async on hip_stream. */
+atb_status atb_layer_norm(const void *x, int64_t ldx, const void *weight, const void *bias, double eps, void *y, int64_t ldy,
+                          float *mean, float *rstd, int64_t M, int64_t D, atb_type type, atb_type param_type, void *hip_stream);
+
+/* Bytes of atb_layer_norm_backward's workspace (partial sums of the parameters' gradients); 0 on invalid arguments or M == 0. */
+size_t atb_layer_norm_workspace(int64_t M, int64_t D);
+
+/* Its backward pass: with xh = (x - mean) rstd and g = dy weight,
+ *     dx = rstd (g - sum(g) / D - xh sum(g xh) / D),  dweight = sum over rows of dy xh,  dbias = sum over rows of dy.
+ * dx: M rows of `type`; dweight, dbias: D elements of `param_type`, each may be NULL (not asked for; dx too).  workspace: DEVICE, 16-byte
+ * aligned, needed where dweight or dbias is asked for.  The sums over rows are taken in an order that M and D alone
+ * decide: the same inputs give the same bits. */
+atb_status atb_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, const float *mean, const float *rstd,
+                                   const void *weight, void *dx, int64_t lddx, void *dweight, void *dbias, void *workspace,
+                                   int64_t M, int64_t D, atb_type type, atb_type param_type, void *hip_stream);
+
+/* The gated block  y = (act(x Wg^T) o (x Wu^T)) Wd^T  of M tokens in bf16: x M x D, Wg and Wu F x D, Wd D x F (the
+ * layout in which frameworks keep the weights of linear layers), y M x D.  Both first products, the activation and the
+ * product are one kernel. */
+typedef struct atb_ffn {
+    const void *x, *w_gate, *w_up, *w_down;     /* DEVICE, bf16, 16-byte aligned */
+    int64_t ldx, ld_gate, ld_up, ld_down;       /* multiples of 8, below 2^22 */
+    int64_t M, D, F;                            /* 0 <= M <= 2^23; D, F multiples of 8, 8 .. 2^22 - 8 */
+    atb_activation act;
+} atb_ffn;
+
+/* Bytes of the buffer that keeps x Wg^T and x Wu^T for the backward pass, 6 M F: three planes of M x F 16-bit words, the upper halves of
+ * the two products in fp32 and the next byte of both (24 of their 32 bits: in bf16 they would double the variance of dx's error); 0 on
+ * invalid arguments or M == 0. */
+size_t atb_ffn_kept_bytes(int64_t M, int64_t F);
+
+/* h: DEVICE, M x F bf16 (pitch F), the block's inner activations: workspace, and what the backward pass takes.  kept: DEVICE,
+ * atb_ffn_kept_bytes(M, F) bytes, 16-byte aligned, or NULL: nothing is kept.  y: DEVICE, bf16, pitch ldy (a multiple of 8).
+ * Async on hip_stream. */
+atb_status atb_ffn_forward(const atb_ffn *f, void *h, void *kept, void *y, int64_t ldy, void *hip_stream);
+
+/* Gradients of a loss with dy (M x D bf16, pitch lddy): with g = x Wg^T, u = x Wu^T, dh = dy Wd,
+ *     dg = dh o u o act'(g),  du = dh o act(g),
+ *     dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h.
+ * h, kept: of the forward pass.  dgate, dup: DEVICE, M x F bf16 (pitch F), workspace: dg and du (rounded to bf16; dh is not).  dx: M x D,
+ * pitch lddx; dw_gate, dw_up: F x D, dw_down: D x F, contiguous, bf16; each of the four may be NULL: not asked for (dw_gate and
+ * dw_up together).  All 16-byte aligned. */
+atb_status atb_ffn_backward(const atb_ffn *f, const void *h, const void *kept, const void *dy, int64_t lddy, void *dgate, void *dup,
+                            void *dx, int64_t lddx, void *dw_gate, void *dw_up, void *dw_down, void *hip_stream);
+
+/* A weight of N outputs and K inputs in 4 bits: w[n][k] = s[n][k / group] (q[n][k] - z[n][k / group]), 0 <= q <= 15. */
+typedef struct atb_q4 {
+    const void *packed;    /* DEVICE, N x K/2 bytes: q[n][k] in the low half of byte k / 2 for even k, in the high half for odd k; 16-byte aligned */
+    const void *scales;    /* DEVICE, N x K/group bf16 */
+    const void *zeros;     /* DEVICE, N x K/group uint8 (0 .. 15), or NULL: 8 everywhere */
+    int64_t N, K;          /* 1 <= N <= 2^24; K a multiple of group, at most 2^22 */
+    int group;             /* 32, 64 or 128 */
+} atb_q4;
+
+/* Quantise W (DEVICE, N x K of `type`, pitch ldw) to 4 bits.  Without zero points (zeros == NULL) s = max|w| / 7 over the group, rounded to
+ * bf16, and q = 8 + rint(w / s); with them s = (max(w, 0) - min(w, 0)) / 15 rounded, z = rint(-min(w, 0) / s) and q = z + rint(w / s); q and z are clamped to
+ * 0 .. 15, and a group of zeros has s = 0 and q = z.  Inputs must be finite. */
+atb_status atb_q4_quantize(const void *W, int64_t ldw, atb_type type, void *packed, void *scales, void *zeros,
+                           int64_t N, int64_t K, int group, void *hip_stream);
+
+/* The values that a 4-bit weight stands for: out, DEVICE, N x K of out_type (in fp32 exact, in bf16 rounded to nearest even). */
+atb_status atb_q4_decode(const atb_q4 *w, void *out, atb_type out_type, void *hip_stream);
+
+/* y = x W^T for few rows: x DEVICE, M x K bf16 (pitch ldx, a multiple of 8; 16-byte aligned), y M x N of y_type (pitch ldy).  Any M up to 2^23
+ * is right; weights are read once per 32 rows.  Async on hip_stream. */
+atb_status atb_q4_matvec(const atb_q4 *w, const void *x, int64_t ldx, void *y, int64_t ldy, atb_type y_type, int64_t M, void *hip_stream);
+
+/* h = act(x Wg^T) o (x Wu^T) in one launch, h M x N bf16: Wg and Wu with the same N, K, group, both with or both without zero points. */
+atb_status atb_q4_gated(const atb_q4 *w_gate, const atb_q4 *w_up, atb_activation act, const void *x, int64_t ldx, void *h, int64_t ldh,
+                        int64_t M, void *hip_stream);
+
 /* ------------------------------------------------- model and tile selector */
 
 /* Machine constants of the paper's performance model (Secs. 3 and 5). */

@@ -74,12 +74,26 @@ class KernelInfo(ctypes.Structure):
         return self.T_MA, self.T_MC, self.T_K, self.T_N
 
 
+class Ffn(ctypes.Structure):
+    """atb_ffn: the operands of a gated block."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w_gate", "w_up", "w_down")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ld_gate", "ld_up", "ld_down", "M", "D", "F")] + [("act", ctypes.c_int)]
+
+
+class Q4(ctypes.Structure):
+    """atb_q4: a weight in 4 bits."""
+    _fields_ = [("packed", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("group", ctypes.c_int)]
+
+
 # every symbol include/atb.h declares
 EXPORTS = [
     "atb_status_string", "atb_last_hip_error", "atb_gemm_create", "atb_gemm_create_fmt", "atb_gemm_run", "atb_gemm_destroy",
     "atb_gemm_launch_info", "atb_gemm_kernel", "atb_gemm_streams", "atb_instance_count", "atb_instance_get", "atb_bfp16_layout", "atb_bfp16_bytes",
     "atb_bfp16_quantize", "atb_bfp16_decode", "atb_hw_params_xdna2", "atb_hw_params_mi355x",
     "atb_model_eval", "atb_select_tiles", "atb_model_microkernel", "atb_instance_geometry", "atb_mfma_probe",
+    "atb_layer_norm", "atb_layer_norm_workspace", "atb_layer_norm_backward", "atb_ffn_kept_bytes", "atb_ffn_forward", "atb_ffn_backward",
+    "atb_q4_quantize", "atb_q4_decode", "atb_q4_matvec", "atb_q4_gated",
 ]
 
 
@@ -134,6 +148,26 @@ def lib() -> ctypes.CDLL:
     L.atb_instance_geometry.argtypes = [ci, pi, pi, pi, pi]
     L.atb_mfma_probe.restype = ci
     L.atb_mfma_probe.argtypes = [vp, vp, ci, ci, ci, ci, vp, ctypes.POINTER(ctypes.c_double)]
+    L.atb_layer_norm.restype = ci
+    L.atb_layer_norm.argtypes = [vp, i64, vp, vp, ctypes.c_double, vp, i64, vp, vp, i64, i64, ci, ci, vp]
+    L.atb_layer_norm_workspace.restype = ctypes.c_size_t
+    L.atb_layer_norm_workspace.argtypes = [i64, i64]
+    L.atb_layer_norm_backward.restype = ci
+    L.atb_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, ci, ci, vp]
+    L.atb_ffn_forward.restype = ci
+    L.atb_ffn_forward.argtypes = [ctypes.POINTER(Ffn), vp, vp, vp, i64, vp]
+    L.atb_ffn_kept_bytes.restype = ctypes.c_size_t
+    L.atb_ffn_kept_bytes.argtypes = [i64, i64]
+    L.atb_ffn_backward.restype = ci
+    L.atb_ffn_backward.argtypes = [ctypes.POINTER(Ffn), vp, vp, vp, i64, vp, vp, vp, i64, vp, vp, vp, vp]
+    L.atb_q4_quantize.restype = ci
+    L.atb_q4_quantize.argtypes = [vp, i64, ci, vp, vp, vp, i64, i64, ci, vp]
+    L.atb_q4_decode.restype = ci
+    L.atb_q4_decode.argtypes = [ctypes.POINTER(Q4), vp, ci, vp]
+    L.atb_q4_matvec.restype = ci
+    L.atb_q4_matvec.argtypes = [ctypes.POINTER(Q4), vp, i64, vp, i64, ci, i64, vp]
+    L.atb_q4_gated.restype = ci
+    L.atb_q4_gated.argtypes = [ctypes.POINTER(Q4), ctypes.POINTER(Q4), ci, vp, i64, vp, i64, i64, vp]
     _lib = L
     return L
 
@@ -409,3 +443,7 @@ class Gemm:
             self.close()
         except Exception:
             pass
+
+
+from .layers import (FeedForwardState, Q4Weight, feed_forward, feed_forward_backward, layer_norm, layer_norm_backward, q4_decode,  # noqa: E402
+                     q4_feed_forward, q4_matvec, q4_quantize)

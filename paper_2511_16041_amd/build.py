@@ -28,7 +28,9 @@ ALIGNED = ["-falign-loops=64"]
 # (source, object name, extra flags): the GEMM instance table is cut into three groups that compile side by side
 SOURCES = [("atb_gemm.hip", "atb_gemm_g0", ["-DATB_GROUP=0"]), ("atb_gemm.hip", "atb_gemm_g1", ["-DATB_GROUP=1"] + ALIGNED),
            ("atb_gemm.hip", "atb_gemm_g2", ["-DATB_GROUP=2"]), ("atb_skinny.hip", "atb_skinny", SKINNY_FLAGS), ("atb_rows.hip", "atb_rows", WHOLE_PHIS), ("atb_bfp16.hip", "atb_bfp16", []), ("atb_probe.hip", "atb_probe", []),
-           ("atb_model.cpp", "atb_model", []), ("atb_api.cpp", "atb_api", [])]
+           ("atb_ffn.hip", "atb_ffn", WHOLE_PHIS), ("atb_ffn_grad.hip", "atb_ffn_grad", WHOLE_PHIS), ("atb_stream.hip", "atb_stream", []),
+           ("atb_norm.hip", "atb_norm", []), ("atb_q4.hip", "atb_q4", []),
+           ("atb_model.cpp", "atb_model", []), ("atb_api.cpp", "atb_api", []), ("atb_layers_api.cpp", "atb_layers_api", [])]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -69,7 +71,7 @@ def build_binding(verbose: bool = False) -> str:
     includes += [d for d in include_paths("cuda") if d not in includes]          # torch's ROCm, where HIPCC is not inside one
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I", os.path.join(ROOT, "include")]
     for d in includes:
         cmd += ["-isystem", d]
     cmd += [os.path.join(CSRC, BINDING_SOURCE), "-o", part, "-L" + libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
@@ -134,7 +136,7 @@ def ensure_built() -> str:
 def ensure_binding() -> str:
     """Path of the extension module, likewise."""
     out = binding_path()
-    if _older(out, [os.path.join(CSRC, BINDING_SOURCE)]):
+    if _older(out, [os.path.join(CSRC, BINDING_SOURCE), os.path.join(ROOT, "include", "atb.h")]):
         build_binding()
     return out
 

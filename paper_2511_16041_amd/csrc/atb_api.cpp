@@ -18,15 +18,19 @@ struct atb_gemm {
 };
 
 namespace {
-
 thread_local int g_last_hip_error = 0;
+}
 
-atb_status hip_status(hipError_t e)
+atb_status atb::hip_status(hipError_t e)
 {
     if (e == hipSuccess) return ATB_OK;
     g_last_hip_error = (int)e;
     return ATB_ERR_HIP;
 }
+
+namespace {
+
+using atb::hip_status;
 
 int device_cus()
 {

@@ -52,6 +52,9 @@ const Instance &instance(int i);
 // index of the instance with these factors, or -1
 int find_instance(int T_MA, int T_MC, int T_K, int T_N);
 
+// ATB_OK, or ATB_ERR_HIP and the error kept for atb_last_hip_error.
+atb_status hip_status(hipError_t e);
+
 // Compute units of the current device, 0 if there is none.
 int compute_units();
 

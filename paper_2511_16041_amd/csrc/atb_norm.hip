@@ -1,0 +1,441 @@
+// Layer norm for gfx950, forward and backward.  Bound: HBM; a small call is its launch.
+//
+// mu = sum(x) / D, r = 1 / sqrt(sum((x - mu)^2) / D + eps), y = (x - mu) r w + b.  A row is held in registers, 16 elements per thread, so it is read
+// once and the variance is the sum of squares about the mean itself (no E[x^2] - mu^2, which loses the digits of a row far off centre).
+// Backward, with xh = (x - mu) r and g = dy w: dx = r (g - mean(g) - xh mean(g xh)); dw = sum over rows of dy xh, db = sum of dy: every
+// workgroup walks rows a grid apart and keeps its share of both sums in registers, 16 columns per thread; a second kernel adds the
+// workgroups' sums in order.  No atomics: the same bits every time.
+// Rows begin anywhere: 16-byte requests at any element, and the elements of the last, incomplete chunk one by one.
+#include "atb_device.h"
+#include "atb_layers.h"
+
+namespace atb {
+namespace {
+
+constexpr int kPerThread = 16;                 // elements of a row that a thread holds
+constexpr int kMaxRow = 1024 * kPerThread;     // longer rows are read again for every sum
+constexpr int kGradThreads = 512;              // workgroup of the backward pass: 256 registers per thread
+constexpr int kMaxGradRow = kGradThreads * kPerThread;
+
+template <class T> struct Chunk;               // 16 bytes of a row
+template <> struct Chunk<__bf16> {
+    static constexpr int E = 8;
+    typedef bf16x8 vec;
+    typedef bf16x8 any __attribute__((aligned(2)));
+};
+template <> struct Chunk<float> {
+    static constexpr int E = 4;
+    typedef floatx4 vec;
+    typedef floatx4 any __attribute__((aligned(4)));
+};
+
+// Elements at .. at + E - 1 of a row of D; `other` past its end.
+template <class T, int E>
+ATB_DEV void load(const T *row, int at, int D, float (&v)[E], float other)
+{
+    constexpr int C = Chunk<T>::E;
+    if (at + E <= D) {
+#pragma unroll
+        for (int c = 0; c < E; c += C) {
+            const typename Chunk<T>::vec w = *reinterpret_cast<const typename Chunk<T>::any *>(row + at + c);
+#pragma unroll
+            for (int e = 0; e < (C < E ? C : E); ++e) v[c + e] = (float)w[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = at + e < D ? (float)row[at + e] : other;
+    }
+}
+// (half a chunk: parameters in bf16 of rows in fp32)
+template <>
+ATB_DEV void load<__bf16, 4>(const __bf16 *row, int at, int D, float (&v)[4], float other)
+{
+    if (at + 4 <= D) {
+        const bf16x4 w = *reinterpret_cast<const bf16x4_u *>(row + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)w[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = at + e < D ? (float)row[at + e] : other;
+    }
+}
+
+template <class T, int E>
+ATB_DEV void store(T *row, int at, int D, const float (&v)[E])
+{
+    static_assert(E == Chunk<T>::E, "one chunk");
+    if (at + E <= D) {
+        typename Chunk<T>::vec w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] = (T)v[e];
+        *reinterpret_cast<typename Chunk<T>::any *>(row + at) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (at + e < D) row[at + e] = (T)v[e];
+    }
+}
+
+ATB_DEV float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// Sums over the T threads of a row group.  `scratch`: one float per wave of the workgroup and sum; every thread of the workgroup calls it.
+template <int T, int N>
+ATB_DEV void row_sums(float (&v)[N], float *scratch)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (T > 64) {
+        constexpr int W = T / 64;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) scratch[wave * N + i] = v[i];
+        __syncthreads();
+        const float *mine = scratch + (wave / W) * W * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) s += mine[w * N + i];
+            v[i] = s;
+        }
+    }
+}
+
+// T threads per row, blockDim.x / T rows per workgroup.
+template <class X, class P, int T>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(const NormParams p)
+{
+    constexpr int E = Chunk<X>::E, C = kPerThread / E, NT = T < 256 ? 256 : T;
+    __shared__ float scratch[2][NT / 64];
+    const int64_t row = (int64_t)blockIdx.x * (NT / T) + threadIdx.x / T;
+    const int t = threadIdx.x % T, D = (int)p.D;
+    const bool live = row < p.M;
+    const X *x = static_cast<const X *>(p.x) + (live ? row : 0) * p.ldx;
+    float v[C][E], sum[1] = {0.0f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        load<X, E>(x, (c * T + t) * E, D, v[c], 0.0f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[0] += v[c][e];
+    }
+    row_sums<T, 1>(sum, scratch[0]);
+    const float mean = sum[0] / (float)D;
+    sum[0] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[c][e] -= mean;
+            if ((c * T + t) * E + e < D) sum[0] += v[c][e] * v[c][e];
+        }
+    row_sums<T, 1>(sum, scratch[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
+    if (!live) return;
+    if (t == 0) {
+        if (p.mean) p.mean[row] = mean;
+        if (p.rstd) p.rstd[row] = rstd;
+    }
+    X *y = static_cast<X *>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * T + t) * E;
+        if (at >= D) break;
+        float w[E], b[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) { w[e] = 1.0f; b[e] = 0.0f; }
+        if (p.weight) load<P, E>(static_cast<const P *>(p.weight), at, D, w, 0.0f);
+        if (p.bias) load<P, E>(static_cast<const P *>(p.bias), at, D, b, 0.0f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * rstd * w[e] + b[e];
+        store<X, E>(y, at, D, v[c]);
+    }
+}
+
+// Rows of any length: read three times (from the second time on out of a cache).
+template <class X, class P>
+__global__ void __launch_bounds__(1024) norm_long_kernel(const NormParams p)
+{
+    __shared__ float scratch[2][16];
+    const int64_t row = blockIdx.x;
+    const int D = (int)p.D;
+    const X *x = static_cast<const X *>(p.x) + row * p.ldx;
+    float sum[1] = {0.0f};
+    for (int i = threadIdx.x; i < D; i += 1024) sum[0] += (float)x[i];
+    row_sums<1024, 1>(sum, scratch[0]);
+    const float mean = sum[0] / (float)D;
+    sum[0] = 0.0f;
+    for (int i = threadIdx.x; i < D; i += 1024) {
+        const float d = (float)x[i] - mean;
+        sum[0] += d * d;
+    }
+    row_sums<1024, 1>(sum, scratch[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
+    if (threadIdx.x == 0) {
+        if (p.mean) p.mean[row] = mean;
+        if (p.rstd) p.rstd[row] = rstd;
+    }
+    X *y = static_cast<X *>(p.y) + row * p.ldy;
+    const P *w = static_cast<const P *>(p.weight), *b = static_cast<const P *>(p.bias);
+    for (int i = threadIdx.x; i < D; i += 1024)
+        y[i] = (X)(((float)x[i] - mean) * rstd * (w ? (float)w[i] : 1.0f) + (b ? (float)b[i] : 0.0f));
+}
+
+// dx, and (PARAMS) the workgroup's part of dw and db: partial[workgroup][2][D].
+template <class X, class P, int T, bool PARAMS>
+__global__ void __launch_bounds__(T > kGradThreads ? T : kGradThreads) norm_grad_kernel(const NormParams p, int rounds)
+{
+    constexpr int E = Chunk<X>::E, C = kPerThread / E, NT = T > kGradThreads ? T : kGradThreads, R = NT / T;
+    __shared__ float scratch[2][2 * NT / 64];
+    const int t = threadIdx.x % T, group = threadIdx.x / T, D = (int)p.D;
+    const X *x0 = static_cast<const X *>(p.x), *dy0 = static_cast<const X *>(p.dy);
+    float dw[C][E], db[C][E], w[C][E];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) { dw[c][e] = db[c][e] = 0.0f; w[c][e] = 1.0f; }
+        if (p.weight) load<P, E>(static_cast<const P *>(p.weight), (c * T + t) * E, D, w[c], 0.0f);
+    }
+    for (int n = 0; n < rounds; ++n) {                        // the same number for every thread of the workgroup
+        const int64_t row = ((int64_t)n * gridDim.x + blockIdx.x) * R + group;
+        const bool live = row < p.M;
+        const int64_t at_row = live ? row : 0;
+        const float mean = p.mean[at_row], rstd = p.rstd[at_row];
+        float xh[C][E], g[C][E], s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * T + t) * E;
+            load<X, E>(x0 + at_row * p.ldx, at, D, xh[c], mean);          // xh = 0 past the end
+            load<X, E>(dy0 + at_row * p.lddy, at, D, g[c], 0.0f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                xh[c][e] = (xh[c][e] - mean) * rstd;
+                if constexpr (PARAMS) {
+                    if (live) {
+                        dw[c][e] += g[c][e] * xh[c][e];
+                        db[c][e] += g[c][e];
+                    }
+                }
+                g[c][e] *= w[c][e];
+                s[0] += g[c][e];
+                s[1] += g[c][e] * xh[c][e];
+            }
+        }
+        row_sums<T, 2>(s, scratch[n & 1]);
+        if (live && p.dx) {
+            const float m0 = s[0] / (float)D, m1 = s[1] / (float)D;
+            X *dx = static_cast<X *>(p.dx) + row * p.lddx;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = (c * T + t) * E;
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[c][e] = rstd * (g[c][e] - m0 - xh[c][e] * m1);
+                if (at < D) store<X, E>(dx, at, D, g[c]);
+            }
+        }
+    }
+    if constexpr (PARAMS) {
+        // the row groups one after the other
+        extern __shared__ float sums[];                       // [2][D]
+        float *out = p.partial + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll 1
+        for (int r = 0; r < R; ++r) {
+            if (R > 1) __syncthreads();
+            if (group != r) continue;
+            float *to = r == R - 1 ? out : sums;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int at = (c * T + t) * E + e;
+                    if (at < D) {
+                        const float a = r > 0 ? sums[at] : 0.0f, b = r > 0 ? sums[D + at] : 0.0f;
+                        to[at] = a + dw[c][e];
+                        to[D + at] = b + db[c][e];
+                    }
+                }
+        }
+    }
+}
+
+// Rows of any length.
+template <class X, class P>
+__global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormParams p)
+{
+    __shared__ float scratch[2 * 16];
+    const int64_t row = blockIdx.x;
+    const int D = (int)p.D;
+    const X *x = static_cast<const X *>(p.x) + row * p.ldx, *dy = static_cast<const X *>(p.dy) + row * p.lddy;
+    const P *w = static_cast<const P *>(p.weight);
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float s[2] = {0.0f, 0.0f};
+    for (int i = threadIdx.x; i < D; i += 1024) {
+        const float g = (float)dy[i] * (w ? (float)w[i] : 1.0f);
+        s[0] += g;
+        s[1] += g * (((float)x[i] - mean) * rstd);
+    }
+    row_sums<1024, 2>(s, scratch);
+    const float m0 = s[0] / (float)D, m1 = s[1] / (float)D;
+    X *dx = static_cast<X *>(p.dx) + row * p.lddx;
+    for (int i = threadIdx.x; i < D; i += 1024) {
+        const float g = (float)dy[i] * (w ? (float)w[i] : 1.0f), xh = ((float)x[i] - mean) * rstd;
+        dx[i] = (X)(rstd * (g - m0 - xh * m1));
+    }
+}
+// ... their dw and db: a thread has one column of the rows blockIdx.y, blockIdx.y + gridDim.y, ..
+template <class X>
+__global__ void __launch_bounds__(256) norm_columns_kernel(const NormParams p)
+{
+    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (col >= p.D) return;
+    float dw = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.y; row < p.M; row += gridDim.y) {
+        const float dy = (float)static_cast<const X *>(p.dy)[row * p.lddy + col];
+        dw += dy * (((float)static_cast<const X *>(p.x)[row * p.ldx + col] - p.mean[row]) * p.rstd[row]);
+        db += dy;
+    }
+    p.partial[((int64_t)blockIdx.y * 2) * p.D + col] = dw;
+    p.partial[((int64_t)blockIdx.y * 2 + 1) * p.D + col] = db;
+}
+
+// dw, db = the partial sums added in order: 64 columns per workgroup, 16 waves with a run of the partial sums each.
+template <class P>
+__global__ void __launch_bounds__(1024) norm_params_kernel(const NormParams p, int partials)
+{
+    __shared__ float sums[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    const int which = blockIdx.y;                             // 0: dw, 1: db
+    P *out = static_cast<P *>(which ? p.dbias : p.dweight);
+    if (!out) return;                                         // the whole workgroup
+    const int run = (partials + 15) / 16, first = wave * run, end = min(first + run, partials);
+    float s = 0.0f;
+    if (col < p.D)
+        for (int i = first; i < end; ++i) s += p.partial[((int64_t)i * 2 + which) * p.D + col];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && col < p.D) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += sums[i][lane];
+        out[col] = (P)s;
+    }
+}
+
+// Threads per row: the power of two, 64 to 1024, that holds it in 16 elements each.
+int threads_of(int64_t D)
+{
+    int t = 64;
+    while (t < 1024 && (int64_t)t * kPerThread < D) t *= 2;
+    return t;
+}
+
+template <class X, class P, int T>
+hipError_t forward_of(const NormParams &p, hipStream_t stream)
+{
+    constexpr int NT = T < 256 ? 256 : T;
+    const int64_t grid = (p.M + NT / T - 1) / (NT / T);
+    hipLaunchKernelGGL((norm_kernel<X, P, T>), dim3((unsigned)grid), dim3(NT), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <class X, class P>
+hipError_t forward(const NormParams &p, hipStream_t stream)
+{
+    if (p.D > kMaxRow) {
+        hipLaunchKernelGGL((norm_long_kernel<X, P>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
+        return hipGetLastError();
+    }
+    switch (threads_of(p.D)) {
+        case 64: return forward_of<X, P, 64>(p, stream);
+        case 128: return forward_of<X, P, 128>(p, stream);
+        case 256: return forward_of<X, P, 256>(p, stream);
+        case 512: return forward_of<X, P, 512>(p, stream);
+        default: return forward_of<X, P, 1024>(p, stream);
+    }
+}
+
+// T threads per row: dx, and with PARAMS the partial sums of dw and db as well.
+template <class X, class P, int T, bool PARAMS>
+hipError_t backward_of(const NormParams &p, int64_t grid, hipStream_t stream)
+{
+    constexpr int NT = T > kGradThreads ? T : kGradThreads, R = NT / T;
+    const int rounds = (int)((p.M + grid * R - 1) / (grid * R));
+    const size_t lds = PARAMS && R > 1 ? (size_t)p.D * 2 * sizeof(float) : 0;        // at most 32 KiB: R > 1 ends with D = 4096
+    hipLaunchKernelGGL((norm_grad_kernel<X, P, T, PARAMS>), dim3((unsigned)grid), dim3(NT), lds, stream, p, rounds);
+    return hipGetLastError();
+}
+
+template <class X, class P, int T>
+hipError_t backward_short(const NormParams &p, hipStream_t stream)
+{
+    if (p.dweight || p.dbias) return backward_of<X, P, T, true>(p, norm_partials(p.M, p.D), stream);
+    const int64_t rows = kGradThreads / T, grid = (p.M + rows - 1) / rows;
+    return backward_of<X, P, T, false>(p, grid < 2048 ? grid : 2048, stream);
+}
+
+// Rows of more than kMaxGradRow elements: with both sums beside the row a thread would need more registers than it has (16 elements in each of
+// 1024 threads: 38 spilled), so dw and db are a pass of their own over x and dy.
+template <class X, class P>
+hipError_t backward_long(const NormParams &p, hipStream_t stream)
+{
+    hipError_t e = hipSuccess;
+    if (p.dx && p.D <= kMaxRow) {
+        e = backward_of<X, P, 1024, false>(p, p.M < 2048 ? p.M : 2048, stream);
+    } else if (p.dx) {
+        hipLaunchKernelGGL((norm_grad_long_kernel<X, P>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || !(p.dweight || p.dbias)) return e;
+    hipLaunchKernelGGL((norm_columns_kernel<X>), dim3((unsigned)((p.D + 255) / 256), (unsigned)norm_partials(p.M, p.D)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <class X, class P>
+hipError_t backward(const NormParams &p, hipStream_t stream)
+{
+    const bool params = p.dweight || p.dbias;
+    hipError_t e = hipSuccess;
+    if (p.M > 0 && (p.dx || params)) {
+        if (p.D > kMaxGradRow) e = backward_long<X, P>(p, stream);
+        else switch (threads_of(p.D)) {
+            case 64: e = backward_short<X, P, 64>(p, stream); break;
+            case 128: e = backward_short<X, P, 128>(p, stream); break;
+            case 256: e = backward_short<X, P, 256>(p, stream); break;
+            default: e = backward_short<X, P, 512>(p, stream); break;
+        }
+    }
+    if (e != hipSuccess || !params) return e;
+    hipLaunchKernelGGL((norm_params_kernel<P>), dim3((unsigned)((p.D + 63) / 64), 2), dim3(1024), 0, stream, p, (int)norm_partials(p.M, p.D));      // no rows: zeros
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Workgroups of the backward pass: one per CU of the 256, fewer where there are not as many rows (a workgroup takes kGradThreads / T at a time).
+int64_t norm_partials(int64_t M, int64_t D)
+{
+    if (M <= 0) return 0;
+    if (D > kMaxGradRow) return M < 64 ? M : 64;
+    const int64_t rows = kGradThreads / threads_of(D), n = (M + rows - 1) / rows;
+    return n < 256 ? n : 256;
+}
+
+hipError_t launch_norm(const NormParams &p, hipStream_t stream)
+{
+    if (p.M == 0) return hipSuccess;
+    if (p.x_type == ATB_TYPE_F32) return p.w_type == ATB_TYPE_F32 ? forward<float, float>(p, stream) : forward<float, __bf16>(p, stream);
+    return p.w_type == ATB_TYPE_F32 ? forward<__bf16, float>(p, stream) : forward<__bf16, __bf16>(p, stream);
+}
+
+hipError_t launch_norm_backward(const NormParams &p, hipStream_t stream)
+{
+    if (p.x_type == ATB_TYPE_F32) return p.w_type == ATB_TYPE_F32 ? backward<float, float>(p, stream) : backward<float, __bf16>(p, stream);
+    return p.w_type == ATB_TYPE_F32 ? backward<__bf16, float>(p, stream) : backward<__bf16, __bf16>(p, stream);
+}
+
+}  // namespace atb

@@ -1,0 +1,104 @@
+// 4-bit weights with group scales: quantiser and decoder.  Bound: HBM.
+// w = s (q - z), q and z in 0 .. 15; a group is G neighbouring k of one row with a scale in bf16 and, if kept, a zero point.
+#include "atb_device.h"
+#include "atb_layers.h"
+
+namespace atb {
+namespace {
+
+// A group is 8 (G = 32) to 32 (G = 128) lanes of four k each.  s is rounded to bf16 first and the codes are taken with the rounded one.
+template <class X, int G, bool ZEROS>
+__global__ void __launch_bounds__(256) q4_quantize_kernel(const X *__restrict__ w, int64_t ldw, uint8_t *__restrict__ packed, uint16_t *__restrict__ scales,
+                                                          uint8_t *__restrict__ zeros, int64_t N, int64_t K)
+{
+    constexpr int LANES = G / 4;
+    const int64_t quads = K / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool live = at < N * quads;                        // whole groups: K % G == 0
+    const int64_t n = live ? at / quads : 0, k = live ? at % quads * 4 : 0;
+    float x[4], hi = 0.0f, lo = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = live ? (float)w[n * ldw + k + e] : 0.0f;
+        hi = fmaxf(hi, x[e]);
+        lo = fminf(lo, x[e]);
+    }
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) {
+        hi = fmaxf(hi, __shfl_xor(hi, d));
+        lo = fminf(lo, __shfl_xor(lo, d));
+    }
+    const float step = ZEROS ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f;
+    union { __bf16 b; uint16_t w; } s;
+    s.b = (__bf16)step;
+    const float scale = (float)s.b;
+    float z = 8.0f;
+    if (ZEROS) z = scale > 0.0f ? fminf(fmaxf(rintf(-lo / scale), 0.0f), 15.0f) : 0.0f;
+    unsigned code = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float c = scale > 0.0f ? fminf(fmaxf(rintf(x[e] / scale) + z, 0.0f), 15.0f) : z;
+        code |= (unsigned)c << (4 * e);
+    }
+    if (!live) return;
+    *reinterpret_cast<uint16_t *>(packed + n * (K / 2) + k / 2) = (uint16_t)code;
+    if (k % G == 0) {
+        scales[n * (K / G) + k / G] = s.w;
+        if (ZEROS) zeros[n * (K / G) + k / G] = (uint8_t)z;
+    }
+}
+
+// Eight k per thread.
+template <class X>
+__global__ void __launch_bounds__(256) q4_decode_kernel(const uint8_t *__restrict__ packed, const uint16_t *__restrict__ scales, const uint8_t *__restrict__ zeros,
+                                                        X *__restrict__ out, int64_t N, int64_t K, int group)
+{
+    const int64_t eights = K / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= N * eights) return;
+    const int64_t n = at / eights, k = at % eights * 8, g = n * (K / group) + k / group;
+    const unsigned code = *reinterpret_cast<const unsigned *>(packed + n * (K / 2) + k / 2);
+    const float s = __uint_as_float((unsigned)scales[g] << 16), z = zeros ? (float)zeros[g] : 8.0f;
+    X v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (X)(s * ((float)((code >> (4 * e)) & 15u) - z));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[n * K + k + e] = v[e];
+}
+
+template <class X, int G>
+hipError_t quantize(const void *w, int64_t ldw, uint8_t *packed, uint16_t *scales, uint8_t *zeros, int64_t N, int64_t K, hipStream_t stream)
+{
+    const int64_t grid = (N * (K / 4) + 255) / 256;
+    if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (zeros) hipLaunchKernelGGL((q4_quantize_kernel<X, G, true>), dim3((unsigned)grid), dim3(256), 0, stream, static_cast<const X *>(w), ldw, packed, scales, zeros, N, K);
+    else hipLaunchKernelGGL((q4_quantize_kernel<X, G, false>), dim3((unsigned)grid), dim3(256), 0, stream, static_cast<const X *>(w), ldw, packed, scales, zeros, N, K);
+    return hipGetLastError();
+}
+
+template <class X>
+hipError_t quantize(const void *w, int64_t ldw, uint8_t *packed, uint16_t *scales, uint8_t *zeros, int64_t N, int64_t K, int group, hipStream_t stream)
+{
+    if (group == 32) return quantize<X, 32>(w, ldw, packed, scales, zeros, N, K, stream);
+    if (group == 64) return quantize<X, 64>(w, ldw, packed, scales, zeros, N, K, stream);
+    return quantize<X, 128>(w, ldw, packed, scales, zeros, N, K, stream);
+}
+
+}  // namespace
+
+hipError_t launch_q4_quantize(const void *w, int w_type, int64_t ldw, uint8_t *packed, uint16_t *scales, uint8_t *zeros,
+                              int64_t N, int64_t K, int group, hipStream_t stream)
+{
+    if (w_type == ATB_TYPE_F32) return quantize<float>(w, ldw, packed, scales, zeros, N, K, group, stream);
+    return quantize<__bf16>(w, ldw, packed, scales, zeros, N, K, group, stream);
+}
+
+hipError_t launch_q4_decode(const uint8_t *packed, const uint16_t *scales, const uint8_t *zeros, void *out, int out_type,
+                            int64_t N, int64_t K, int group, hipStream_t stream)
+{
+    const int64_t grid = (N * (K / 8) + 255) / 256;
+    if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (out_type == ATB_TYPE_F32) hipLaunchKernelGGL((q4_decode_kernel<float>), dim3((unsigned)grid), dim3(256), 0, stream, packed, scales, zeros, static_cast<float *>(out), N, K, group);
+    else hipLaunchKernelGGL((q4_decode_kernel<__bf16>), dim3((unsigned)grid), dim3(256), 0, stream, packed, scales, zeros, static_cast<__bf16 *>(out), N, K, group);
+    return hipGetLastError();
+}
+
+}  // namespace atb

@@ -1,0 +1,591 @@
+// bf16 products in tiles: the kernel behind the gated block and its gradients (atb_ffn.hip, atb_ffn_grad.hip).
+//
+// C tile = A tile x B tile with fp32 accumulation in MFMA accumulators; K-steps of 64, two LDS buffers per operand, filled by
+// requests that go from memory straight into LDS.  An operand whose reduction index is contiguous lies in LDS as rows of 64 k
+// (128 bytes) and is read with plain 16-byte reads; one whose other index is contiguous lies there as 64 rows of k and is read
+// through the transposing read, so no operand of the backward pass is ever transposed in memory.
+//
+// Time line of a K-step s (its tile is in LDS buffer s % 2, its first k-slice of 32 already in registers):
+//   first half    the MFMAs of k-slice 0; the fragments of k-slice 1 are read under them
+//   barrier       every wave has all of tile s in registers, and tile s + 1, asked for one whole K-step ago, is complete
+//   second half   the MFMAs of k-slice 1; tile s + 2 is asked for, into the buffer that tile s has left, and the fragments of
+//                 k-slice 0 of tile s + 1 are read under them
+// so after the barrier no MFMA waits for LDS.
+#pragma once
+
+#include "atb_activation.h"
+#include "atb_layers.h"
+
+namespace atb {
+
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+template <int TM_, int TN_, int WM_, int WN_>
+struct TileShape {
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;       // tile, wave grid
+    static constexpr int NT = WM * WN * 64;
+    static constexpr int TK = 64;
+    static constexpr int MI = TM / WM / 16, NI = TN / WN / 16;         // 16 x 16 blocks of a wave
+    static constexpr int A_BYTES = TM * TK * 2, B_BYTES = TN * TK * 2;
+    static constexpr int LDS_BYTES = 2 * (A_BYTES + B_BYTES);
+    static constexpr int RA = A_BYTES / 16 / NT, RB = B_BYTES / 16 / NT;   // requests per thread and tile
+    static_assert(TN / WN == 64, "a wave's columns: 64, of a gated product 32 of each weight");
+    static_assert(RA * NT * 16 == A_BYTES && RB * NT * 16 == B_BYTES, "whole requests");
+};
+
+// Where a thread's requests for a tile of an operand read.  R: rows (or, with ROWS, columns) of the operand in the tile.  A request covers as
+// many rows of LDS in every turn, so request i reads `pitch` bytes behind request i - 1.
+// ROWS: 64 rows of k; chunk c (16 bytes) of row k lies at c ^ swizzle(k), so that the rows that a transposing read touches fall into different banks
+// (per 32 lanes the rows k0 .. k0 + 3 and k0 + 8 .. k0 + 11 of 16 columns).  Otherwise rows of 64 k; chunk c of row r lies at c ^ (r % 8).
+template <int R, int NT, bool ROWS>
+struct Requests {
+    static constexpr int CPR = ROWS ? R / 8 : 8;          // chunks per LDS row
+    static constexpr int STEP = NT / CPR;                 // LDS rows of a request
+    static_assert(!ROWS || (R >= 128 && STEP % 16 == 0), "the swizzle repeats after 16 rows of 16 chunks or more");
+    static_assert(ROWS || STEP % 8 == 0, "... and after 8");
+    int first, pitch;
+
+    static ATB_DEV int swizzle(int row) { return ROWS ? ((row & 3) << 2) | (((row >> 3) & 1) << 1) : row & 7; }
+    static ATB_DEV int chunk(int tid) { return (tid % CPR) ^ swizzle(tid / CPR); }
+
+    ATB_DEV void place(int tid, int64_t ld)
+    {
+        first = (tid / CPR) * (int)(ld * 2) + chunk(tid) * 16;
+        pitch = __builtin_amdgcn_readfirstlane(STEP * (int)(ld * 2));
+    }
+    // The last tile of a reduction that is not a multiple of 64: what follows the end of a row of K-contiguous elements is the next row's, so
+    // the lanes of those chunks ask for nothing (K % 8 == 0: a chunk is inside or outside).  Rows of k end with the operand.
+    ATB_DEV void cut(int tid, int k_left)
+    {
+        if constexpr (!ROWS)
+            if (chunk(tid) * 8 >= k_left) first |= (int)0x80000000;       // past the end of every descriptor: reads as zero
+    }
+    template <int i> ATB_DEV int offset() const { return first + i * pitch; }
+};
+
+// A descriptor's four dwords, advanced by whole K-steps.
+struct Source {
+    const char *ptr;
+    int64_t left;          // bytes from ptr to the end of the operand
+    ATB_DEV intx4 words() const
+    {
+        const uint64_t a = reinterpret_cast<uint64_t>(ptr);
+        const int64_t n = left < 0 ? 0 : left > 0x7fffffff ? 0x7fffffff : left;
+        return intx4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF),
+                     __builtin_amdgcn_readfirstlane((int)n), kRsrcFlags};
+    }
+};
+
+template <class S, bool AT, bool BROWS, int EPI>
+struct Tile {
+    static constexpr bool GATED = EPI == kGated || EPI == kGatedKeep;
+    const TileParams &p;
+    const int tid, lane, wave, wm, wn;
+    int m0, n0, problem;
+    typedef Requests<S::TM, S::NT, AT> ARequests;
+    typedef Requests<S::TN, S::NT, BROWS> BRequests;
+    ARequests a_off;
+    BRequests b_off, b2_off;
+    Source a_src, b_src, b2_src;           // b2: the up weight of a gated product
+    intx4 a_words, b_words, b2_words;
+    int k_left, segment;                   // reduction left to ask for in this segment
+    int req_step, steps;                   // K-steps asked for, all of them
+    const char *a_rd[AT ? S::MI : 2], *b_rd[BROWS ? S::NI : 2];
+    char *a_req, *b_req;
+    floatx4 acc[S::MI][S::NI];
+    bf16x8 af[2][S::MI], bf[2][S::NI];
+
+    ATB_DEV Tile(const TileParams &p_, char *lds, int m0_, int n0_, int problem_)
+        : p(p_), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)), wm(wave / S::WN), wn(wave % S::WN),
+          m0(m0_), n0(n0_), problem(problem_)
+    {
+        char *a_lds = lds, *b_lds = lds + 2 * S::A_BYTES;
+        a_req = a_lds + wave * 1024;
+        b_req = b_lds + wave * 1024;
+        const int q = lane >> 4, c = lane & 15;
+        if constexpr (AT) {
+            rows_addresses<S::MI, S::TM>(a_rd, a_lds, wm * (S::TM / S::WM));
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) a_rd[ks] = a_lds + (wm * (S::TM / S::WM) + c) * 128 + (((4 * ks + q) ^ (c & 7)) * 16);
+        }
+        if constexpr (BROWS) {
+            rows_addresses<S::NI, S::TN>(b_rd, b_lds, wn * 64);
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) b_rd[ks] = b_lds + (wn * (GATED ? 32 : 64) + c) * 128 + (((4 * ks + q) ^ (c & 7)) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        steps = p.segments * ((p.K + S::TK - 1) / S::TK);
+        req_step = 0;
+        segment = -1;
+        open();
+    }
+
+    // The transposing read of 16 columns and 8 k: in a group of 16 lanes, lane i addresses columns 4 (i % 4) .. + 3 of row i / 4 and lane j
+    // receives column j of the four rows; group g takes rows 8 g .. 8 g + 3 of the k-slice, a second read 4 rows on the others.
+    template <int BLOCKS, int R>
+    ATB_DEV void rows_addresses(const char *(&rd)[BLOCKS], const char *base, int first) const
+    {
+        const int j = lane & 15, row = 8 * (lane >> 4) + (j >> 2);
+#pragma unroll
+        for (int e = 0; e < BLOCKS; ++e) {
+            const int chunk = first / 8 + 2 * e + ((j & 3) >> 1);
+            rd[e] = base + row * (R * 2) + ((chunk ^ (Requests<R, S::NT, true>::swizzle(row))) * 16) + (j & 1) * 8;
+        }
+    }
+
+    // ---- requests
+
+    // Bytes from an operand's element (row, col) to its end; rows of `cols` elements, ld apart.
+    static ATB_DEV int64_t bytes_left(int64_t rows, int64_t cols, int64_t ld, int64_t row, int64_t col) { return ((rows - 1 - row) * ld + cols - col) * 2; }
+
+    // The next segment's operands.
+    ATB_DEV void open()
+    {
+        ++segment;
+        k_left = p.K;
+        const int s = p.segments > 1 ? segment : problem;
+        if constexpr (AT) a_src = {reinterpret_cast<const char *>(p.A[s] + m0), bytes_left(p.K, p.M, p.lda[s], 0, m0)};
+        else a_src = {reinterpret_cast<const char *>(p.A[s] + (int64_t)m0 * p.lda[s]), bytes_left(p.M, p.K, p.lda[s], m0, 0)};
+        a_off.place(tid, p.lda[s]);
+        if constexpr (GATED) {
+            // rows 0 .. TN / 2 - 1 of the LDS tile are columns of the gate weight, the others the same columns of the up weight
+            b_src = {reinterpret_cast<const char *>(p.B[0] + (int64_t)n0 * p.ldb[0]), bytes_left(p.N, p.K, p.ldb[0], n0, 0)};
+            b2_src = {reinterpret_cast<const char *>(p.B[1] + (int64_t)n0 * p.ldb[1]), bytes_left(p.N, p.K, p.ldb[1], n0, 0)};
+            b_off.place(tid, p.ldb[0]);
+            b2_off.place(tid, p.ldb[1]);
+        } else {
+            if constexpr (BROWS) b_src = {reinterpret_cast<const char *>(p.B[s] + n0), bytes_left(p.K, p.N, p.ldb[s], 0, n0)};
+            else b_src = {reinterpret_cast<const char *>(p.B[s] + (int64_t)n0 * p.ldb[s]), bytes_left(p.N, p.K, p.ldb[s], n0, 0)};
+            b_off.place(tid, p.ldb[s]);
+        }
+        cut_last();
+        make_words();
+    }
+
+    ATB_DEV void cut_last()
+    {
+        if (k_left < S::TK) {
+            a_off.cut(tid, k_left);
+            b_off.cut(tid, k_left);
+            if constexpr (GATED) b2_off.cut(tid, k_left);
+        }
+    }
+
+    ATB_DEV void make_words()
+    {
+        a_words = a_src.words();
+        b_words = b_src.words();
+        if constexpr (GATED) b2_words = b2_src.words();
+    }
+
+    // After the last request of a tile: one K-step on.  Past the last one the descriptors are empty: nothing is asked of memory.
+    ATB_DEV void advance()
+    {
+        ++req_step;
+        k_left -= S::TK;
+        if (req_step >= steps) {
+            a_src.left = b_src.left = 0;
+            if constexpr (GATED) b2_src.left = 0;
+            make_words();
+        } else if (k_left <= 0) {
+            open();
+        } else {
+            const int s = p.segments > 1 ? segment : problem;
+            const int64_t da = AT ? S::TK * 2 * p.lda[s] : S::TK * 2, db = BROWS ? S::TK * 2 * p.ldb[s] : S::TK * 2;
+            a_src.ptr += da; a_src.left -= da;
+            b_src.ptr += db; b_src.left -= db;
+            if constexpr (GATED) { b2_src.ptr += db; b2_src.left -= db; }
+            cut_last();
+            make_words();
+        }
+    }
+
+    // 16 bytes per lane from memory to LDS.  By hand, so that the compiler does not wait for it before every read of LDS that follows; the wait is
+    // the one ahead of the barrier.  M0, the LDS address, is put back: the compiler is not told about it.
+    static ATB_DEV void request_one(intx4 words, int off, const char *to)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const unsigned addr = (unsigned)reinterpret_cast<uintptr_t>(to);
+        int saved;
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved)
+                     : "s"(__builtin_amdgcn_readfirstlane((int)addr)), "v"(off), "s"(words) : "memory");
+#endif
+    }
+
+    // Request r (0 .. RA + RB - 1) of the next tile into buffer `buf`.
+    template <int r, int buf>
+    ATB_DEV void request()
+    {
+        if constexpr (r < S::RA) {
+            request_one(a_words, a_off.template offset<r>(), a_req + buf * S::A_BYTES + r * S::NT * 16);
+        } else {
+            constexpr int i = r - S::RA;
+            char *to = b_req + buf * S::B_BYTES + i * S::NT * 16;
+            if constexpr (GATED && i >= S::RB / 2) request_one(b2_words, b2_off.template offset<i - S::RB / 2>(), to);
+            else request_one(b_words, b_off.template offset<i>(), to);
+        }
+        if constexpr (r == S::RA + S::RB - 1) advance();
+    }
+
+    template <int buf, int r = 0>
+    ATB_DEV void request_all()
+    {
+        if constexpr (r < S::RA + S::RB) {
+            request<r, buf>();
+            request_all<buf, r + 1>();
+        }
+    }
+
+    // ---- LDS -> registers
+
+    template <int R>
+    static ATB_DEV bf16x8 read_rows(const char *src)
+    {
+        bf16x8 r = {};
+#if defined(__HIP_DEVICE_COMPILE__)
+        typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+        union { shortx4 s[2]; bf16x8 b; } u;
+        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(src));
+        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(src + 4 * R * 2));
+        r = u.b;
+#endif
+        return r;
+    }
+    // Fragment f of a k-slice in the order of first use
+    template <int ks, int buf, int f>
+    ATB_DEV void read_frag()
+    {
+        // a0, b0 .. b(NI-1), a1 .. a(MI-1)
+        if constexpr (f >= 1 && f <= S::NI) {
+            constexpr int j = f - 1;
+            if constexpr (BROWS) bf[ks][j] = read_rows<S::TN>(b_rd[j] + buf * S::B_BYTES + ks * 32 * S::TN * 2);
+            else bf[ks][j] = *reinterpret_cast<const bf16x8 *>(b_rd[ks] + buf * S::B_BYTES + (GATED && j >= 2 ? S::TN / 2 * 128 + (j - 2) * 2048 : j * 2048));
+        } else {
+            constexpr int i = f == 0 ? 0 : f - S::NI;
+            if constexpr (AT) af[ks][i] = read_rows<S::TM>(a_rd[i] + buf * S::A_BYTES + ks * 32 * S::TM * 2);
+            else af[ks][i] = *reinterpret_cast<const bf16x8 *>(a_rd[ks] + buf * S::A_BYTES + i * 2048);
+        }
+    }
+    static constexpr int FRAGS = S::MI + S::NI;
+    template <int ks, int buf, int f = 0>
+    ATB_DEV void read_all()
+    {
+        if constexpr (f < FRAGS) {
+            read_frag<ks, buf, f>();
+            read_all<ks, buf, f + 1>();
+        }
+    }
+
+    // ---- a half K-step: MI x NI MFMAs and their side work
+
+    template <int ks>
+    ATB_DEV void mfma(int i, int j)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[ks][j], af[ks][i], acc[i][j], 0, 0, 0);
+#endif
+    }
+    static constexpr int SLOTS = S::MI * S::NI;
+    static constexpr int REQS = S::RA + S::RB;
+
+    template <int buf, int t = 0>
+    ATB_DEV void first_half()
+    {
+        if constexpr (t < SLOTS) {
+            mfma<0>(t / S::NI, t % S::NI);
+            // fragment f behind MFMA 2 f (1 f where there are fewer MFMAs)
+            constexpr int every = SLOTS >= 2 * FRAGS ? 2 : 1;
+            if constexpr (t % every == 0 && t / every < FRAGS) read_frag<1, buf, t / every>();
+            __builtin_amdgcn_sched_barrier(0);
+            first_half<buf, t + 1>();
+        }
+    }
+    template <int buf, int t = 0>
+    ATB_DEV void second_half()
+    {
+        if constexpr (t < SLOTS) {
+            mfma<1>(t / S::NI, t % S::NI);
+            constexpr int side = FRAGS + REQS, per = (side + SLOTS - 1) / SLOTS;
+            side_work<buf, t * per, t * per + per>();
+            __builtin_amdgcn_sched_barrier(0);
+            second_half<buf, t + 1>();
+        }
+    }
+    // requests and reads in turns
+    template <int buf, int from, int to>
+    ATB_DEV void side_work()
+    {
+        if constexpr (from < to && from < FRAGS + REQS) {
+            constexpr int both = 2 * (REQS < FRAGS ? REQS : FRAGS);
+            if constexpr (from < both) {
+                if constexpr (from % 2 == 0) request<from / 2, buf>();
+                else read_frag<0, buf ^ 1, from / 2>();
+            } else if constexpr (REQS < FRAGS) {
+                read_frag<0, buf ^ 1, from - REQS>();
+            } else {
+                request<from - FRAGS, buf>();
+            }
+            side_work<buf, from + 1, to>();
+        }
+    }
+
+    template <int younger>
+    static ATB_DEV void wait_requests()
+    {
+        static_assert(younger >= 0 && younger < 64, "vmcnt is a 6-bit counter");
+        __builtin_amdgcn_s_waitcnt((younger & 15) | (7 << 4) | (15 << 8) | ((younger >> 4) << 14));
+    }
+
+    template <int buf>
+    ATB_DEV void step()
+    {
+        first_half<buf>();
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        second_half<buf>();
+    }
+
+    ATB_DEV void multiply()
+    {
+        request_all<0>();
+        request_all<1>();
+        wait_requests<REQS>();
+        asm volatile("s_barrier" ::: "memory");
+        read_all<0, 0>();
+        for (int s = 0; s < steps; s += 2) {
+            step<0>();
+            if (s + 1 == steps) break;
+            step<1>();
+        }
+        wait_requests<0>();
+    }
+
+    // x, which the compiler is not to know ahead of this place: it would work out the addresses of the whole tile before the first store
+    static ATB_DEV int here(int x)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" : "+v"(x));
+#endif
+        return x;
+    }
+    // The bits of a sum, likewise: it would carry the accumulators round the K loop a second time, as integers
+    static ATB_DEV unsigned bits(float x)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" : "+v"(x));
+#endif
+        return __float_as_uint(x);
+    }
+
+    // ---- epilogue: a lane holds row 16 i + lane % 16 of the wave's part and, of column block j, columns 4 (lane / 16) .. + 3.  One swap of
+    // lanes per register makes of two neighbouring column blocks eight consecutive columns per lane.
+
+    static ATB_DEV void swap_halves(unsigned &x, unsigned &y)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+        const uintx2 r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+        x = r.x;
+        y = r.y;
+#endif
+    }
+    ATB_DEV int piece_col() const { return ((lane >> 4) & 1) * 16 + (lane >> 5) * 8; }
+
+    static ATB_DEV unsigned pack(float a, float b)
+    {
+        union { bf16x2 v; unsigned w; } u;
+        u.v = bf16x2{(__bf16)a, (__bf16)b};
+        return u.w;
+    }
+    // column blocks x, y of a row block -> this lane's eight columns as bf16
+    static ATB_DEV intx4 piece(const floatx4 &x, const floatx4 &y)
+    {
+        unsigned a0 = pack(x[0], x[1]), a1 = pack(x[2], x[3]), b0 = pack(y[0], y[1]), b1 = pack(y[2], y[3]);
+        swap_halves(a0, b0);
+        swap_halves(a1, b1);
+        return intx4{(int)a0, (int)a1, (int)b0, (int)b1};
+    }
+    // (rows of C begin at multiples of 16 bytes: N, the pitch and the pointer are multiples of 8 elements)
+    ATB_DEV void store(uint16_t *c, int64_t ld, int row, int col, intx4 v) const
+    {
+        if (row < p.M && col < p.N) *reinterpret_cast<intx4 *>(c + (int64_t)row * ld + col) = v;
+    }
+
+    // g and u as the backward pass needs them, 24 of their 32 bits (16 of the mantissa): plane 0 has the upper 16 of g, plane 1 those of u, plane 2 the next byte
+    // of g and, above it, of u.  In bf16, 16 bits each, their rounding makes as large a part of the error of dx and the weights' gradients as the
+    // rounding of dg and du and that of the result (3.1e-3 in the 2-norm instead of 2.4e-3).
+    static ATB_DEV unsigned bytes(unsigned hi, unsigned lo, unsigned select)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        return __builtin_amdgcn_perm(hi, lo, select);
+#else
+        return 0;
+#endif
+    }
+    ATB_DEV void keep(int row, int col, const floatx4 &g0, const floatx4 &g1, const floatx4 &u0, const floatx4 &u1) const
+    {
+        unsigned w[3][2][2];            // plane, column block, pair of columns
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const floatx4 &g = b ? g1 : g0, &u = b ? u1 : u0;
+                const unsigned ga = bits(g[2 * e]), gb = bits(g[2 * e + 1]), ua = bits(u[2 * e]), ub = bits(u[2 * e + 1]);
+                w[0][b][e] = bytes(gb, ga, 0x07060302u);
+                w[1][b][e] = bytes(ub, ua, 0x07060302u);
+                w[2][b][e] = bytes(bytes(ub, gb, 0x0c0c0501u), bytes(ua, ga, 0x0c0c0501u), 0x05040100u);
+            }
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            swap_halves(w[n][0][0], w[n][1][0]);
+            swap_halves(w[n][0][1], w[n][1][1]);
+            store(p.kept + n * ((int64_t)p.M * p.N), p.N, row, col, intx4{(int)w[n][0][0], (int)w[n][0][1], (int)w[n][1][0], (int)w[n][1][1]});
+        }
+    }
+    ATB_DEV void kept(int row, int col, float (&g)[8], float (&u)[8]) const
+    {
+        intx4 w[3];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) w[n] = *reinterpret_cast<const intx4 *>(p.kept + n * ((int64_t)p.M * p.N) + (int64_t)row * p.N + col);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned gh = (unsigned)w[0][e], uh = (unsigned)w[1][e], lo = (unsigned)w[2][e];
+            g[2 * e] = __uint_as_float(bytes(gh, lo, 0x0504000cu));
+            g[2 * e + 1] = __uint_as_float(bytes(gh, lo, 0x0706020cu));
+            u[2 * e] = __uint_as_float(bytes(uh, lo, 0x0504010cu));
+            u[2 * e + 1] = __uint_as_float(bytes(uh, lo, 0x0706030cu));
+        }
+    }
+
+    ATB_DEV void finish_plain()
+    {
+        const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), col0 = n0 + wn * 64 + piece_col();
+        uint16_t *c = p.C[problem];
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NI; j += 2) store(c, p.ldc, row0 + 16 * i, col0 + 16 * j, piece(acc[i][j], acc[i][j + 1]));
+    }
+
+    ATB_DEV void finish_gated()
+    {
+        const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), col = n0 + wn * 32 + piece_col();
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i) {
+            const int row = here(row0 + 16 * i);
+            if constexpr (EPI == kGatedKeep) keep(row, col, acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+            floatx4 h[2];
+            with_activation(p.act, [&](auto a) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[j][e] = activate<decltype(a)::value>(acc[i][j][e]) * acc[i][j + 2][e];
+            });
+            store(p.C[0], p.ldc, row, col, piece(h[0], h[1]));
+            __builtin_amdgcn_sched_barrier(0);             // row block by row block: registers
+        }
+    }
+
+    ATB_DEV void finish_grad()
+    {
+        const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), col0 = n0 + wn * 64 + piece_col();
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NI; j += 2) {
+                const int row = here(row0 + 16 * i), col = col0 + 16 * j;
+                float d[8];                                    // dh of this lane's eight columns
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    unsigned x = bits(acc[i][j][e]), y = bits(acc[i][j + 1][e]);
+                    swap_halves(x, y);
+                    d[e] = __uint_as_float(x);
+                    d[4 + e] = __uint_as_float(y);
+                }
+                if (row < p.M && col < p.N) {
+                    float g[8], u[8];
+                    kept(row, col, g, u);
+                    bf16x8 dg, du;
+                    with_activation(p.act, [&](auto act) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float a, slope;
+                            activate_grad<decltype(act)::value>(g[e], a, slope);
+                            dg[e] = (__bf16)(d[e] * u[e] * slope);
+                            du[e] = (__bf16)(d[e] * a);
+                        }
+                    });
+                    const int64_t to = (int64_t)row * p.ldc + col;
+                    *reinterpret_cast<bf16x8 *>(p.C[0] + to) = dg;
+                    *reinterpret_cast<bf16x8 *>(p.C[1] + to) = du;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+
+    ATB_DEV void finish()
+    {
+        if constexpr (EPI == kStore) finish_plain();
+        else if constexpr (EPI == kGatedGrad) finish_grad();
+        else finish_gated();
+    }
+};
+
+// Tile of workgroup b: workgroups are dealt round-robin to the 8 XCDs, each with an L2 of its own; XCD x takes a contiguous run of tiles,
+// walked in bands of group_m tile rows, so that those resident on it share rows of A and columns of B.
+template <class S, bool GATED>
+ATB_DEV bool tile_of(const TileParams &p, int b, int &m0, int &n0)
+{
+    const int total = p.tiles_m * p.tiles_n, per_xcd = (total + 7) / 8;
+    const int t = (b % 8) * per_xcd + b / 8;
+    if (b / 8 >= per_xcd || t >= total) return false;
+    const int band_size = p.group_m * p.tiles_n, band = t / band_size, in_band = t % band_size;
+    const int rows = min(p.group_m, p.tiles_m - band * p.group_m);
+    m0 = (band * p.group_m + in_band % rows) * S::TM;
+    n0 = (in_band / rows) * (GATED ? S::TN / 2 : S::TN);
+    return true;
+}
+
+template <class S, bool AT, bool BROWS, int EPI>
+__global__ void __launch_bounds__(S::NT, S::NT == 512 ? 2 : 2) tile_kernel(const TileParams p)
+{
+    __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES];
+    int m0 = 0, n0 = 0;
+    if (!tile_of<S, (EPI == kGated || EPI == kGatedKeep)>(p, blockIdx.x, m0, n0)) return;
+    Tile<S, AT, BROWS, EPI> tile(p, lds, m0, n0, blockIdx.y);
+    tile.multiply();
+    tile.finish();
+}
+
+template <class S, bool AT, bool BROWS, int EPI>
+hipError_t launch_shape(TileParams &p, hipStream_t stream)
+{
+    constexpr int cols = EPI == kGated || EPI == kGatedKeep ? S::TN / 2 : S::TN;
+    p.tiles_m = (p.M + S::TM - 1) / S::TM;
+    p.tiles_n = (p.N + cols - 1) / cols;
+    p.group_m = 2048 / S::TM;
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
+    if (total > 0x7fffff00) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((tile_kernel<S, AT, BROWS, EPI>), dim3((unsigned)((total + 7) / 8 * 8), p.problems), dim3(S::NT), 0, stream, p);
+    return hipGetLastError();
+}
+
+typedef TileShape<256, 256, 2, 4> Tile256;
+typedef TileShape<128, 128, 2, 2> Tile128;
+
+// Tiles of 256 x 256, one workgroup per CU, or of 128 x 128, two per CU.
+template <bool AT, bool BROWS, int EPI>
+hipError_t launch_tiles(TileParams &p, hipStream_t stream)
+{
+    const int64_t n = EPI == kGated || EPI == kGatedKeep ? 2 * (int64_t)p.N : p.N;
+    const int64_t large = ((p.M + 255) / 256) * ((n + 255) / 256) * p.problems;
+    if (large >= 192) return launch_shape<Tile256, AT, BROWS, EPI>(p, stream);
+    return launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
+}
+
+}  // namespace atb

@@ -1,0 +1,177 @@
+"""Layer norm and its backward pass on the GPU against the formulas in 64 bits.
+
+Tolerances.  fp32 sums in trees of at most 2^10 lanes and chains of at most 32 elements per lane err by less than 2^-20 of the sum of the terms' sizes; the
+statistics, a difference and three products add a few 2^-24 of theirs.  A bf16 result adds its rounding, at most 2^-8 of its size."""
+import pytest
+import torch
+
+import paper_2511_16041_amd as atb
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -19
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def rounding(t):
+    return 2.0 ** -8 if t == BF16 else 2.0 ** -23
+
+
+def inputs(M, D, dtype, ptype, seed, affine="both", pad=0, offset=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    wide = torch.randn((M, D + pad), generator=g, device="cuda") * torch.exp(torch.randn((M, 1), generator=g, device="cuda")) + offset * torch.randn((M, 1), generator=g, device="cuda")
+    x = wide.to(dtype)
+    x[:, D:] = float("nan")                          # what lies between the rows is never used
+    dy = torch.randn((M, D + pad), generator=g, device="cuda").to(dtype)
+    dy[:, D:] = float("nan")
+    w = (1 + 0.3 * torch.randn(D, generator=g, device="cuda")).to(ptype) if affine != "none" else None
+    b = (0.3 * torch.randn(D, generator=g, device="cuda")).to(ptype) if affine == "both" else None
+    return x[:, :D], dy[:, :D], w, b
+
+
+def reference(x, dy, w, b, eps):
+    """Results in 64 bits and what each may be off."""
+    x, dy = x.double(), dy.double()
+    D = x.shape[1]
+    one = torch.ones(D, dtype=torch.float64, device="cuda")
+    wd, bd = (w.double() if w is not None else one), (b.double() if b is not None else 0 * one)
+    mean = x.sum(1, keepdim=True) / D
+    rstd = ((x - mean).square().sum(1, keepdim=True) / D + eps).rsqrt()
+    xh = (x - mean) * rstd
+    top = x.abs().amax(1, keepdim=True) * rstd       # an error of 2^-24 of x, in xh
+    e_xh = E * (xh.abs() + top)
+    y = xh * wd + bd
+    g = dy * wd
+    m0, m1 = g.sum(1, keepdim=True) / D, (g * xh).sum(1, keepdim=True) / D
+    dx = rstd * (g - m0 - xh * m1)
+    e_m1 = E * (g * xh).abs().mean(1, keepdim=True) + (g.abs() * e_xh).mean(1, keepdim=True)
+    return {"y": (y, e_xh * wd.abs() + E * (y.abs() + bd.abs())), "mean": (mean[:, 0], E * x.abs().amax(1)), "rstd": (rstd[:, 0], (E * rstd * (1 + top))[:, 0]),
+            "dx": (dx, rstd * (E * (g.abs() + g.abs().mean(1, keepdim=True) + xh.abs() * m1.abs()) + e_xh * m1.abs() + xh.abs() * e_m1)),
+            "dw": ((dy * xh).sum(0), E * (dy * xh).abs().sum(0) + (dy.abs() * e_xh).sum(0)), "db": (dy.sum(0), E * dy.abs().sum(0))}
+
+
+def close(got, want, name):
+    ref, tol = want
+    assert got.shape == ref.shape, name
+    limit = tol + rounding(got.dtype) * ref.abs() + 1e-30
+    off = (got.double() - ref).abs()
+    assert bool((off <= limit).all()), f"{name}: worst {float((off / limit).max())} of the tolerance"
+
+
+def run(x, dy, w, b, eps):
+    y, mean, rstd = atb.layer_norm(x, w, b, eps, stats=True)
+    dx, dw, db = atb.layer_norm_backward(dy, x, mean, rstd, w, bias=b is not None)
+    return {"y": y, "mean": mean, "rstd": rstd, "dx": dx, "dw": dw, "db": db}
+
+
+SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (9, 63), (33, 64), (17, 65), (64, 512), (7, 1000), (300, 1024), (9, 1025), (1, 4096), (600, 4096), (40, 5001), (700, 8192), (6, 8193),
+         (5, 9000), (3, 16384), (4, 16385), (70, 16390), (2, 40000), (4000, 96)]
+
+
+@pytest.mark.parametrize("dtype,ptype", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("M,D", SIZES)
+def test_forward_and_backward(M, D, dtype, ptype):
+    x, dy, w, b = inputs(M, D, dtype, ptype, seed=M * 7 + D)
+    want, got = reference(x, dy, w, b, 1e-5), run(x, dy, w, b, 1e-5)
+    for name in want:
+        close(got[name], want[name], name)
+    assert torch.equal(got["y"], atb.layer_norm(x, w, b))           # without statistics, default eps
+
+
+@pytest.mark.parametrize("affine", ["weight", "none"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,D,pad", [(37, 1000, 3), (5, 8192, 1), (3, 17000, 5), (130, 77, 51)])
+def test_strides_and_missing_parameters(M, D, pad, dtype, affine):
+    x, dy, w, b = inputs(M, D, dtype, dtype, 5, affine, pad)
+    want, got = reference(x, dy, w, b, 1e-5), run(x, dy, w, b, 1e-5)
+    assert got["db"] is None and (got["dw"] is None) == (w is None)
+    for name in ("y", "mean", "rstd", "dx") + (("dw",) if w is not None else ()):
+        close(got[name], want[name], name)
+
+
+def test_bias_without_a_weight():
+    x, dy, _, _ = inputs(50, 300, BF16, BF16, 6, "none")
+    b = torch.randn(300, device="cuda")
+    y, mean, rstd = atb.layer_norm(x, None, b, 1e-5, stats=True)
+    want = reference(x, dy, None, b, 1e-5)
+    close(y, want["y"], "y")
+    dx, dw, db = atb.layer_norm_backward(dy, x, mean, rstd, None, bias=True)
+    assert dw is None and db.dtype == BF16
+    close(dx, want["dx"], "dx")
+    close(db, want["db"], "db")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_far_off_centre(dtype):
+    """The variance is taken about the mean: rows whose mean is thousands of their deviation keep their digits."""
+    x, dy, w, b = inputs(20, 2048, dtype, dtype, 8, offset=3000.0)
+    want, got = reference(x, dy, w, b, 1e-5), run(x, dy, w, b, 1e-5)
+    for name in want:
+        close(got[name], want[name], name)
+
+
+def test_constant_rows_and_rows_that_are_not_finite():
+    x, dy, w, b = inputs(6, 700, F32, F32, 9)
+    x = x.clone()
+    x[1] = 3.0                        # variance 0: y is the bias
+    x[2, 5] = float("nan")
+    x[4, 699] = float("inf")
+    got = run(x, dy, w, b, 1e-5)
+    assert torch.equal(got["y"][1], b)
+    assert got["y"][[2, 4]].isnan().all() and got["dx"][[2, 4]].isnan().all()
+    rows = [0, 1, 3, 5]
+    want = reference(x[rows], dy[rows], w, b, 1e-5)
+    close(got["y"][rows], want["y"], "y")
+    close(got["dx"][rows], want["dx"], "dx")
+
+
+def test_no_rows():
+    w = torch.ones(96, device="cuda")
+    x = torch.empty((0, 96), device="cuda")
+    y, mean, rstd = atb.layer_norm(x, w, w, stats=True)
+    dx, dw, db = atb.layer_norm_backward(x, x, mean, rstd, w)
+    assert y.shape == dx.shape == (0, 96) and mean.shape == (0,) and not dw.any() and not db.any()
+
+
+def test_more_elements_than_32_bits_count():
+    M, D = 131081, 16400
+    x = torch.zeros((M, D), dtype=BF16, device="cuda")
+    rows = [0, 131071, 131080]
+    x[rows] = torch.randn((3, D), device="cuda").to(BF16)
+    y, mean, rstd = atb.layer_norm(x, eps=1e-5, stats=True)
+    want = reference(x[rows], x[rows], None, None, 1e-5)
+    close(y[rows], want["y"], "y")
+    del y
+    dx, _, db = atb.layer_norm_backward(x, x, mean, rstd, None, bias=True)
+    close(dx[rows], want["dx"], "dx")
+    close(db, want["db"], "db")
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    x, dy, w, b = inputs(3000, 1000, BF16, BF16, 10)
+    first = run(x, dy, w, b, 1e-5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y, mean, rstd = atb.layer_norm(x, w, b, 1e-5, stats=True, stream=side)
+    dx, dw, db = atb.layer_norm_backward(dy, x, mean, rstd, w, stream=side)
+    side.synchronize()
+    for a, c in zip((y, mean, rstd, dx, dw, db), first.values()):
+        assert torch.equal(a, c)
+
+
+def test_gradients_against_differences():
+    """The kernels' own forward pass in fp32, moved both ways along a direction."""
+    x, dy, w, b = inputs(8, 600, F32, F32, 11)
+    got = run(x, dy, w, b, 1e-3)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    for name, grad, at in (("x", got["dx"], 0), ("weight", got["dw"], 1), ("bias", got["db"], 2)):
+        args = [x, w, b]
+        v = torch.randn(args[at].shape, generator=g, device="cuda")
+        h = 2.0 ** -6
+        moved = []
+        for sign in (1, -1):
+            args[at] = (x, w, b)[at] + sign * h * v
+            moved.append((atb.layer_norm(*args, 1e-3).double() * dy.double()).sum())
+        slope, want = float((moved[0] - moved[1]) / (2 * h)), float((grad.double() * v.double()).sum())
+        # the loss's rounding over 2 h, and the third derivative's share, h^2
+        size = float((got["y"].double() * dy.double()).abs().sum())
+        assert abs(slope - want) <= 2.0 ** -23 * size / h + h * h * size, (name, slope, want)
