@@ -1,16 +1,15 @@
 // bf16 products in tiles: the kernel behind the gated block and its gradients (atb_ffn.hip, atb_ffn_grad.hip).
 //
-// C tile = A tile x B tile with fp32 accumulation in MFMA accumulators; K-steps of 64, two LDS buffers per operand, filled by
-// requests that go from memory straight into LDS.  An operand whose reduction index is contiguous lies in LDS as rows of 64 k
-// (128 bytes) and is read with plain 16-byte reads; one whose other index is contiguous lies there as 64 rows of k and is read
-// through the transposing read, so no operand of the backward pass is ever transposed in memory.
+// C tile = A tile x B tile with fp32 accumulation in MFMA accumulators, in K-steps of 64.  The tiles of a K-step come straight from memory into
+// LDS: three buffers for A and two for B, all of a CU's 160 KiB.  An operand whose reduction index is contiguous lies in LDS as rows of 64 k (128
+// bytes) and is read with plain 16-byte reads; one whose other index is contiguous lies there as 64 rows of k and is read through
+// the transposing read, so no operand of the backward pass is ever transposed in memory.
 //
-// Time line of a K-step s (its tile is in LDS buffer s % 2, its first k-slice of 32 already in registers):
+// Time line of K-step s (the fragments of its first k-slice of 32 are in registers):
 //   first half    the MFMAs of k-slice 0; the fragments of k-slice 1 are read under them
-//   barrier       every wave has all of tile s in registers, and tile s + 1, asked for one whole K-step ago, is complete
-//   second half   the MFMAs of k-slice 1; tile s + 2 is asked for, into the buffer that tile s has left, and the fragments of
-//                 k-slice 0 of tile s + 1 are read under them
-// so after the barrier no MFMA waits for LDS.
+//   barrier       every wave has all of tile s in registers, so its buffers are free, and tile s + 1 is complete
+//   second half   the MFMAs of k-slice 1; B's tile s + 2 and A's tile s + 3 are asked for, and the fragments of k-slice 0 of tile s + 1 are read
+// so no MFMA behind the barrier waits for LDS, and A's tile s + 2 is still on its way at the barrier.
 #pragma once
 
 #include "atb_activation.h"
@@ -27,7 +26,7 @@ struct TileShape {
     static constexpr int TK = 64;
     static constexpr int MI = TM / WM / 16, NI = TN / WN / 16;         // 16 x 16 blocks of a wave
     static constexpr int A_BYTES = TM * TK * 2, B_BYTES = TN * TK * 2;
-    static constexpr int LDS_BYTES = 2 * (A_BYTES + B_BYTES);
+    static constexpr int LDS_BYTES = 3 * A_BYTES + 2 * B_BYTES;
     static constexpr int RA = A_BYTES / 16 / NT, RB = B_BYTES / 16 / NT;   // requests per thread and tile
     static_assert(TN / WN == 64, "a wave's columns: 64, of a gated product 32 of each weight");
     static_assert(RA * NT * 16 == A_BYTES && RB * NT * 16 == B_BYTES, "whole requests");
@@ -53,20 +52,38 @@ struct Requests {
         first = (tid / CPR) * (int)(ld * 2) + chunk(tid) * 16;
         pitch = __builtin_amdgcn_readfirstlane(STEP * (int)(ld * 2));
     }
-    // The last tile of a reduction that is not a multiple of 64: what follows the end of a row of K-contiguous elements is the next row's, so
-    // the lanes of those chunks ask for nothing (K % 8 == 0: a chunk is inside or outside).  Rows of k end with the operand.
-    ATB_DEV void cut(int tid, int k_left)
+    // (by hand: worked out ahead of the K loop, as the compiler would, it holds a register for the whole kernel)
+    template <int i>
+    ATB_DEV int added() const
     {
-        if constexpr (!ROWS)
-            if (chunk(tid) * 8 >= k_left) first |= (int)0x80000000;       // past the end of every descriptor: reads as zero
+        int r = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("v_add_u32 %0, %1, %2" : "=v"(r) : "s"(i * pitch), "v"(first));
+#endif
+        return r;
     }
-    template <int i> ATB_DEV int offset() const { return first + i * pitch; }
+    // Request i of a tile with k_left of the reduction from its first k on.  What follows the end of a row of K-contiguous elements is the next row's,
+    // so the lanes of chunks behind it ask for nothing (K % 8 == 0: a chunk is inside or outside): an offset past the end of every descriptor, which
+    // reads as zero.  Rows of k end with the operand.
+    template <int i>
+    ATB_DEV int offset(int tid, int k_left) const
+    {
+        int at = first;
+        if constexpr (i > 0) at = added<i>();
+        if constexpr (ROWS) return at;
+        return chunk(tid) * 8 >= k_left ? (int)0x80000000 : at;
+    }
 };
 
 // A descriptor's four dwords, advanced by whole K-steps.
 struct Source {
     const char *ptr;
     int64_t left;          // bytes from ptr to the end of the operand
+    ATB_DEV void move(int64_t step, bool more)
+    {
+        ptr += step;
+        left = more ? left - step : 0;
+    }
     ATB_DEV intx4 words() const
     {
         const uint64_t a = reinterpret_cast<uint64_t>(ptr);
@@ -87,11 +104,12 @@ struct Tile {
     ARequests a_off;
     BRequests b_off, b2_off;
     Source a_src, b_src, b2_src;           // b2: the up weight of a gated product
-    intx4 a_words, b_words, b2_words;
-    int k_left, segment;                   // reduction left to ask for in this segment
-    int req_step, steps;                   // K-steps asked for, all of them
-    const char *a_rd[AT ? S::MI : 2], *b_rd[BROWS ? S::NI : 2];
-    char *a_req, *b_req;
+    int64_t a_step, b_step;                // bytes of a K-step
+    int a_left, b_left;                    // reduction left to ask for
+    int steps;                             // K-steps
+    unsigned a_rd, b_rd;                   // LDS addresses: this lane's part of a fragment in the first buffer
+    unsigned a_req, b_req;                 // ... this wave's part of a request
+    int slot;                              // A's buffer of the tile that is multiplied: its offset
     floatx4 acc[S::MI][S::NI];
     bf16x8 af[2][S::MI], bf[2][S::NI];
 
@@ -99,43 +117,32 @@ struct Tile {
         : p(p_), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)), wm(wave / S::WN), wn(wave % S::WN),
           m0(m0_), n0(n0_), problem(problem_)
     {
-        char *a_lds = lds, *b_lds = lds + 2 * S::A_BYTES;
-        a_req = a_lds + wave * 1024;
-        b_req = b_lds + wave * 1024;
-        const int q = lane >> 4, c = lane & 15;
-        if constexpr (AT) {
-            rows_addresses<S::MI, S::TM>(a_rd, a_lds, wm * (S::TM / S::WM));
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) a_rd[ks] = a_lds + (wm * (S::TM / S::WM) + c) * 128 + (((4 * ks + q) ^ (c & 7)) * 16);
-        }
-        if constexpr (BROWS) {
-            rows_addresses<S::NI, S::TN>(b_rd, b_lds, wn * 64);
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) b_rd[ks] = b_lds + (wn * (GATED ? 32 : 64) + c) * 128 + (((4 * ks + q) ^ (c & 7)) * 16);
-        }
+        const unsigned a_lds = (unsigned)reinterpret_cast<uintptr_t>(lds), b_lds = a_lds + 3 * S::A_BYTES;
+        a_req = __builtin_amdgcn_readfirstlane(a_lds + wave * 1024);
+        b_req = __builtin_amdgcn_readfirstlane(b_lds + wave * 1024);
+        a_rd = AT ? rows_address<S::TM>(a_lds, wm * (S::TM / S::WM)) : k_address(a_lds, wm * (S::TM / S::WM));
+        b_rd = BROWS ? rows_address<S::TN>(b_lds, wn * 64) : k_address(b_lds, wn * (GATED ? 32 : 64));
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
             for (int j = 0; j < S::NI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-        steps = p.segments * ((p.K + S::TK - 1) / S::TK);
-        req_step = 0;
-        segment = -1;
-        open();
+        steps = (p.K + S::TK - 1) / S::TK;
     }
 
-    // The transposing read of 16 columns and 8 k: in a group of 16 lanes, lane i addresses columns 4 (i % 4) .. + 3 of row i / 4 and lane j
-    // receives column j of the four rows; group g takes rows 8 g .. 8 g + 3 of the k-slice, a second read 4 rows on the others.
-    template <int BLOCKS, int R>
-    ATB_DEV void rows_addresses(const char *(&rd)[BLOCKS], const char *base, int first) const
+    // Rows of 64 k: lane l reads row l % 16 of a block of 16 and the 8 k of group l / 16 of a k-slice: chunk l / 16 or, of the second, four on.
+    ATB_DEV unsigned k_address(unsigned base, int first) const
     {
-        const int j = lane & 15, row = 8 * (lane >> 4) + (j >> 2);
-#pragma unroll
-        for (int e = 0; e < BLOCKS; ++e) {
-            const int chunk = first / 8 + 2 * e + ((j & 3) >> 1);
-            rd[e] = base + row * (R * 2) + ((chunk ^ (Requests<R, S::NT, true>::swizzle(row))) * 16) + (j & 1) * 8;
-        }
+        const int row = first + (lane & 15);
+        return base + row * 128 + (((lane >> 4) ^ (row & 7)) * 16);
+    }
+    // Rows of k, the transposing read of 16 columns and 8 k: in a group of 16 lanes, lane i addresses columns 4 (i % 4) .. + 3 of row i / 4 and lane j
+    // receives column j of the four rows; group g takes rows 8 g .. 8 g + 3 of the k-slice, a second read 4 rows on the others.  (The next 16 columns are
+    // two chunks on: the address with 32 added to the bits that the swizzle has been applied to, which are no others' here.)
+    template <int R>
+    ATB_DEV unsigned rows_address(unsigned base, int first) const
+    {
+        const int j = lane & 15, row = 8 * (lane >> 4) + (j >> 2), chunk = first / 8 + ((j & 3) >> 1);
+        return base + row * (R * 2) + ((chunk ^ Requests<R, S::NT, true>::swizzle(row)) * 16) + (j & 1) * 8;
     }
 
     // ---- requests
@@ -143,228 +150,224 @@ struct Tile {
     // Bytes from an operand's element (row, col) to its end; rows of `cols` elements, ld apart.
     static ATB_DEV int64_t bytes_left(int64_t rows, int64_t cols, int64_t ld, int64_t row, int64_t col) { return ((rows - 1 - row) * ld + cols - col) * 2; }
 
-    // The next segment's operands.
-    ATB_DEV void open()
+    // The operands s: a segment of the reduction, or a problem.
+    ATB_DEV void open(int s)
     {
-        ++segment;
-        k_left = p.K;
-        const int s = p.segments > 1 ? segment : problem;
-        if constexpr (AT) a_src = {reinterpret_cast<const char *>(p.A[s] + m0), bytes_left(p.K, p.M, p.lda[s], 0, m0)};
-        else a_src = {reinterpret_cast<const char *>(p.A[s] + (int64_t)m0 * p.lda[s]), bytes_left(p.M, p.K, p.lda[s], m0, 0)};
+        a_left = b_left = p.K;
+        a_step = AT ? S::TK * 2 * p.lda[s] : S::TK * 2;
+        b_step = BROWS ? S::TK * 2 * p.ldb[s] : S::TK * 2;
+        Source a, b, up = {};
+        if constexpr (AT) a = {reinterpret_cast<const char *>(p.A[s] + m0), bytes_left(p.K, p.M, p.lda[s], 0, m0)};
+        else a = {reinterpret_cast<const char *>(p.A[s] + (int64_t)m0 * p.lda[s]), bytes_left(p.M, p.K, p.lda[s], m0, 0)};
         a_off.place(tid, p.lda[s]);
         if constexpr (GATED) {
             // rows 0 .. TN / 2 - 1 of the LDS tile are columns of the gate weight, the others the same columns of the up weight
-            b_src = {reinterpret_cast<const char *>(p.B[0] + (int64_t)n0 * p.ldb[0]), bytes_left(p.N, p.K, p.ldb[0], n0, 0)};
-            b2_src = {reinterpret_cast<const char *>(p.B[1] + (int64_t)n0 * p.ldb[1]), bytes_left(p.N, p.K, p.ldb[1], n0, 0)};
+            b = {reinterpret_cast<const char *>(p.B[0] + (int64_t)n0 * p.ldb[0]), bytes_left(p.N, p.K, p.ldb[0], n0, 0)};
+            up = {reinterpret_cast<const char *>(p.B[1] + (int64_t)n0 * p.ldb[1]), bytes_left(p.N, p.K, p.ldb[1], n0, 0)};
             b_off.place(tid, p.ldb[0]);
             b2_off.place(tid, p.ldb[1]);
         } else {
-            if constexpr (BROWS) b_src = {reinterpret_cast<const char *>(p.B[s] + n0), bytes_left(p.K, p.N, p.ldb[s], 0, n0)};
-            else b_src = {reinterpret_cast<const char *>(p.B[s] + (int64_t)n0 * p.ldb[s]), bytes_left(p.N, p.K, p.ldb[s], n0, 0)};
+            if constexpr (BROWS) b = {reinterpret_cast<const char *>(p.B[s] + n0), bytes_left(p.K, p.N, p.ldb[s], 0, n0)};
+            else b = {reinterpret_cast<const char *>(p.B[s] + (int64_t)n0 * p.ldb[s]), bytes_left(p.N, p.K, p.ldb[s], n0, 0)};
             b_off.place(tid, p.ldb[s]);
         }
-        cut_last();
-        make_words();
-    }
-
-    ATB_DEV void cut_last()
-    {
-        if (k_left < S::TK) {
-            a_off.cut(tid, k_left);
-            b_off.cut(tid, k_left);
-            if constexpr (GATED) b2_off.cut(tid, k_left);
-        }
-    }
-
-    ATB_DEV void make_words()
-    {
-        a_words = a_src.words();
-        b_words = b_src.words();
-        if constexpr (GATED) b2_words = b2_src.words();
-    }
-
-    // After the last request of a tile: one K-step on.  Past the last one the descriptors are empty: nothing is asked of memory.
-    ATB_DEV void advance()
-    {
-        ++req_step;
-        k_left -= S::TK;
-        if (req_step >= steps) {
-            a_src.left = b_src.left = 0;
-            if constexpr (GATED) b2_src.left = 0;
-            make_words();
-        } else if (k_left <= 0) {
-            open();
-        } else {
-            const int s = p.segments > 1 ? segment : problem;
-            const int64_t da = AT ? S::TK * 2 * p.lda[s] : S::TK * 2, db = BROWS ? S::TK * 2 * p.ldb[s] : S::TK * 2;
-            a_src.ptr += da; a_src.left -= da;
-            b_src.ptr += db; b_src.left -= db;
-            if constexpr (GATED) { b2_src.ptr += db; b2_src.left -= db; }
-            cut_last();
-            make_words();
-        }
+        a_src = a;
+        b_src = b;
+        b2_src = up;
     }
 
     // 16 bytes per lane from memory to LDS.  By hand, so that the compiler does not wait for it before every read of LDS that follows; the wait is
     // the one ahead of the barrier.  M0, the LDS address, is put back: the compiler is not told about it.
-    static ATB_DEV void request_one(intx4 words, int off, const char *to)
+    static ATB_DEV void request_one(intx4 words, int off, unsigned to)
     {
 #if defined(__HIP_DEVICE_COMPILE__)
-        const unsigned addr = (unsigned)reinterpret_cast<uintptr_t>(to);
         int saved;
         asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
                      : "=&s"(saved)
-                     : "s"(__builtin_amdgcn_readfirstlane((int)addr)), "v"(off), "s"(words) : "memory");
+                     : "s"(to), "v"(off), "s"(words) : "memory");
 #endif
     }
 
-    // Request r (0 .. RA + RB - 1) of the next tile into buffer `buf`.
+    // Request r of A's next tile into the buffer at `to`, of B's into its buffer `buf`.  After a tile's last one the stream moves on by a K-step; past the
+    // last K-step its descriptor is empty and nothing is asked of memory.
+    template <int r>
+    ATB_DEV void request_a(int to)
+    {
+        request_one(a_src.words(), a_off.template offset<r>(tid, a_left), a_req + to + r * S::NT * 16);
+        if constexpr (r == S::RA - 1) {
+            a_left -= S::TK;
+            a_src.move(a_step, a_left > 0);
+        }
+    }
     template <int r, int buf>
-    ATB_DEV void request()
+    ATB_DEV void request_b()
+    {
+        const unsigned to = b_req + buf * S::B_BYTES + r * S::NT * 16;
+        if constexpr (GATED && r >= S::RB / 2) request_one(b2_src.words(), b2_off.template offset<r - S::RB / 2>(tid, b_left), to);
+        else request_one(b_src.words(), b_off.template offset<r>(tid, b_left), to);
+        if constexpr (r == S::RB - 1) {
+            b_left -= S::TK;
+            b_src.move(b_step, b_left > 0);
+            if constexpr (GATED) b2_src.move(b_step, b_left > 0);
+        }
+    }
+    template <int r = 0>
+    ATB_DEV void request_all_a(int to)
     {
         if constexpr (r < S::RA) {
-            request_one(a_words, a_off.template offset<r>(), a_req + buf * S::A_BYTES + r * S::NT * 16);
-        } else {
-            constexpr int i = r - S::RA;
-            char *to = b_req + buf * S::B_BYTES + i * S::NT * 16;
-            if constexpr (GATED && i >= S::RB / 2) request_one(b2_words, b2_off.template offset<i - S::RB / 2>(), to);
-            else request_one(b_words, b_off.template offset<i>(), to);
+            request_a<r>(to);
+            request_all_a<r + 1>(to);
         }
-        if constexpr (r == S::RA + S::RB - 1) advance();
     }
-
     template <int buf, int r = 0>
-    ATB_DEV void request_all()
+    ATB_DEV void request_all_b()
     {
-        if constexpr (r < S::RA + S::RB) {
-            request<r, buf>();
-            request_all<buf, r + 1>();
+        if constexpr (r < S::RB) {
+            request_b<r, buf>();
+            request_all_b<buf, r + 1>();
         }
     }
+    static constexpr int REQS = S::RA + S::RB;
 
     // ---- LDS -> registers
 
     template <int R>
-    static ATB_DEV bf16x8 read_rows(const char *src)
+    static ATB_DEV bf16x8 read_rows(unsigned at)
     {
         bf16x8 r = {};
 #if defined(__HIP_DEVICE_COMPILE__)
         typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
         union { shortx4 s[2]; bf16x8 b; } u;
-        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(src));
-        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(src + 4 * R * 2));
+        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)at);
+        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(at + 4 * R * 2));
         r = u.b;
 #endif
         return r;
     }
-    // Fragment f of a k-slice in the order of first use
-    template <int ks, int buf, int f>
-    ATB_DEV void read_frag()
+    static ATB_DEV bf16x8 read_k(unsigned at)
     {
-        // a0, b0 .. b(NI-1), a1 .. a(MI-1)
+        bf16x8 r = {};
+#if defined(__HIP_DEVICE_COMPILE__)
+        r = *(const __attribute__((address_space(3))) bf16x8 *)at;
+#endif
+        return r;
+    }
+    // Fragment f of k-slice ks of the tile in A's buffer at `from` and B's buffer `buf`, in the order of first use: a0, b0 .. b(NI - 1), a1 .. a(MI - 1)
+    template <int ks, int buf, int f>
+    ATB_DEV void read_frag(int from)
+    {
         if constexpr (f >= 1 && f <= S::NI) {
             constexpr int j = f - 1;
-            if constexpr (BROWS) bf[ks][j] = read_rows<S::TN>(b_rd[j] + buf * S::B_BYTES + ks * 32 * S::TN * 2);
-            else bf[ks][j] = *reinterpret_cast<const bf16x8 *>(b_rd[ks] + buf * S::B_BYTES + (GATED && j >= 2 ? S::TN / 2 * 128 + (j - 2) * 2048 : j * 2048));
+            if constexpr (BROWS) bf[ks][j] = read_rows<S::TN>((b_rd ^ (j * 32)) + buf * S::B_BYTES + ks * 32 * S::TN * 2);
+            else bf[ks][j] = read_k((b_rd ^ (ks * 64)) + buf * S::B_BYTES + (GATED && j >= 2 ? S::TN / 2 * 128 + (j - 2) * 2048 : j * 2048));
         } else {
             constexpr int i = f == 0 ? 0 : f - S::NI;
-            if constexpr (AT) af[ks][i] = read_rows<S::TM>(a_rd[i] + buf * S::A_BYTES + ks * 32 * S::TM * 2);
-            else af[ks][i] = *reinterpret_cast<const bf16x8 *>(a_rd[ks] + buf * S::A_BYTES + i * 2048);
+            if constexpr (AT) af[ks][i] = read_rows<S::TM>(((a_rd + from) ^ (i * 32)) + ks * 32 * S::TM * 2);
+            else af[ks][i] = read_k(((a_rd + from) ^ (ks * 64)) + i * 2048);
         }
     }
     static constexpr int FRAGS = S::MI + S::NI;
     template <int ks, int buf, int f = 0>
-    ATB_DEV void read_all()
+    ATB_DEV void read_all(int from)
     {
         if constexpr (f < FRAGS) {
-            read_frag<ks, buf, f>();
-            read_all<ks, buf, f + 1>();
+            read_frag<ks, buf, f>(from);
+            read_all<ks, buf, f + 1>(from);
         }
     }
 
-    // ---- a half K-step: MI x NI MFMAs and their side work
+    // ---- half a K-step: MI x NI MFMAs and their side work
 
-    template <int ks>
-    ATB_DEV void mfma(int i, int j)
+    static constexpr int SLOTS = S::MI * S::NI;
+    template <int ks, int t>
+    ATB_DEV void mfma()
     {
 #if defined(__HIP_DEVICE_COMPILE__)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[ks][j], af[ks][i], acc[i][j], 0, 0, 0);
+        acc[t / S::NI][t % S::NI] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[ks][t % S::NI], af[ks][t / S::NI], acc[t / S::NI][t % S::NI], 0, 0, 0);
 #endif
     }
-    static constexpr int SLOTS = S::MI * S::NI;
-    static constexpr int REQS = S::RA + S::RB;
-
     template <int buf, int t = 0>
     ATB_DEV void first_half()
     {
         if constexpr (t < SLOTS) {
-            mfma<0>(t / S::NI, t % S::NI);
-            // fragment f behind MFMA 2 f (1 f where there are fewer MFMAs)
+            mfma<0, t>();
             constexpr int every = SLOTS >= 2 * FRAGS ? 2 : 1;
-            if constexpr (t % every == 0 && t / every < FRAGS) read_frag<1, buf, t / every>();
+            if constexpr (t % every == 0 && t / every < FRAGS) read_frag<1, buf, t / every>(slot);
             __builtin_amdgcn_sched_barrier(0);
             first_half<buf, t + 1>();
         }
     }
     template <int buf, int t = 0>
-    ATB_DEV void second_half()
+    ATB_DEV void second_half(int next)
     {
         if constexpr (t < SLOTS) {
-            mfma<1>(t / S::NI, t % S::NI);
-            constexpr int side = FRAGS + REQS, per = (side + SLOTS - 1) / SLOTS;
-            side_work<buf, t * per, t * per + per>();
+            mfma<1, t>();
+            constexpr int per = (FRAGS + REQS + SLOTS - 1) / SLOTS;
+            side_work<buf, t * per, t * per + per>(next);
             __builtin_amdgcn_sched_barrier(0);
-            second_half<buf, t + 1>();
+            second_half<buf, t + 1>(next);
         }
     }
-    // requests and reads in turns
-    template <int buf, int from, int to>
-    ATB_DEV void side_work()
+    // requests, B's first, and reads in turns
+    template <int buf, int n, int end>
+    ATB_DEV void side_work(int next)
     {
-        if constexpr (from < to && from < FRAGS + REQS) {
-            constexpr int both = 2 * (REQS < FRAGS ? REQS : FRAGS);
-            if constexpr (from < both) {
-                if constexpr (from % 2 == 0) request<from / 2, buf>();
-                else read_frag<0, buf ^ 1, from / 2>();
-            } else if constexpr (REQS < FRAGS) {
-                read_frag<0, buf ^ 1, from - REQS>();
-            } else {
-                request<from - FRAGS, buf>();
+        static_assert(REQS <= FRAGS, "reads are what is left");
+        if constexpr (n < end) {
+            if constexpr (n < 2 * REQS && n % 2 == 0) {
+                if constexpr (n / 2 < S::RB) request_b<n / 2, buf>();
+                else request_a<n / 2 - S::RB>(slot);
+            } else if constexpr (n < FRAGS + REQS) {
+                read_frag<0, buf ^ 1, n < 2 * REQS ? n / 2 : n - REQS>(next);
             }
-            side_work<buf, from + 1, to>();
+            side_work<buf, n + 1, end>(next);
         }
     }
 
+    // The `younger` most recent requests of this wave may be on their way; its reads of LDS are done, and so are those of all waves after it.
     template <int younger>
-    static ATB_DEV void wait_requests()
+    static ATB_DEV void wait_and_barrier()
     {
         static_assert(younger >= 0 && younger < 64, "vmcnt is a 6-bit counter");
-        __builtin_amdgcn_s_waitcnt((younger & 15) | (7 << 4) | (15 << 8) | ((younger >> 4) << 14));
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(younger) : "memory");
     }
 
     template <int buf>
     ATB_DEV void step()
     {
         first_half<buf>();
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        second_half<buf>();
+        wait_and_barrier<S::RA>();
+        const int next = slot == 2 * S::A_BYTES ? 0 : slot + S::A_BYTES;
+        second_half<buf>(next);
+        slot = next;
     }
 
-    ATB_DEV void multiply()
+    ATB_DEV void multiply_segment()
     {
-        request_all<0>();
-        request_all<1>();
-        wait_requests<REQS>();
-        asm volatile("s_barrier" ::: "memory");
-        read_all<0, 0>();
+        request_all_a(0);
+        request_all_b<0>();
+        request_all_a(S::A_BYTES);
+        request_all_b<1>();
+        request_all_a(2 * S::A_BYTES);
+        wait_and_barrier<2 * S::RA + S::RB>();
+        slot = 0;
+        read_all<0, 0>(0);
         for (int s = 0; s < steps; s += 2) {
             step<0>();
             if (s + 1 == steps) break;
             step<1>();
         }
-        wait_requests<0>();
+        wait_and_barrier<0>();                                 // LDS is free again
     }
 
+    // Segments one after the other: the few requests in flight are awaited in between.
+    ATB_DEV void multiply()
+    {
+        for (int s = 0; s < p.segments; ++s) {
+            open(p.segments > 1 ? s : problem);
+            multiply_segment();
+        }
+    }
     // x, which the compiler is not to know ahead of this place: it would work out the addresses of the whole tile before the first store
     static ATB_DEV int here(int x)
     {
@@ -373,14 +376,15 @@ struct Tile {
 #endif
         return x;
     }
-    // The bits of a sum, likewise: it would carry the accumulators round the K loop a second time, as integers
-    static ATB_DEV unsigned bits(float x)
+    // An element of an accumulator, likewise: of elements, or their bits, the compiler makes values that it carries round the K loop beside the accumulators
+    static ATB_DEV float sum(float x)
     {
 #if defined(__HIP_DEVICE_COMPILE__)
         asm volatile("" : "+v"(x));
 #endif
-        return __float_as_uint(x);
+        return x;
     }
+    static ATB_DEV unsigned bits(float x) { return __float_as_uint(sum(x)); }
 
     // ---- epilogue: a lane holds row 16 i + lane % 16 of the wave's part and, of column block j, columns 4 (lane / 16) .. + 3.  One swap of
     // lanes per register makes of two neighbouring column blocks eight consecutive columns per lane.
@@ -447,11 +451,15 @@ struct Tile {
             store(p.kept + n * ((int64_t)p.M * p.N), p.N, row, col, intx4{(int)w[n][0][0], (int)w[n][0][1], (int)w[n][1][0], (int)w[n][1][1]});
         }
     }
-    ATB_DEV void kept(int row, int col, float (&g)[8], float (&u)[8]) const
+    // The three words of a piece (of the last row or column in place of one outside), and g and u from them
+    ATB_DEV void load_kept(int row, int col, intx4 (&w)[3]) const
     {
-        intx4 w[3];
+        const uint16_t *at = p.kept + (int64_t)min(row, p.M - 1) * p.N + min(col, p.N - 8);
 #pragma unroll
-        for (int n = 0; n < 3; ++n) w[n] = *reinterpret_cast<const intx4 *>(p.kept + n * ((int64_t)p.M * p.N) + (int64_t)row * p.N + col);
+        for (int n = 0; n < 3; ++n) w[n] = *reinterpret_cast<const intx4 *>(at + n * ((int64_t)p.M * p.N));
+    }
+    static ATB_DEV void kept(const intx4 (&w)[3], float (&g)[8], float (&u)[8])
+    {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const unsigned gh = (unsigned)w[0][e], uh = (unsigned)w[1][e], lo = (unsigned)w[2][e];
@@ -479,53 +487,66 @@ struct Tile {
         for (int i = 0; i < S::MI; ++i) {
             const int row = here(row0 + 16 * i);
             if constexpr (EPI == kGatedKeep) keep(row, col, acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-            floatx4 h[2];
+            floatx4 h[2], g[2], u[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    g[j][e] = sum(acc[i][j][e]);
+                    u[j][e] = sum(acc[i][j + 2][e]);
+                }
             with_activation(p.act, [&](auto a) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) h[j][e] = activate<decltype(a)::value>(acc[i][j][e]) * acc[i][j + 2][e];
+                    for (int e = 0; e < 4; ++e) h[j][e] = activate<decltype(a)::value>(g[j][e]) * u[j][e];
             });
             store(p.C[0], p.ldc, row, col, piece(h[0], h[1]));
             __builtin_amdgcn_sched_barrier(0);             // row block by row block: registers
         }
     }
 
+    // Pieces of eight columns, AHEAD of them on their way (one by one the 16 of a wave took 33 us of latency, a quarter of a tile of K = 4096)
     ATB_DEV void finish_grad()
     {
+        constexpr int PIECES = S::MI * S::NI / 2, AHEAD = 6;
         const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), col0 = n0 + wn * 64 + piece_col();
+        intx4 w[AHEAD][3];
 #pragma unroll
-        for (int i = 0; i < S::MI; ++i)
+        for (int n = 0; n < AHEAD; ++n) load_kept(row0 + 16 * (n / (S::NI / 2)), col0 + 32 * (n % (S::NI / 2)), w[n]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < S::NI; j += 2) {
-                const int row = here(row0 + 16 * i), col = col0 + 16 * j;
-                float d[8];                                    // dh of this lane's eight columns
+        for (int n = 0; n < PIECES; ++n) {
+            const int i = n / (S::NI / 2), j = 2 * (n % (S::NI / 2));
+            const int row = here(row0 + 16 * i), col = col0 + 16 * j;
+            float d[8];                                    // dh of this lane's eight columns
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    unsigned x = bits(acc[i][j][e]), y = bits(acc[i][j + 1][e]);
-                    swap_halves(x, y);
-                    d[e] = __uint_as_float(x);
-                    d[4 + e] = __uint_as_float(y);
-                }
-                if (row < p.M && col < p.N) {
-                    float g[8], u[8];
-                    kept(row, col, g, u);
-                    bf16x8 dg, du;
-                    with_activation(p.act, [&](auto act) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float a, slope;
-                            activate_grad<decltype(act)::value>(g[e], a, slope);
-                            dg[e] = (__bf16)(d[e] * u[e] * slope);
-                            du[e] = (__bf16)(d[e] * a);
-                        }
-                    });
-                    const int64_t to = (int64_t)row * p.ldc + col;
-                    *reinterpret_cast<bf16x8 *>(p.C[0] + to) = dg;
-                    *reinterpret_cast<bf16x8 *>(p.C[1] + to) = du;
-                }
-                __builtin_amdgcn_sched_barrier(0);
+            for (int e = 0; e < 4; ++e) {
+                unsigned x = bits(acc[i][j][e]), y = bits(acc[i][j + 1][e]);
+                swap_halves(x, y);
+                d[e] = __uint_as_float(x);
+                d[4 + e] = __uint_as_float(y);
             }
+            float g[8], u[8];
+            kept(w[n % AHEAD], g, u);
+            bf16x8 dg, du;
+            with_activation(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float a, slope;
+                    activate_grad<decltype(act)::value>(g[e], a, slope);
+                    dg[e] = (__bf16)(d[e] * u[e] * slope);
+                    du[e] = (__bf16)(d[e] * a);
+                }
+            });
+            if (row < p.M && col < p.N) {
+                const int64_t to = (int64_t)row * p.ldc + col;
+                *reinterpret_cast<bf16x8 *>(p.C[0] + to) = dg;
+                *reinterpret_cast<bf16x8 *>(p.C[1] + to) = du;
+            }
+            if (n + AHEAD < PIECES) load_kept(here(row0 + 16 * ((n + AHEAD) / (S::NI / 2))), col0 + 32 * ((n + AHEAD) % (S::NI / 2)), w[n % AHEAD]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 
     ATB_DEV void finish()
@@ -554,7 +575,7 @@ ATB_DEV bool tile_of(const TileParams &p, int b, int &m0, int &n0)
 template <class S, bool AT, bool BROWS, int EPI>
 __global__ void __launch_bounds__(S::NT, S::NT == 512 ? 2 : 2) tile_kernel(const TileParams p)
 {
-    __shared__ __attribute__((aligned(16))) char lds[S::LDS_BYTES];
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
     int m0 = 0, n0 = 0;
     if (!tile_of<S, (EPI == kGated || EPI == kGatedKeep)>(p, blockIdx.x, m0, n0)) return;
     Tile<S, AT, BROWS, EPI> tile(p, lds, m0, n0, blockIdx.y);
