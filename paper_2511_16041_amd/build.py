@@ -28,7 +28,7 @@ ALIGNED = ["-falign-loops=64"]
 # (source, object name, extra flags): the GEMM instance table is cut into three groups that compile side by side
 SOURCES = [("atb_gemm.hip", "atb_gemm_g0", ["-DATB_GROUP=0"]), ("atb_gemm.hip", "atb_gemm_g1", ["-DATB_GROUP=1"] + ALIGNED),
            ("atb_gemm.hip", "atb_gemm_g2", ["-DATB_GROUP=2"]), ("atb_skinny.hip", "atb_skinny", SKINNY_FLAGS), ("atb_rows.hip", "atb_rows", WHOLE_PHIS), ("atb_bfp16.hip", "atb_bfp16", []), ("atb_probe.hip", "atb_probe", []),
-           ("atb_ffn.hip", "atb_ffn", WHOLE_PHIS), ("atb_ffn_grad.hip", "atb_ffn_grad", WHOLE_PHIS), ("atb_stream.hip", "atb_stream", []),
+           ("atb_ffn.hip", "atb_ffn", WHOLE_PHIS), ("atb_ffn_grad.hip", "atb_ffn_grad", WHOLE_PHIS), ("atb_stream.hip", "atb_stream", []), ("atb_q4_stream.hip", "atb_q4_stream", []),
            ("atb_norm.hip", "atb_norm", []), ("atb_q4.hip", "atb_q4", []),
            ("atb_model.cpp", "atb_model", []), ("atb_api.cpp", "atb_api", []), ("atb_layers_api.cpp", "atb_layers_api", [])]
 

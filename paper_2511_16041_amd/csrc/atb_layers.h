@@ -54,7 +54,7 @@ hipError_t launch_tiles_dx(TileParams p, int epilogue, hipStream_t stream);
 // Gradients of weights: A transposed, B in rows.
 hipError_t launch_tiles_dw(TileParams p, hipStream_t stream);
 
-// ---- products of few rows (atb_stream.hip)
+// ---- products of few rows (atb_stream.hip, atb_q4_stream.hip)
 
 // Whether the gated block of M tokens in bf16 runs on the kernel for few rows.
 static inline bool ffn_streams(int64_t M) { return M <= 32; }
@@ -76,6 +76,7 @@ struct StreamParams {
     int y_type;                  // atb_type
 };
 hipError_t launch_stream(const StreamParams &p, hipStream_t stream);
+hipError_t launch_q4_stream(const StreamParams &p, hipStream_t stream);      // 4 bits; launch_stream calls it
 
 // ---- 4-bit storage (atb_q4.hip)
 
