@@ -248,7 +248,12 @@ typedef struct atb_ffn {
     int64_t ldx, ld_gate, ld_up, ld_down;       /* multiples of 8, below 2^22 */
     int64_t M, D, F;                            /* 0 <= M <= 2^23; D, F multiples of 8, 8 .. 2^22 - 8 */
     atb_activation act;
+    void *workspace;                            /* DEVICE, 16-byte aligned, of the bytes below for the call; NULL: long reductions of few tokens are not shared out */
 } atb_ffn;
+
+/* Bytes of the workspace of a forward pass (keeps != 0: one with `kept`) and of a backward pass, at most 16 MiB; 0: none is used, or invalid arguments. */
+size_t atb_ffn_workspace(int64_t M, int64_t D, int64_t F, int keeps);
+size_t atb_ffn_backward_workspace(int64_t M, int64_t D, int64_t F);
 
 /* Bytes of the buffer that keeps x Wg^T and x Wu^T for the backward pass, 6 M F: three planes of M x F 16-bit words, the upper halves of
  * the two products in fp32 and the next byte of both (24 of their 32 bits: in bf16 they would double the variance of dx's error); 0 on

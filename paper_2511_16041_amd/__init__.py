@@ -77,7 +77,7 @@ class KernelInfo(ctypes.Structure):
 class Ffn(ctypes.Structure):
     """atb_ffn: the operands of a gated block."""
     _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w_gate", "w_up", "w_down")] + \
-               [(n, ctypes.c_int64) for n in ("ldx", "ld_gate", "ld_up", "ld_down", "M", "D", "F")] + [("act", ctypes.c_int)]
+               [(n, ctypes.c_int64) for n in ("ldx", "ld_gate", "ld_up", "ld_down", "M", "D", "F")] + [("act", ctypes.c_int), ("workspace", ctypes.c_void_p)]
 
 
 class Q4(ctypes.Structure):
@@ -92,7 +92,7 @@ EXPORTS = [
     "atb_gemm_launch_info", "atb_gemm_kernel", "atb_gemm_streams", "atb_instance_count", "atb_instance_get", "atb_bfp16_layout", "atb_bfp16_bytes",
     "atb_bfp16_quantize", "atb_bfp16_decode", "atb_hw_params_xdna2", "atb_hw_params_mi355x",
     "atb_model_eval", "atb_select_tiles", "atb_model_microkernel", "atb_instance_geometry", "atb_mfma_probe",
-    "atb_layer_norm", "atb_layer_norm_workspace", "atb_layer_norm_backward", "atb_ffn_kept_bytes", "atb_ffn_forward", "atb_ffn_backward",
+    "atb_layer_norm", "atb_layer_norm_workspace", "atb_layer_norm_backward", "atb_ffn_workspace", "atb_ffn_backward_workspace", "atb_ffn_kept_bytes", "atb_ffn_forward", "atb_ffn_backward",
     "atb_q4_quantize", "atb_q4_decode", "atb_q4_matvec", "atb_q4_gated",
 ]
 
@@ -156,6 +156,9 @@ def lib() -> ctypes.CDLL:
     L.atb_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, ci, ci, vp]
     L.atb_ffn_forward.restype = ci
     L.atb_ffn_forward.argtypes = [ctypes.POINTER(Ffn), vp, vp, vp, i64, vp]
+    L.atb_ffn_workspace.restype = L.atb_ffn_backward_workspace.restype = ctypes.c_size_t
+    L.atb_ffn_workspace.argtypes = [i64, i64, i64, ci]
+    L.atb_ffn_backward_workspace.argtypes = [i64, i64, i64]
     L.atb_ffn_kept_bytes.restype = ctypes.c_size_t
     L.atb_ffn_kept_bytes.argtypes = [i64, i64]
     L.atb_ffn_backward.restype = ci

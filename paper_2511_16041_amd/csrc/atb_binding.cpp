@@ -287,12 +287,14 @@ bool describe(atb_ffn &f, const at::Tensor &x, const at::Tensor &wg, const at::T
     return true;
 }
 
-// ffn_forward(entry, entry of the kept buffer's size, x, w_gate, w_up, w_down, act, save) -> y, or (y, h, kept)
+// ffn_forward(entry, entries of the sizes of the kept buffer and of the workspace, x, w_gate, w_up, w_down, act, save) -> y, or (y, h, kept)
 PyObject *ffn_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 8) return PyErr_Format(PyExc_TypeError, "ffn_forward takes 8 arguments");
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "ffn_forward takes 9 arguments");
     const auto call = reinterpret_cast<decltype(&atb_ffn_forward)>(PyLong_AsVoidPtr(args[0]));
     const auto size = reinterpret_cast<decltype(&atb_ffn_kept_bytes)>(PyLong_AsVoidPtr(args[1]));
+    const auto room = reinterpret_cast<decltype(&atb_ffn_workspace)>(PyLong_AsVoidPtr(args[2]));
+    ++args;
     const long act = PyLong_AsLong(args[6]);
     const int save = PyObject_IsTrue(args[7]);
     if (PyErr_Occurred() || !tensors(args + 2, 4)) return nullptr;
@@ -302,8 +304,11 @@ PyObject *ffn_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (!describe(f, x, THPVariable_Unpack(args[3]), THPVariable_Unpack(args[4]), THPVariable_Unpack(args[5]), act)) return refuse();
     const c10::DeviceGuard guard(x.device());
     const at::Tensor y = make({f.M, f.D}, at::kBFloat16, x.device()), h = make({f.M, f.F}, at::kBFloat16, x.device());
-    std::optional<at::Tensor> kept;
+    std::optional<at::Tensor> kept, work;
     if (save) kept = make({(int64_t)size(f.M, f.F)}, at::kByte, x.device());
+    const int64_t bytes = (int64_t)room(f.M, f.D, f.F, save);
+    if (bytes > 0) work = make({bytes}, at::kByte, x.device());
+    f.workspace = data<void *>(work);
     int st;
     {
         WithoutLock unlocked;
@@ -314,12 +319,14 @@ PyObject *ffn_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// ffn_backward(entry, entry of the kept buffer's size, dy, x, w_gate, w_up, w_down, h, kept, act) -> (dx, dw_gate, dw_up, dw_down)
+// ffn_backward(entry, entries of the sizes of the kept buffer and of the workspace, dy, x, w_gate, w_up, w_down, h, kept, act) -> (dx, dw_gate, dw_up, dw_down)
 PyObject *ffn_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 10) return PyErr_Format(PyExc_TypeError, "ffn_backward takes 10 arguments");
+    if (n != 11) return PyErr_Format(PyExc_TypeError, "ffn_backward takes 11 arguments");
     const auto call = reinterpret_cast<decltype(&atb_ffn_backward)>(PyLong_AsVoidPtr(args[0]));
     const auto size = reinterpret_cast<decltype(&atb_ffn_kept_bytes)>(PyLong_AsVoidPtr(args[1]));
+    const auto room = reinterpret_cast<decltype(&atb_ffn_backward_workspace)>(PyLong_AsVoidPtr(args[2]));
+    ++args;
     const long act = PyLong_AsLong(args[9]);
     if (PyErr_Occurred() || !tensors(args + 2, 7)) return nullptr;
     HANDLE_TH_ERRORS
@@ -331,6 +338,10 @@ PyObject *ffn_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (kept.device() != on || !is_buffer(kept, (int64_t)size(f.M, f.F))) return refuse();
     const c10::DeviceGuard guard(on);
     const at::Tensor dx = make({f.M, f.D}, at::kBFloat16, on), dwg = make({f.F, f.D}, at::kBFloat16, on), dwu = make({f.F, f.D}, at::kBFloat16, on), dwd = make({f.D, f.F}, at::kBFloat16, on);
+    std::optional<at::Tensor> work;
+    const int64_t bytes = (int64_t)room(f.M, f.D, f.F);
+    if (bytes > 0) work = make({bytes}, at::kByte, on);
+    f.workspace = data<void *>(work);
     const at::Tensor dg = make({f.M, f.F}, at::kBFloat16, on), du = make({f.M, f.F}, at::kBFloat16, on);
     int st;
     {

@@ -4,6 +4,8 @@
 
 #include "atb_internal.h"
 
+#include <algorithm>
+
 namespace atb {
 
 // ---- layer norm (atb_norm.hip)
@@ -32,7 +34,11 @@ enum Epilogue {
     kGated = 1,          // C = act(gate sum) * up sum; B is both weights, their columns side by side in a wave's tile
     kGatedKeep = 2,      // ... and writes what the backward pass needs of both sums
     kGatedGrad = 3,      // the sum is dh: writes dg = dh u act'(g) and du = dh act(g)
+    kShare = 4,          // the sum of a share of the reduction, in fp32; what it is for is done where the shares are joined
+    kGatedShare = 5,     // ... of both weights
 };
+constexpr bool is_gated(int epilogue) { return epilogue == kGated || epilogue == kGatedKeep || epilogue == kGatedShare; }
+constexpr bool is_share(int epilogue) { return epilogue == kShare || epilogue == kGatedShare; }
 
 struct TileParams {
     // A: M x K, K contiguous, or (transposed) K x M, M contiguous; B: N x K, K contiguous, or (rows) K x N, N contiguous.
@@ -45,8 +51,43 @@ struct TileParams {
     int M, N, K;
     int segments, problems;
     int act;                     // atb_activation
+    float *shares;               // room for tile_shares() floats, or null: reductions are not shared out
+    // set by the launch
     int tiles_m, tiles_n, group_m;
+    int steps;                   // K-steps of a segment
+    int parts, planes;           // shares of the reduction; planes of M x N in each
 };
+
+struct TilePlan { int tiles_m, tiles_n; };
+static inline TilePlan tile_plan(int64_t M, int64_t N, int tile, bool gated)
+{
+    const int64_t cols = gated ? tile / 2 : tile;
+    return {(int)((M + tile - 1) / tile), (int)((N + cols - 1) / cols)};
+}
+// Tiles of 256 x 256, one workgroup per CU, where there are nearly as many as CUs (192 of 256; forward pass of D = 4096, F = 14336, us: M = 512, 224 of them in the
+// gated product, 195 against 230 with 128 x 128; M = 2048, 128 of them in the down projection, 670 with small ones there, 717 with large ones).  Otherwise tiles of 128 x 128,
+// two per CU, and where these are at most half as many as CUs the reduction is split into shares, at most one workgroup per CU in all, whose sums go to memory
+// in fp32 and are joined by a second kernel.  A workgroup alone on its CU takes 0.74 us per K-step whatever the others do, so at few tokens the length of the
+// reduction is the time.  A share has at least 8 K-steps: below, the second launch costs what it saves.
+// Whole / in shares, us, forward and backward (the sum of the kernels and launches):
+//   M 33, D 1024, F 4096    44 /  24    94 /  39        M 33, D 4096, F 14336   225 /  92    492 / 208
+//   M 256                   47 /  35   102 /  52        M 512                   275 / 206    661 / 522
+//   M 2048                  67 /  61   164 / 153        M 512, D 8192, F 2048    92 /  67    214 / 157
+// Two workgroups per CU write twice the sums and are slower from M = 128 on (D 8192, F 2048, M 128: 48 forward, 98 backward; with one 40 and 87).
+struct TileChoice { bool large; int parts; };
+static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated)
+{
+    const TilePlan large = tile_plan(M, N, 256, gated), small = tile_plan(M, N, 128, gated);
+    if ((int64_t)large.tiles_m * large.tiles_n * problems >= 192) return {true, 1};
+    const int64_t tiles = (int64_t)small.tiles_m * small.tiles_n * problems, steps = (K + 63) / 64 * segments;
+    const int64_t parts = std::min(256 / std::max<int64_t>(tiles, 1), steps / 8);
+    return {false, parts > 1 ? (int)parts : 1};
+}
+static inline int64_t tile_shares(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated)
+{
+    const TileChoice c = choose_tiles(M, N, K, segments, problems, gated);
+    return c.parts > 1 ? c.parts * (gated ? 2 : problems) * M * N : 0;
+}
 // The products of the forward pass (A and B with K contiguous): epilogue kStore, kGated or kGatedKeep.
 hipError_t launch_tiles_forward(TileParams p, int epilogue, hipStream_t stream);
 // dh with its epilogue, and dx = dg Wg + du Wu: B in rows.
@@ -56,7 +97,8 @@ hipError_t launch_tiles_dw(TileParams p, hipStream_t stream);
 
 // ---- products of few rows (atb_stream.hip, atb_q4_stream.hip)
 
-// Whether the gated block of M tokens in bf16 runs on the kernel for few rows.
+// Whether the gated block of M tokens in bf16 runs on the kernel for few rows, whose waves hold at most 32: forward at M = 32, us, 11.9 there and 23 in
+// tiles with D = 1024 and F = 4096, 78 and 92 with D = 4096 and F = 14336.  More would read the weights twice.
 static inline bool ffn_streams(int64_t M) { return M <= 32; }
 
 struct StreamWeight {

@@ -15,9 +15,14 @@ uintptr_t size_of(atb_type t) { return t == ATB_TYPE_F32 ? 4 : 2; }
 // A bf16 matrix that the tile kernels read or write in 16-byte pieces
 bool is_matrix(const void *p, int64_t cols, int64_t ld) { return p && aligned(p, 16) && ld >= cols && ld % 8 == 0 && ld < kMaxPitch; }
 
+bool ffn_lengths(int64_t M, int64_t D, int64_t F)
+{
+    return M >= 0 && M <= kMaxRows && D >= 8 && D % 8 == 0 && D <= kMaxPitch - 8 && F >= 8 && F % 8 == 0 && F <= kMaxPitch - 8;
+}
+
 bool ffn_sizes(const atb_ffn *f)
 {
-    if (!f || f->M < 0 || f->M > kMaxRows || f->D < 8 || f->D % 8 != 0 || f->D > kMaxPitch - 8 || f->F < 8 || f->F % 8 != 0 || f->F > kMaxPitch - 8) return false;
+    if (!f || !ffn_lengths(f->M, f->D, f->F) || !aligned(f->workspace, 16)) return false;
     return is_activation(f->act) && is_matrix(f->w_gate, f->D, f->ld_gate) && is_matrix(f->w_up, f->D, f->ld_up) && is_matrix(f->w_down, f->F, f->ld_down) &&
            (f->M == 0 || is_matrix(f->x, f->D, f->ldx));
 }
@@ -31,9 +36,10 @@ bool is_q4(const atb_q4 *w)
 const uint16_t *u16(const void *p) { return static_cast<const uint16_t *>(p); }
 uint16_t *u16(void *p) { return static_cast<uint16_t *>(p); }
 
-atb::TileParams tiles(int64_t M, int64_t N, int64_t K)
+atb::TileParams tiles(const atb_ffn *f, int64_t M, int64_t N, int64_t K)
 {
     atb::TileParams p = {};
+    p.shares = static_cast<float *>(f->workspace);
     p.M = (int)M;
     p.N = (int)N;
     p.K = (int)K;
@@ -111,6 +117,19 @@ extern "C" size_t atb_ffn_kept_bytes(int64_t M, int64_t F)
     return (size_t)(6 * M * F);
 }
 
+extern "C" size_t atb_ffn_workspace(int64_t M, int64_t D, int64_t F, int keeps)
+{
+    if (!ffn_lengths(M, D, F) || (atb::ffn_streams(M) && !keeps)) return 0;
+    return sizeof(float) * (size_t)std::max(atb::tile_shares(M, F, D, 1, 1, true), atb::tile_shares(M, D, F, 1, 1, false));
+}
+
+extern "C" size_t atb_ffn_backward_workspace(int64_t M, int64_t D, int64_t F)
+{
+    if (!ffn_lengths(M, D, F)) return 0;
+    return sizeof(float) * (size_t)std::max({atb::tile_shares(M, F, D, 1, 1, false), atb::tile_shares(M, D, F, 2, 1, false),       // dh, dx
+                                             atb::tile_shares(F, D, M, 1, 2, false), atb::tile_shares(D, F, M, 1, 1, false)});     // the weights'
+}
+
 extern "C" atb_status atb_ffn_forward(const atb_ffn *f, void *h, void *kept, void *y, int64_t ldy, void *hip_stream)
 {
     if (!ffn_sizes(f)) return ATB_ERR_INVALID_ARG;
@@ -137,7 +156,7 @@ extern "C" atb_status atb_ffn_forward(const atb_ffn *f, void *h, void *kept, voi
         d.y_type = ATB_TYPE_BF16;
         return hip_status(atb::launch_stream(d, stream));
     }
-    atb::TileParams p = tiles(f->M, f->F, f->D);
+    atb::TileParams p = tiles(f, f->M, f->F, f->D);
     operand_a(p, 0, f->x, f->ldx);
     operand_b(p, 0, f->w_gate, f->ld_gate);
     operand_b(p, 1, f->w_up, f->ld_up);
@@ -147,7 +166,7 @@ extern "C" atb_status atb_ffn_forward(const atb_ffn *f, void *h, void *kept, voi
     p.act = f->act;
     const atb_status st = hip_status(atb::launch_tiles_forward(p, kept ? atb::kGatedKeep : atb::kGated, stream));
     if (st != ATB_OK) return st;
-    atb::TileParams d = tiles(f->M, f->D, f->F);
+    atb::TileParams d = tiles(f, f->M, f->D, f->F);
     operand_a(d, 0, h, f->F);
     operand_b(d, 0, f->w_down, f->ld_down);
     d.C[0] = u16(y);
@@ -167,7 +186,7 @@ extern "C" atb_status atb_ffn_backward(const atb_ffn *f, const void *h, const vo
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     atb_status st = ATB_OK;
     if (f->M > 0 && (dx || dw_gate)) {
-        atb::TileParams p = tiles(f->M, f->F, f->D);                 // dh = dy Wd
+        atb::TileParams p = tiles(f, f->M, f->F, f->D);                 // dh = dy Wd
         operand_a(p, 0, dy, lddy);
         operand_b(p, 0, f->w_down, f->ld_down);
         p.C[0] = u16(dgate);
@@ -178,7 +197,7 @@ extern "C" atb_status atb_ffn_backward(const atb_ffn *f, const void *h, const vo
         st = hip_status(atb::launch_tiles_dx(p, atb::kGatedGrad, stream));
     }
     if (st == ATB_OK && f->M > 0 && dx) {
-        atb::TileParams p = tiles(f->M, f->D, f->F);
+        atb::TileParams p = tiles(f, f->M, f->D, f->F);
         operand_a(p, 0, dgate, f->F);
         operand_a(p, 1, dup, f->F);
         operand_b(p, 0, f->w_gate, f->ld_gate);
@@ -191,7 +210,7 @@ extern "C" atb_status atb_ffn_backward(const atb_ffn *f, const void *h, const vo
     // (no tokens: no K-steps, and nothing of the operands is read)
     const int64_t ldx = f->M > 0 ? f->ldx : f->D, ld_dy = f->M > 0 ? lddy : f->D;
     if (st == ATB_OK && dw_gate) {
-        atb::TileParams p = tiles(f->F, f->D, f->M);
+        atb::TileParams p = tiles(f, f->F, f->D, f->M);
         operand_a(p, 0, dgate, f->F);
         operand_a(p, 1, dup, f->F);
         operand_b(p, 0, f->x, ldx);
@@ -203,7 +222,7 @@ extern "C" atb_status atb_ffn_backward(const atb_ffn *f, const void *h, const vo
         st = hip_status(atb::launch_tiles_dw(p, stream));
     }
     if (st == ATB_OK && dw_down) {
-        atb::TileParams p = tiles(f->D, f->F, f->M);
+        atb::TileParams p = tiles(f, f->D, f->F, f->M);
         operand_a(p, 0, dy, ld_dy);
         operand_b(p, 0, h, f->F);
         p.C[0] = u16(dw_down);

@@ -10,6 +10,7 @@
 //   barrier       every wave has all of tile s in registers, so its buffers are free, and tile s + 1 is complete
 //   second half   the MFMAs of k-slice 1; B's tile s + 2 and A's tile s + 3 are asked for, and the fragments of k-slice 0 of tile s + 1 are read
 // so no MFMA behind the barrier waits for LDS, and A's tile s + 2 is still on its way at the barrier.
+// Where there are fewer tiles than CUs a workgroup takes a share of the reduction (choose_tiles).
 #pragma once
 
 #include "atb_activation.h"
@@ -18,6 +19,7 @@
 namespace atb {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 
 template <int TM_, int TN_, int WM_, int WN_>
 struct TileShape {
@@ -95,7 +97,7 @@ struct Source {
 
 template <class S, bool AT, bool BROWS, int EPI>
 struct Tile {
-    static constexpr bool GATED = EPI == kGated || EPI == kGatedKeep;
+    static constexpr bool GATED = is_gated(EPI);
     const TileParams &p;
     const int tid, lane, wave, wm, wn;
     int m0, n0, problem;
@@ -126,7 +128,6 @@ struct Tile {
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
             for (int j = 0; j < S::NI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-        steps = (p.K + S::TK - 1) / S::TK;
     }
 
     // Rows of 64 k: lane l reads row l % 16 of a block of 16 and the 8 k of group l / 16 of a k-slice: chunk l / 16 or, of the second, four on.
@@ -150,25 +151,27 @@ struct Tile {
     // Bytes from an operand's element (row, col) to its end; rows of `cols` elements, ld apart.
     static ATB_DEV int64_t bytes_left(int64_t rows, int64_t cols, int64_t ld, int64_t row, int64_t col) { return ((rows - 1 - row) * ld + cols - col) * 2; }
 
-    // The operands s: a segment of the reduction, or a problem.
-    ATB_DEV void open(int s)
+    // The operands s: a segment of the reduction, or a problem; K-steps first .. end - 1 of it.
+    ATB_DEV void open(int s, int first, int end)
     {
-        a_left = b_left = p.K;
+        const int k0 = first * S::TK;
+        steps = end - first;
+        a_left = b_left = min(p.K, end * S::TK) - k0;
         a_step = AT ? S::TK * 2 * p.lda[s] : S::TK * 2;
         b_step = BROWS ? S::TK * 2 * p.ldb[s] : S::TK * 2;
         Source a, b, up = {};
-        if constexpr (AT) a = {reinterpret_cast<const char *>(p.A[s] + m0), bytes_left(p.K, p.M, p.lda[s], 0, m0)};
-        else a = {reinterpret_cast<const char *>(p.A[s] + (int64_t)m0 * p.lda[s]), bytes_left(p.M, p.K, p.lda[s], m0, 0)};
+        if constexpr (AT) a = {reinterpret_cast<const char *>(p.A[s] + k0 * p.lda[s] + m0), bytes_left(p.K, p.M, p.lda[s], k0, m0)};
+        else a = {reinterpret_cast<const char *>(p.A[s] + m0 * p.lda[s] + k0), bytes_left(p.M, p.K, p.lda[s], m0, k0)};
         a_off.place(tid, p.lda[s]);
         if constexpr (GATED) {
             // rows 0 .. TN / 2 - 1 of the LDS tile are columns of the gate weight, the others the same columns of the up weight
-            b = {reinterpret_cast<const char *>(p.B[0] + (int64_t)n0 * p.ldb[0]), bytes_left(p.N, p.K, p.ldb[0], n0, 0)};
-            up = {reinterpret_cast<const char *>(p.B[1] + (int64_t)n0 * p.ldb[1]), bytes_left(p.N, p.K, p.ldb[1], n0, 0)};
+            b = {reinterpret_cast<const char *>(p.B[0] + n0 * p.ldb[0] + k0), bytes_left(p.N, p.K, p.ldb[0], n0, k0)};
+            up = {reinterpret_cast<const char *>(p.B[1] + n0 * p.ldb[1] + k0), bytes_left(p.N, p.K, p.ldb[1], n0, k0)};
             b_off.place(tid, p.ldb[0]);
             b2_off.place(tid, p.ldb[1]);
         } else {
-            if constexpr (BROWS) b = {reinterpret_cast<const char *>(p.B[s] + n0), bytes_left(p.K, p.N, p.ldb[s], 0, n0)};
-            else b = {reinterpret_cast<const char *>(p.B[s] + (int64_t)n0 * p.ldb[s]), bytes_left(p.N, p.K, p.ldb[s], n0, 0)};
+            if constexpr (BROWS) b = {reinterpret_cast<const char *>(p.B[s] + k0 * p.ldb[s] + n0), bytes_left(p.K, p.N, p.ldb[s], k0, n0)};
+            else b = {reinterpret_cast<const char *>(p.B[s] + n0 * p.ldb[s] + k0), bytes_left(p.N, p.K, p.ldb[s], n0, k0)};
             b_off.place(tid, p.ldb[s]);
         }
         a_src = a;
@@ -360,11 +363,14 @@ struct Tile {
         wait_and_barrier<0>();                                 // LDS is free again
     }
 
-    // Segments one after the other: the few requests in flight are awaited in between.
-    ATB_DEV void multiply()
+    // K-steps first .. end - 1 of the whole reduction.  Segments one after the other: the few requests in flight are awaited in between.
+    ATB_DEV void multiply(int first, int end)
     {
+        const int all = p.steps;
         for (int s = 0; s < p.segments; ++s) {
-            open(p.segments > 1 ? s : problem);
+            const int from = max(first - s * all, 0), to = min(end - s * all, all);
+            if (from >= to) continue;
+            open(p.segments > 1 ? s : problem, from, to);
             multiply_segment();
         }
     }
@@ -392,7 +398,6 @@ struct Tile {
     static ATB_DEV void swap_halves(unsigned &x, unsigned &y)
     {
 #if defined(__HIP_DEVICE_COMPILE__)
-        typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
         const uintx2 r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
         x = r.x;
         y = r.y;
@@ -549,22 +554,42 @@ struct Tile {
         }
     }
 
-    ATB_DEV void finish()
+    // A share of the sums, in fp32: plane 0 has the gate's or the (first problem's) sums, plane 1 the up projection's or the second problem's
+    ATB_DEV void finish_share(int share)
     {
-        if constexpr (EPI == kStore) finish_plain();
+        const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), cols = GATED ? 32 : 64, col0 = n0 + wn * cols + 4 * (lane >> 4);
+        const int64_t plane = (int64_t)p.M * p.N;
+        float *to = p.shares + (int64_t)share * p.planes * plane + (GATED ? 0 : problem * plane);
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i) {
+            const int row = row0 + 16 * i;
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j) {
+                const int col = col0 + 16 * (j % (cols / 16));
+                if (row < p.M && col < p.N) *reinterpret_cast<floatx4 *>(to + (GATED && j >= 2 ? plane : 0) + (int64_t)row * p.N + col) = acc[i][j];
+            }
+        }
+    }
+
+    ATB_DEV void finish(int share)
+    {
+        if constexpr (is_share(EPI)) finish_share(share);
+        else if constexpr (EPI == kStore) finish_plain();
         else if constexpr (EPI == kGatedGrad) finish_grad();
         else finish_gated();
     }
 };
 
-// Tile of workgroup b: workgroups are dealt round-robin to the 8 XCDs, each with an L2 of its own; XCD x takes a contiguous run of tiles,
-// walked in bands of group_m tile rows, so that those resident on it share rows of A and columns of B.
+// Tile and share of workgroup b: workgroups are dealt round-robin to the 8 XCDs, each with an L2 of its own; XCD x takes a contiguous run of the
+// tiles of one share after the other, walked in bands of group_m tile rows, so that those resident on it share rows of A and columns of B.
 template <class S, bool GATED>
-ATB_DEV bool tile_of(const TileParams &p, int b, int &m0, int &n0)
+ATB_DEV bool tile_of(const TileParams &p, int b, int &m0, int &n0, int &share)
 {
-    const int total = p.tiles_m * p.tiles_n, per_xcd = (total + 7) / 8;
-    const int t = (b % 8) * per_xcd + b / 8;
+    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.parts, per_xcd = (total + 7) / 8;
+    int t = (b % 8) * per_xcd + b / 8;
     if (b / 8 >= per_xcd || t >= total) return false;
+    share = t / tiles;
+    t -= share * tiles;
     const int band_size = p.group_m * p.tiles_n, band = t / band_size, in_band = t % band_size;
     const int rows = min(p.group_m, p.tiles_m - band * p.group_m);
     m0 = (band * p.group_m + in_band % rows) * S::TM;
@@ -573,40 +598,109 @@ ATB_DEV bool tile_of(const TileParams &p, int b, int &m0, int &n0)
 }
 
 template <class S, bool AT, bool BROWS, int EPI>
-__global__ void __launch_bounds__(S::NT, S::NT == 512 ? 2 : 2) tile_kernel(const TileParams p)
+__global__ void __launch_bounds__(S::NT, 2) tile_kernel(const TileParams p)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
-    int m0 = 0, n0 = 0;
-    if (!tile_of<S, (EPI == kGated || EPI == kGatedKeep)>(p, blockIdx.x, m0, n0)) return;
+    int m0 = 0, n0 = 0, share = 0;
+    if (!tile_of<S, is_gated(EPI)>(p, blockIdx.x, m0, n0, share)) return;
     Tile<S, AT, BROWS, EPI> tile(p, lds, m0, n0, blockIdx.y);
-    tile.multiply();
-    tile.finish();
+    const int all = p.steps * p.segments;
+    if constexpr (is_share(EPI)) tile.multiply((int)((int64_t)share * all / p.parts), (int)((int64_t)(share + 1) * all / p.parts));
+    else tile.multiply(0, all);
+    tile.finish(share);
 }
 
-template <class S, bool AT, bool BROWS, int EPI>
-hipError_t launch_shape(TileParams &p, hipStream_t stream)
+// The shares of a tile's sums, added in order, and the epilogue: four columns per thread.
+template <int EPI>
+__global__ void __launch_bounds__(256) join_kernel(const TileParams p)
 {
-    constexpr int cols = EPI == kGated || EPI == kGatedKeep ? S::TN / 2 : S::TN;
-    p.tiles_m = (p.M + S::TM - 1) / S::TM;
-    p.tiles_n = (p.N + cols - 1) / cols;
-    p.group_m = 2048 / S::TM;
-    const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
-    if (total > 0x7fffff00) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((tile_kernel<S, AT, BROWS, EPI>), dim3((unsigned)((total + 7) / 8 * 8), p.problems), dim3(S::NT), 0, stream, p);
-    return hipGetLastError();
+    const int pieces = p.N / 4, at = blockIdx.x * 256 + threadIdx.x;
+    if (at >= p.M * pieces) return;
+    const int row = at / pieces, col = (at - row * pieces) * 4;
+    const int64_t plane = (int64_t)p.M * p.N, place = (int64_t)row * p.N + col;
+    constexpr int PLANES = is_gated(EPI) ? 2 : 1;
+    const float *from = p.shares + place + blockIdx.y * plane;
+    floatx4 sum[PLANES] = {};
+#pragma unroll 4
+    for (int s = 0; s < p.parts; ++s, from += p.planes * plane)
+#pragma unroll
+        for (int n = 0; n < PLANES; ++n) sum[n] += *reinterpret_cast<const floatx4 *>(from + n * plane);
+    const int64_t to = (int64_t)row * p.ldc + col;
+    if constexpr (EPI == kStore) {
+        bf16x4 c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = (__bf16)sum[0][e];
+        *reinterpret_cast<bf16x4 *>(p.C[blockIdx.y] + to) = c;
+    } else if constexpr (EPI == kGatedGrad) {
+        uintx2 w[3];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) w[n] = *reinterpret_cast<const uintx2 *>(p.kept + n * plane + place);
+        bf16x4 dg, du;
+        with_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned shift = 16 * (e & 1), gh = w[0][e / 2] >> shift, uh = w[1][e / 2] >> shift, lo = w[2][e / 2] >> shift;
+                const float g = __uint_as_float(gh << 16 | (lo & 0xff) << 8), u = __uint_as_float(uh << 16 | (lo & 0xff00));
+                float a, slope;
+                activate_grad<decltype(act)::value>(g, a, slope);
+                dg[e] = (__bf16)(sum[0][e] * u * slope);
+                du[e] = (__bf16)(sum[0][e] * a);
+            }
+        });
+        *reinterpret_cast<bf16x4 *>(p.C[0] + to) = dg;
+        *reinterpret_cast<bf16x4 *>(p.C[1] + to) = du;
+    } else {
+        bf16x4 h;
+        with_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = (__bf16)(activate<decltype(act)::value>(sum[0][e]) * sum[PLANES - 1][e]);
+        });
+        *reinterpret_cast<bf16x4 *>(p.C[0] + to) = h;
+        if constexpr (EPI == kGatedKeep) {
+            uintx2 w[3] = {};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned shift = 16 * (e & 1), g = __float_as_uint(sum[0][e]), u = __float_as_uint(sum[PLANES - 1][e]);
+                w[0][e / 2] |= g >> 16 << shift;
+                w[1][e / 2] |= u >> 16 << shift;
+                w[2][e / 2] |= ((g >> 8 & 0xff) | (u & 0xff00)) << shift;
+            }
+#pragma unroll
+            for (int n = 0; n < 3; ++n) *reinterpret_cast<uintx2 *>(p.kept + n * plane + place) = w[n];
+        }
+    }
 }
 
 typedef TileShape<256, 256, 2, 4> Tile256;
 typedef TileShape<128, 128, 2, 2> Tile128;
 
-// Tiles of 256 x 256, one workgroup per CU, or of 128 x 128, two per CU.
+template <class S, bool AT, bool BROWS, int EPI>
+hipError_t launch_shape(TileParams &p, hipStream_t stream)
+{
+    const TilePlan plan = tile_plan(p.M, p.N, S::TM, is_gated(EPI));
+    p.tiles_m = plan.tiles_m;
+    p.tiles_n = plan.tiles_n;
+    p.group_m = 2048 / S::TM;
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n * p.parts;
+    if (total > 0x7fffff00) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((tile_kernel<S, AT, BROWS, EPI>), dim3((unsigned)((total + 7) / 8 * 8), p.problems), dim3(S::NT), 0, stream, p);
+    return hipGetLastError();
+}
+
 template <bool AT, bool BROWS, int EPI>
 hipError_t launch_tiles(TileParams &p, hipStream_t stream)
 {
-    const int64_t n = EPI == kGated || EPI == kGatedKeep ? 2 * (int64_t)p.N : p.N;
-    const int64_t large = ((p.M + 255) / 256) * ((n + 255) / 256) * p.problems;
-    if (large >= 192) return launch_shape<Tile256, AT, BROWS, EPI>(p, stream);
-    return launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
+    const TileChoice how = choose_tiles(p.M, p.N, p.K, p.segments, p.problems, is_gated(EPI));
+    p.steps = (p.K + 63) / 64;
+    p.planes = is_gated(EPI) ? 2 : p.problems;
+    p.parts = p.shares ? how.parts : 1;
+    if (how.large) return launch_shape<Tile256, AT, BROWS, EPI>(p, stream);
+    if (p.parts == 1) return launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
+    const hipError_t e = launch_shape<Tile128, AT, BROWS, is_gated(EPI) ? kGatedShare : kShare>(p, stream);
+    if (e != hipSuccess) return e;
+    const int64_t threads = (int64_t)p.M * (p.N / 4);          // (few tiles: far below 2^31)
+    hipLaunchKernelGGL((join_kernel<EPI>), dim3((unsigned)((threads + 255) / 256), p.problems), dim3(256), 0, stream, p);
+    return hipGetLastError();
 }
 
 }  // namespace atb

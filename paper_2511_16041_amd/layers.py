@@ -59,14 +59,14 @@ class FeedForwardState(NamedTuple):
 def feed_forward(x, w_gate, w_up, w_down, act: str = "silu", save: bool = False, stream=None):
     """(act(x w_gate^T) * (x w_up^T)) w_down^T in bf16: x M x D, w_gate and w_up F x D, w_down D x F (as a linear layer's weight is kept), D and F
     multiples of 8.  act: "silu", "gelu" or "gelu_tanh".  save: returns (y, FeedForwardState)."""
-    out = _call("ffn_forward", "atb_ffn_forward", stream, _address("atb_ffn_forward"), _address("atb_ffn_kept_bytes"), x, w_gate, w_up, w_down,
+    out = _call("ffn_forward", "atb_ffn_forward", stream, _address("atb_ffn_forward"), _address("atb_ffn_kept_bytes"), _address("atb_ffn_workspace"), x, w_gate, w_up, w_down,
                 _activation(act), save)
     return (out[0], FeedForwardState(*out[1:], act)) if save else out
 
 
 def feed_forward_backward(dy, x, w_gate, w_up, w_down, state: FeedForwardState, stream=None):
     """(dx, dw_gate, dw_up, dw_down) of feed_forward, in bf16."""
-    return _call("ffn_backward", "atb_ffn_backward", stream, _address("atb_ffn_backward"), _address("atb_ffn_kept_bytes"), dy, x, w_gate, w_up, w_down,
+    return _call("ffn_backward", "atb_ffn_backward", stream, _address("atb_ffn_backward"), _address("atb_ffn_kept_bytes"), _address("atb_ffn_backward_workspace"), dy, x, w_gate, w_up, w_down,
                  state.h, state.kept, _activation(state.act))
 
 

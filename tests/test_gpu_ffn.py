@@ -176,3 +176,46 @@ def test_only_the_gradients_that_are_asked_for():
                                   ptr["dwd"], stream) == 0
         for k, t in out.items():
             assert torch.equal(t, all_of[k]) if k in asked else not t.any(), (asked, k)
+
+
+# few tiles and a long reduction, in each of the products: shares of it are summed apart and joined; shares of unequal length, one that ends in the other segment of dx, a
+# last K-step that is not whole
+@pytest.mark.parametrize("M,D,F", [(1, 1024, 2048), (33, 1032, 1544), (64, 2056, 520), (129, 520, 4104), (2000, 136, 72), (1337, 72, 200)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_reductions_in_shares(M, D, F, act):
+    assert atb.lib().atb_ffn_backward_workspace(M, D, F) > 0
+    x, wg, wu, wd, dy = make(M, D, F, seed=M + D + F, pad=8)
+    want = reference(x, wg, wu, wd, dy, act)
+    first = train(x, wg, wu, wd, dy, act)
+    close(first, want)
+    close({"y": atb.feed_forward(x, wg, wu, wd, act)}, {"y": want["y"]})
+    again = train(x, wg, wu, wd, dy, act)
+    assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+def test_without_a_workspace():
+    """The C entry points without room for shares: the same products in one run each."""
+    import ctypes
+    M, D, F = 100, 1032, 1544
+    x, wg, wu, wd, dy = make(M, D, F, 10)
+    want = reference(x, wg, wu, wd, dy, "silu")
+    f = atb.Ffn(x.data_ptr(), wg.data_ptr(), wu.data_ptr(), wd.data_ptr(), D, D, D, F, M, D, F, 0)
+    new = lambda rows, cols: torch.full((rows, cols), float("nan"), dtype=torch.bfloat16, device="cuda")
+    h, y, kept = new(M, F), new(M, D), torch.empty(6 * M * F, dtype=torch.uint8, device="cuda")
+    dg, du, out = new(M, F), new(M, F), {"dx": new(M, D), "dwg": new(F, D), "dwu": new(F, D), "dwd": new(D, F)}
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert atb.lib().atb_ffn_forward(ctypes.byref(f), h.data_ptr(), kept.data_ptr(), y.data_ptr(), D, stream) == 0
+    assert atb.lib().atb_ffn_backward(ctypes.byref(f), h.data_ptr(), kept.data_ptr(), dy.data_ptr(), D, dg.data_ptr(), du.data_ptr(), out["dx"].data_ptr(), D,
+                                      out["dwg"].data_ptr(), out["dwu"].data_ptr(), out["dwd"].data_ptr(), stream) == 0
+    close({"y": y, **out}, want)
+
+
+def test_shares_of_rows_that_are_not_finite():
+    x, wg, wu, wd, dy = make(70, 1032, 1544, 11)
+    want = reference(x, wg, wu, wd, None, "silu")["y"]
+    x = x.clone()
+    x[3, 1031] = float("nan")
+    y = atb.feed_forward(x, wg, wu, wd)
+    rows = [i for i in range(70) if i != 3]
+    assert not y[3].isfinite().any()
+    close({"y": y[rows]}, {"y": (want[0][rows], want[1][rows])})
