@@ -6,8 +6,9 @@
 // workgroup walks rows a grid apart and keeps its share of both sums in registers, 16 columns per thread; a second kernel adds the
 // workgroups' sums in order.  No atomics: the same bits every time.
 // Rows begin anywhere: 16-byte requests at any element, and the elements of the last, incomplete chunk one by one.
-// Measured (a copy reaches 4.9 TB/s here): 8192 x 4096 in bf16 forward 28.9 us, 4.6 TB/s; backward 38.2 us, 5.3 TB/s (its inputs come partly out of
-// the Infinity Cache), and the sums of dw and db 4.6 us; 3000 x 5001 in fp32 forward 26.9 us, 4.5 TB/s, backward 46.2 us; 1 x 4096 in bf16 3.3 us.
+// Measured (a copy reaches 4.9 TB/s here; inputs of this size come partly out of the Infinity Cache): 8192 x 4096 in bf16 forward 29.1 us, 4.6 TB/s, backward
+// 34.0 us, 5.9 TB/s, and the sums of dw and db 4.7 us; 3000 x 5001 in fp32 forward 26.6 us, 4.5 TB/s, backward 44.8 us; 1 x 4096 in bf16 3.3 us; 4096 x 8200 in bf16
+// 40 us and 42 + 28 + 5: half of the 1024 threads have nothing to do.
 #include "atb_device.h"
 #include "atb_layers.h"
 
@@ -138,14 +139,19 @@ ATB_DEV void row_sums(float (&v)[N], float *scratch)
     }
 }
 
-// T threads per row, NT / T rows of a workgroup at a time.  bf16: workgroups walk rows a grid apart, so that weight and bias are read once (for every row they were twice
-// its own bytes, out of a cache: 8192 x 4096 in 32.1 us, now 28.9) and the next row is on its way while this one is summed.  fp32 has twice the registers for the same
-// elements, and half the waves that way: one row per group, more waves (3000 x 5001 in 26.9 us, walking 31.4).
+// Whether workgroups walk rows a grid apart, so that weight and bias are read once (for every row they were twice its own bytes, out of a cache) and the next row is
+// on its way while this one is summed: bf16 rows of 256 or 512 threads (walking / not, us, tensors in turn that stay in part in the cache: 8192 x 4096 25.4 / 27.9, 4096 x 8192 27.3 / 28.9).  Shorter rows and the
+// longest ones are faster with one row per group and more waves (8192 x 64 9.1 / 7.2, 8192 x 2048 15.2 / 14.2, 4096 x 8200 48.3 / 44.3), and so is fp32, with
+// twice the registers for the same elements (3000 x 5001 31.4 / 26.9).
+template <class X, int T>
+constexpr bool walks() { return sizeof(X) == 2 && T >= 256 && T < 1024; }
+
+// T threads per row, NT / T rows of a workgroup at a time.
 template <class X, class P, int T>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) norm_kernel(const NormParams p, int rounds)
 {
     constexpr int E = Chunk<X>::E, C = kPerThread / E, NT = T < 256 ? 256 : T, R = NT / T;
-    constexpr bool WALKS = sizeof(X) == 2;
+    constexpr bool WALKS = walks<X, T>();
     typedef typename Chunk<X>::vec Vec;
     __shared__ float scratch[2][NT / 64];
     const int t = threadIdx.x % T, group = threadIdx.x / T, D = (int)p.D;
@@ -242,6 +248,13 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormParams p)
         y[i] = (X)(((float)x[i] - mean) * rstd * (w ? (float)w[i] : 1.0f) + (b ? (float)b[i] : 0.0f));
 }
 
+// Four consecutive of a thread's sums
+template <int C, int E>
+ATB_DEV floatx4 quarter(const float (&v)[C][E], int q)
+{
+    return floatx4{v[q * 4 / E][q * 4 % E], v[q * 4 / E][q * 4 % E + 1], v[q * 4 / E][q * 4 % E + 2], v[q * 4 / E][q * 4 % E + 3]};
+}
+
 // dx, and (PARAMS) the workgroup's part of dw and db: partial[workgroup][2][D].
 template <class X, class P, int T, bool PARAMS>
 __global__ void __launch_bounds__(T > kGradThreads ? T : kGradThreads) norm_grad_kernel(const NormParams p, int rounds)
@@ -257,7 +270,7 @@ __global__ void __launch_bounds__(T > kGradThreads ? T : kGradThreads) norm_grad
         for (int e = 0; e < E; ++e) { dw[c][e] = db[c][e] = 0.0f; w[c][e] = 1.0f; }
         if (p.weight) load<P, E>(static_cast<const P *>(p.weight), (c * T + t) * E, D, w[c], 0.0f);
     }
-    // the next row is on its way while this one is summed (8192 x 4096 in 64.4 us without, 38.2 with)
+    // the next row is on its way while this one is summed (8192 x 4096 in 64.4 us without, 38.2 with, as the rest was then)
     typedef typename Chunk<X>::vec Vec;
     Vec next_x[C], next_dy[C];
     float next_mean = 0.0f, next_rstd = 0.0f;
@@ -317,25 +330,43 @@ __global__ void __launch_bounds__(T > kGradThreads ? T : kGradThreads) norm_grad
         }
     }
     if constexpr (PARAMS) {
-        // the row groups one after the other
-        extern __shared__ float sums[];                       // [2][D]
-        float *out = p.partial + (int64_t)blockIdx.x * 2 * D;
-#pragma unroll 1
-        for (int r = 0; r < R; ++r) {
-            if (R > 1) __syncthreads();
-            if (group != r) continue;
-            float *to = r == R - 1 ? out : sums;
+        // the row groups' sums, the upper half of the groups onto the lower one in every step
+        extern __shared__ float sums[];                       // [R / 2][2][16 T]
+        constexpr int ROOM = 2 * kPerThread * T;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+        for (int half = R / 2; half >= 1; half /= 2) {
+            __syncthreads();
+            if (group >= half && group < 2 * half) {
+                float *to = sums + (group - half) * ROOM + t * 4;
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int at = (c * T + t) * E + e;
-                    if (at < D) {
-                        const float a = r > 0 ? sums[at] : 0.0f, b = r > 0 ? sums[D + at] : 0.0f;
-                        to[at] = a + dw[c][e];
-                        to[D + at] = b + db[c][e];
-                    }
+                for (int c = 0; c < kPerThread / 4; ++c) {
+                    *reinterpret_cast<floatx4 *>(to + c * T * 4) = quarter(dw, c);
+                    *reinterpret_cast<floatx4 *>(to + ROOM / 2 + c * T * 4) = quarter(db, c);
                 }
+            }
+            __syncthreads();
+            if (group < half) {
+                const float *from = sums + group * ROOM + t * 4;
+#pragma unroll
+                for (int c = 0; c < kPerThread / 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        dw[c * 4 / E][c * 4 % E + e] += from[c * T * 4 + e];
+                        db[c * 4 / E][c * 4 % E + e] += from[ROOM / 2 + c * T * 4 + e];
+                    }
+            }
+        }
+        if (group > 0) return;
+        float *out = p.partial + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll
+        for (int c = 0; c < kPerThread / 4; ++c) {
+            const int at = (c * 4 / E * T + t) * E + c * 4 % E;
+            const floatx4 a = quarter(dw, c), b = quarter(db, c);
+            const float fa[4] = {a[0], a[1], a[2], a[3]}, fb[4] = {b[0], b[1], b[2], b[3]};
+            if (at < D) {
+                store<float, 4>(out, at, D, fa);
+                store<float, 4>(out + D, at, D, fb);
+            }
         }
     }
 }
@@ -364,20 +395,32 @@ __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormParams p
         dx[i] = (X)(rstd * (g - m0 - xh * m1));
     }
 }
-// ... their dw and db: a thread has one column of the rows blockIdx.y, blockIdx.y + gridDim.y, ..
+// ... their dw and db: a thread has a chunk of columns of the rows blockIdx.y, blockIdx.y + gridDim.y, ..
 template <class X>
 __global__ void __launch_bounds__(256) norm_columns_kernel(const NormParams p)
 {
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= p.D) return;
-    float dw = 0.0f, db = 0.0f;
+    constexpr int E = Chunk<X>::E;
+    const int D = (int)p.D, col = (blockIdx.x * 256 + threadIdx.x) * E;
+    if (col >= D) return;
+    const X *x = static_cast<const X *>(p.x), *dy = static_cast<const X *>(p.dy);
+    float dw[E] = {}, db[E] = {};
+#pragma unroll 4
     for (int64_t row = blockIdx.y; row < p.M; row += gridDim.y) {
-        const float dy = (float)static_cast<const X *>(p.dy)[row * p.lddy + col];
-        dw += dy * (((float)static_cast<const X *>(p.x)[row * p.ldx + col] - p.mean[row]) * p.rstd[row]);
-        db += dy;
+        const typename Chunk<X>::vec g = load_chunk<X>(dy + row * p.lddy, col, D), v = load_chunk<X>(x + row * p.ldx, col, D);
+        const float mean = p.mean[row], rstd = p.rstd[row];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            dw[e] += (float)g[e] * (((float)v[e] - mean) * rstd);
+            db[e] += (float)g[e];
+        }
     }
-    p.partial[((int64_t)blockIdx.y * 2) * p.D + col] = dw;
-    p.partial[((int64_t)blockIdx.y * 2 + 1) * p.D + col] = db;
+    float *out = p.partial + (int64_t)blockIdx.y * 2 * D + col;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (col + e < D) {
+            out[e] = dw[e];
+            out[D + e] = db[e];
+        }
 }
 
 // dw, db = the partial sums added in order: 64 columns per workgroup, 16 waves with a run of the partial sums each.
@@ -418,7 +461,7 @@ template <class X, class P, int T>
 hipError_t forward_of(const NormParams &p, hipStream_t stream)
 {
     constexpr int NT = T < 256 ? 256 : T, R = NT / T, MOST = 256 * (1024 / NT);        // 16 waves per CU
-    const int64_t all = (p.M + R - 1) / R, grid = sizeof(X) > 2 || all < MOST ? all : MOST;
+    const int64_t all = (p.M + R - 1) / R, grid = !walks<X, T>() || all < MOST ? all : MOST;
     hipLaunchKernelGGL((norm_kernel<X, P, T>), dim3((unsigned)grid), dim3(NT), 0, stream, p, (int)((all + grid - 1) / grid));
     return hipGetLastError();
 }
@@ -445,7 +488,7 @@ hipError_t backward_of(const NormParams &p, int64_t grid, hipStream_t stream)
 {
     constexpr int NT = T > kGradThreads ? T : kGradThreads, R = NT / T;
     const int rounds = (int)((p.M + grid * R - 1) / (grid * R));
-    const size_t lds = PARAMS && R > 1 ? (size_t)p.D * 2 * sizeof(float) : 0;        // at most 32 KiB: R > 1 ends with D = 4096
+    const size_t lds = PARAMS && R > 1 ? (size_t)(R / 2) * 2 * kPerThread * T * sizeof(float) : 0;       // 32 KiB
     hipLaunchKernelGGL((norm_grad_kernel<X, P, T, PARAMS>), dim3((unsigned)grid), dim3(NT), lds, stream, p, rounds);
     return hipGetLastError();
 }
@@ -471,7 +514,8 @@ hipError_t backward_long(const NormParams &p, hipStream_t stream)
         e = hipGetLastError();
     }
     if (e != hipSuccess || !(p.dweight || p.dbias)) return e;
-    hipLaunchKernelGGL((norm_columns_kernel<X>), dim3((unsigned)((p.D + 255) / 256), (unsigned)norm_partials(p.M, p.D)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((norm_columns_kernel<X>), dim3((unsigned)((p.D + 256 * Chunk<X>::E - 1) / (256 * Chunk<X>::E)), (unsigned)norm_partials(p.M, p.D)), dim3(256), 0,
+                       stream, p);
     return hipGetLastError();
 }
 
