@@ -251,7 +251,7 @@ typedef struct atb_ffn {
     void *workspace;                            /* DEVICE, 16-byte aligned, of the bytes below for the call; NULL: long reductions of few tokens are not shared out */
 } atb_ffn;
 
-/* Bytes of the workspace of a forward pass (keeps != 0: one with `kept`) and of a backward pass, at most 16 MiB; 0: none is used, or invalid arguments. */
+/* Bytes of the workspace of a forward pass (keeps != 0: one with `kept`) and of a backward pass, at most 64 MiB; 0: none is used, or invalid arguments. */
 size_t atb_ffn_workspace(int64_t M, int64_t D, int64_t F, int keeps);
 size_t atb_ffn_backward_workspace(int64_t M, int64_t D, int64_t F);
 

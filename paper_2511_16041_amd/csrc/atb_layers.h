@@ -64,22 +64,28 @@ static inline TilePlan tile_plan(int64_t M, int64_t N, int tile, bool gated)
     const int64_t cols = gated ? tile / 2 : tile;
     return {(int)((M + tile - 1) / tile), (int)((N + cols - 1) / cols)};
 }
-// Tiles of 256 x 256, one workgroup per CU, where there are nearly as many as CUs (192 of 256; forward pass of D = 4096, F = 14336, us: M = 512, 224 of them in the
-// gated product, 195 against 230 with 128 x 128; M = 2048, 128 of them in the down projection, 670 with small ones there, 717 with large ones).  Otherwise tiles of 128 x 128,
-// two per CU, and where these are at most half as many as CUs the reduction is split into shares, at most one workgroup per CU in all, whose sums go to memory
-// in fp32 and are joined by a second kernel.  A workgroup alone on its CU takes 0.74 us per K-step whatever the others do, so at few tokens the length of the
-// reduction is the time.  A share has at least 8 K-steps: below, the second launch costs what it saves.
+// Tiles of 256 x 256, one workgroup per CU, where there are nearly as many as CUs (192 of 256; forward pass of D = 4096, F = 14336, M = 512, 224 of them in the
+// gated product, us: 195, with 128 x 128 230; M = 2048, 128 of them in the down projection: 670 with small ones there, 717 with large ones).  Otherwise the reduction
+// is split into shares, whose sums go to memory in fp32 and are joined by a second kernel, so that there are nearly as many workgroups as CUs: in large
+// tiles where a share has 28 K-steps or more (more than 128 rows, which would leave half of a tile empty; not gated products, whose reduction is the short one: D = 8192,
+// F = 2048, M = 512 68 without, 70 with), else in tiles of 128 x 128 where these are at most half as many as CUs.  A workgroup alone on its CU takes 0.74 us
+// per K-step whatever the others do, so at few tokens the length of the reduction is the time.  A share has at least 8 K-steps: below, the second launch
+// costs what it saves.  What is left, tiles of 128 x 128, two per CU.
 // Whole / in shares, us, forward and backward (the sum of the kernels and launches):
 //   M 33, D 1024, F 4096    44 /  24    94 /  39        M 33, D 4096, F 14336   225 /  92    492 / 208
 //   M 256                   47 /  35   102 /  52        M 512                   275 / 206    661 / 522
 //   M 2048                  67 /  61   164 / 153        M 512, D 8192, F 2048    92 /  67    214 / 157
-// Two workgroups per CU write twice the sums and are slower from M = 128 on (D 8192, F 2048, M 128: 48 forward, 98 backward; with one 40 and 87).
+// Large tiles in shares / small ones: D 4096, F 14336, M 640 276 / 348 and 538 / 689, M 1024 318 / 370 and 692 / 799, M 2048 593 / 659 and 1259 / 1404; D 2048, F 5504,
+// M 2048 148 / 145 and 340 / 374.  With shares of 24 K-steps D 5120, F 1536, M 1500 takes 199 backward instead of 174.
+// Two workgroups per CU with small tiles write twice the sums and are slower from M = 128 on (D 8192, F 2048, M 128: 48 forward, 98 backward; with one 40 and 87).
 struct TileChoice { bool large; int parts; };
 static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated)
 {
     const TilePlan large = tile_plan(M, N, 256, gated), small = tile_plan(M, N, 128, gated);
     if ((int64_t)large.tiles_m * large.tiles_n * problems >= 192) return {true, 1};
-    const int64_t tiles = (int64_t)small.tiles_m * small.tiles_n * problems, steps = (K + 63) / 64 * segments;
+    const int64_t steps = (K + 63) / 64 * segments, tiles = (int64_t)small.tiles_m * small.tiles_n * problems;
+    const int64_t few = (int64_t)large.tiles_m * large.tiles_n * problems, each = 256 / std::max<int64_t>(few, 1);
+    if (!gated && M > 128 && few > 0 && few * each >= 192 && steps >= 28 * each) return {true, (int)each};
     const int64_t parts = std::min(256 / std::max<int64_t>(tiles, 1), steps / 8);
     return {false, parts > 1 ? (int)parts : 1};
 }

@@ -694,9 +694,9 @@ hipError_t launch_tiles(TileParams &p, hipStream_t stream)
     p.steps = (p.K + 63) / 64;
     p.planes = is_gated(EPI) ? 2 : p.problems;
     p.parts = p.shares ? how.parts : 1;
-    if (how.large) return launch_shape<Tile256, AT, BROWS, EPI>(p, stream);
-    if (p.parts == 1) return launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
-    const hipError_t e = launch_shape<Tile128, AT, BROWS, is_gated(EPI) ? kGatedShare : kShare>(p, stream);
+    constexpr int SHARE = is_gated(EPI) ? kGatedShare : kShare;
+    if (p.parts == 1) return how.large ? launch_shape<Tile256, AT, BROWS, EPI>(p, stream) : launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
+    const hipError_t e = how.large ? launch_shape<Tile256, AT, BROWS, SHARE>(p, stream) : launch_shape<Tile128, AT, BROWS, SHARE>(p, stream);
     if (e != hipSuccess) return e;
     const int64_t threads = (int64_t)p.M * (p.N / 4);          // (few tiles: far below 2^31)
     hipLaunchKernelGGL((join_kernel<EPI>), dim3((unsigned)((threads + 255) / 256), p.problems), dim3(256), 0, stream, p);

@@ -180,7 +180,7 @@ def test_only_the_gradients_that_are_asked_for():
 
 # few tiles and a long reduction, in each of the products: shares of it are summed apart and joined; shares of unequal length, one that ends in the other segment of dx, a
 # last K-step that is not whole
-@pytest.mark.parametrize("M,D,F", [(1, 1024, 2048), (33, 1032, 1544), (64, 2056, 520), (129, 520, 4104), (2000, 136, 72), (1337, 72, 200)])
+@pytest.mark.parametrize("M,D,F", [(1, 1024, 2048), (33, 1032, 1544), (64, 2056, 520), (129, 520, 4104), (2000, 136, 72), (1337, 72, 200), (257, 264, 7176), (3500, 200, 264)])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_reductions_in_shares(M, D, F, act):
     assert atb.lib().atb_ffn_backward_workspace(M, D, F) > 0
@@ -190,6 +190,17 @@ def test_reductions_in_shares(M, D, F, act):
     close(first, want)
     close({"y": atb.feed_forward(x, wg, wu, wd, act)}, {"y": want["y"]})
     again = train(x, wg, wu, wd, dy, act)
+    assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+# the same with enough rows for the large tiles: y and dx; the gradient of the down projection; dh
+@pytest.mark.parametrize("M,D,F", [(2600, 2056, 3592), (3600, 2056, 3080), (2600, 3592, 2056)])
+def test_reductions_in_shares_of_large_tiles(M, D, F):
+    x, wg, wu, wd, dy = make(M, D, F, seed=M + D + F, scale=0.02)
+    want = reference(x, wg, wu, wd, dy, "silu")
+    first = train(x, wg, wu, wd, dy, "silu")
+    close(first, want)
+    again = train(x, wg, wu, wd, dy, "silu")
     assert all(torch.equal(first[k], again[k]) for k in first)
 
 

@@ -209,7 +209,7 @@ def test_workspace_of_a_gated_block():
         for D in (64, 1032, 8192):
             for F in (64, 1544, 16384):
                 for size in (L.atb_ffn_workspace(M, D, F, 0), L.atb_ffn_workspace(M, D, F, 1), L.atb_ffn_backward_workspace(M, D, F)):
-                    assert 0 <= size <= 16 << 20 and size % 16 == 0, (M, D, F)
+                    assert 0 <= size <= 64 << 20 and size % 16 == 0, (M, D, F)
     assert L.atb_ffn_workspace(1, 4096, 14336, 0) == 0 < L.atb_ffn_workspace(1, 4096, 14336, 1)
     for bad in ((-1, 64, 64), (1, 60, 64), (1, 64, 0), (2 ** 23 + 1, 64, 64), (1, 2 ** 22, 64)):
         assert L.atb_ffn_workspace(*bad, 1) == 0 and L.atb_ffn_backward_workspace(*bad) == 0
