@@ -293,7 +293,8 @@ atb_status atb_q4_quantize(const void *W, int64_t ldw, atb_type type, void *pack
 atb_status atb_q4_decode(const atb_q4 *w, void *out, atb_type out_type, void *hip_stream);
 
 /* y = x W^T for few rows: x DEVICE, M x K bf16 (pitch ldx, a multiple of 8; 16-byte aligned), y M x N of y_type (pitch ldy).  Any M up to 2^23
- * is right; weights are read once per 16 rows.  Async on hip_stream. */
+ * is right; weights are read once per 16 rows.  A row with an infinity in x, or whose sums pass fp32's range, is not finite, NaN also where the formula
+ * has an infinity: (16 + q) x is summed and (16 + z) x taken off again.  Async on hip_stream. */
 atb_status atb_q4_matvec(const atb_q4 *w, const void *x, int64_t ldx, void *y, int64_t ldy, atb_type y_type, int64_t M, void *hip_stream);
 
 /* h = act(x Wg^T) o (x Wu^T) in one launch, h M x N bf16: Wg and Wu with the same N, K, group, both with or both without zero points. */

@@ -9,6 +9,8 @@
 // w = s (q - z).  A code becomes bf16 without a conversion: 0x4180 | q << 3 is the number 16 + q.  The MFMAs of a group sum (16 + q) x; one more,
 // shared by all columns, sums x; then y += s (sum - (16 + z) sum of x), all in fp32.  (With 0x4300 | q, 128 + q, the sum that is subtracted again is
 // 30 times the result's size and not 5, and the error against 64 bits 1.8e-6.)
+// Measured: one row, 4096 -> 4096 in groups of 128 5.0 us; gated 4096 -> 14336 in groups of 64 with zero points 22.2 us, 2.9 TB/s, and back 12.8; 16 rows,
+// 8192 -> 8192 in groups of 32 with zero points 17.5 us, 2.3 TB/s: from there on decoding is what counts.
 #include "atb_stream.h"
 
 namespace atb {

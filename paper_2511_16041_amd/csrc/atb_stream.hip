@@ -8,6 +8,7 @@
 // A wave's panels come straight from memory into two LDS buffers of its own (no barriers: it waits for its own requests), the next one on its way
 // while one is multiplied.  A lane of an MFMA needs 16 bytes of one row, its neighbour of the next row; asked for like that, every lane is an
 // access of the L1 (63 a request, 86 000 a CU for the block of 16 tokens of 4096, 14336: 36 of its 48 us).  Into LDS eight neighbouring lanes ask for one line.
+// Measured, 16 rows: gated 4096 -> 14336 46.7 us, 5.0 TB/s; plain 14336 -> 4096 26.7 us, 4.4 TB/s.
 #include "atb_stream.h"
 
 namespace atb {

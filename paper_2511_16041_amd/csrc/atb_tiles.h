@@ -11,6 +11,10 @@
 //   second half   the MFMAs of k-slice 1; B's tile s + 2 and A's tile s + 3 are asked for, and the fragments of k-slice 0 of tile s + 1 are read
 // so no MFMA behind the barrier waits for LDS, and A's tile s + 2 is still on its way at the barrier.
 // Where there are fewer tiles than CUs a workgroup takes a share of the reduction (choose_tiles).
+//
+// Bound: the path by which requests come into a CU (43 to 60 GB/s each; without requests a K-step takes 59 % of its time, without MFMAs 94 %), then power.
+// Measured, M = 8192, D = 4096, F = 14336: gated 1636 us, 1176 TFLOP/s; down 731, 1316; dh with its epilogue 964, 998; dx 1450, 1327; the gradients of
+// the gate and up weights 1500, 1282, of the down weight 884, 1088 (3.5 rounds of tiles).
 #pragma once
 
 #include "atb_activation.h"
@@ -610,7 +614,7 @@ __global__ void __launch_bounds__(S::NT, 2) tile_kernel(const TileParams p)
     tile.finish(share);
 }
 
-// The shares of a tile's sums, added in order, and the epilogue: four columns per thread.
+// The shares of a tile's sums, added in order, and the epilogue: four columns per thread.  Bound: the bytes of the shares (two of 2048 x 4096 in 13.7 us, 6.1 TB/s).
 template <int EPI>
 __global__ void __launch_bounds__(256) join_kernel(const TileParams p)
 {

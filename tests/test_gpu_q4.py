@@ -1,6 +1,6 @@
 """4-bit weights on the GPU: storage against its definition, products against 64 bits.
 
-Tolerances of the products.  The accumulators sum (128 + q) x over a group, at most 143 |x| a term and up to 128 terms, and subtract (128 + z) times the sum of
+Tolerances of the products.  The accumulators sum (c + q) x over a group, with c = 16 or at most 128, so at most 143 |x| a term and up to 128 terms, and subtract (c + z) times the sum of
 x: 2^-20 of 143 s sum |x| covers the roundings of such a chain (128 of 2^-24, added as a random walk: 11 of them); adding groups costs 2^-20 of the result's terms.  A bf16 result adds 2^-8 of its
 size; the block's inner activations are rounded to bf16, 2^-8 of theirs."""
 import numpy as np
