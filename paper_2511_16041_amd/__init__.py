@@ -5,6 +5,8 @@ for device memory and streams, nothing else.  There is no CPU fallback: if the
 shared library is missing or a call fails, an exception is raised.
 The calls that launch a GEMM or the quantiser go through a small extension
 module (csrc/atb_binding.cpp), everything else through ctypes.
+The operators of a transformer's feed-forward sublayer (layer norm, the gated
+block, products with 4-bit weights) are in layers.py and reached from here.
 """
 from __future__ import annotations
 
