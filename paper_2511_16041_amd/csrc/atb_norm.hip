@@ -457,6 +457,29 @@ int threads_of(int64_t D)
     return t;
 }
 
+// Rows of a launch with a workgroup a row: of up to 1024 threads, and a launch has fewer than 2^32.
+constexpr int64_t kMostRows = (int64_t)1 << 21;
+
+// f, called with the rows of p, kMostRows of them at a time
+template <class F>
+hipError_t by_rows(const NormParams &p, F f)
+{
+    const int64_t size = p.x_type == ATB_TYPE_F32 ? 4 : 2;
+    for (int64_t row = 0; row < p.M; row += kMostRows) {
+        NormParams part = p;
+        part.M = p.M - row < kMostRows ? p.M - row : kMostRows;
+        if (p.x) part.x = static_cast<const char *>(p.x) + row * p.ldx * size;
+        if (p.dy) part.dy = static_cast<const char *>(p.dy) + row * p.lddy * size;
+        if (p.y) part.y = static_cast<char *>(p.y) + row * p.ldy * size;
+        if (p.dx) part.dx = static_cast<char *>(p.dx) + row * p.lddx * size;
+        if (p.mean) part.mean = p.mean + row;
+        if (p.rstd) part.rstd = p.rstd + row;
+        const hipError_t e = f(part);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <class X, class P, int T>
 hipError_t forward_of(const NormParams &p, hipStream_t stream)
 {
@@ -510,8 +533,10 @@ hipError_t backward_long(const NormParams &p, hipStream_t stream)
     if (p.dx && p.D <= kMaxRow) {
         e = backward_of<X, P, 1024, false>(p, p.M < 2048 ? p.M : 2048, stream);
     } else if (p.dx) {
-        hipLaunchKernelGGL((norm_grad_long_kernel<X, P>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
-        e = hipGetLastError();
+        e = by_rows(p, [&](const NormParams &part) {
+            hipLaunchKernelGGL((norm_grad_long_kernel<X, P>), dim3((unsigned)part.M), dim3(1024), 0, stream, part);
+            return hipGetLastError();
+        });
     }
     if (e != hipSuccess || !(p.dweight || p.dbias)) return e;
     hipLaunchKernelGGL((norm_columns_kernel<X>), dim3((unsigned)((p.D + 256 * Chunk<X>::E - 1) / (256 * Chunk<X>::E)), (unsigned)norm_partials(p.M, p.D)), dim3(256), 0,
@@ -551,9 +576,10 @@ int64_t norm_partials(int64_t M, int64_t D)
 
 hipError_t launch_norm(const NormParams &p, hipStream_t stream)
 {
-    if (p.M == 0) return hipSuccess;
-    if (p.x_type == ATB_TYPE_F32) return p.w_type == ATB_TYPE_F32 ? forward<float, float>(p, stream) : forward<float, __bf16>(p, stream);
-    return p.w_type == ATB_TYPE_F32 ? forward<__bf16, float>(p, stream) : forward<__bf16, __bf16>(p, stream);
+    return by_rows(p, [&](const NormParams &part) {
+        if (part.x_type == ATB_TYPE_F32) return part.w_type == ATB_TYPE_F32 ? forward<float, float>(part, stream) : forward<float, __bf16>(part, stream);
+        return part.w_type == ATB_TYPE_F32 ? forward<__bf16, float>(part, stream) : forward<__bf16, __bf16>(part, stream);
+    });
 }
 
 hipError_t launch_norm_backward(const NormParams &p, hipStream_t stream)

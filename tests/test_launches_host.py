@@ -1,0 +1,65 @@
+"""The launches of the feed-forward sublayer's operators, recorded without a GPU (tests/native/launches.cpp): none leaves what the runtime takes, fewer
+than 2^32 threads in x and at most 65535 workgroups in y, and together they take every row once."""
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2511_16041_amd import build
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM_INC = "/opt/rocm/include"
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir(ROCM_INC), reason="needs g++ and the HIP headers")
+MOST_ROWS = 2 ** 23
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    """launches(operator, sizes ..) -> [{"grid": workgroups in x and y, "block": threads in x and y, and what the program prints of the arguments}]"""
+    lib = build.ensure_built()
+    exe = str(tmp_path_factory.mktemp("launches") / "launches")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INC, "-I", os.path.join(ROOT, "include"), "-I", build.CSRC,
+                    os.path.join(ROOT, "tests", "native", "launches.cpp"), "-o", exe, "-rdynamic", lib, "-Wl,-rpath," + os.path.dirname(lib)], check=True)
+
+    def run(*args):
+        out = subprocess.run([exe] + [str(a) for a in args], capture_output=True, text=True, check=True, timeout=60).stdout.splitlines()
+        assert out[-1] == "status 0", (args, out[-1])
+        found = []
+        for line in out[:-1]:
+            n = [int(x) for x in re.match(r"launch (\d+) (\d+) (\d+) (\d+)", line).groups()]
+            found.append({"grid": n[:2], "block": n[2:], **{k: int(x) for k, x in re.findall(r" ([a-z]+) (-?\d+)", line)}})
+        for one in found:
+            assert one["grid"][0] * one["block"][0] < 2 ** 32 and 1 <= one["grid"][1] <= 65535, (args, one)
+        return found
+    return run
+
+
+def consecutive(found, M, pitches):
+    """The launches take rows 0 .. M - 1 in order; pitches: bytes from a row to the next in each operand."""
+    row = 0
+    for one in found:
+        for name, pitch in pitches.items():
+            assert one[name] == row * pitch, (one, name)
+        row += one["rows"]
+    assert row == M
+
+
+@pytest.mark.parametrize("type", [0, 1])
+@pytest.mark.parametrize("D", [1, 64, 1000, 2049, 4097, 8192, 8193, 16384, 16385, 2 ** 24])
+def test_layer_norm(launches, D, type):
+    size = 4 if type else 2
+    for M in (1, 1000, 2 ** 21 - 1, 2 ** 21, 2 ** 22 + 3, MOST_ROWS):
+        found = launches("norm", M, D, type, D + 8, D + 16)
+        consecutive(found, M, {"x": (D + 8) * size, "y": (D + 16) * size, "mean": 4, "rstd": 4})
+
+
+@pytest.mark.parametrize("type", [0, 1])
+@pytest.mark.parametrize("D", [1, 1000, 4097, 8193, 16384, 16385, 2 ** 24])
+def test_layer_norm_backward(launches, D, type):
+    size = 4 if type else 2
+    for M in (1, 1000, 2 ** 22 + 3, MOST_ROWS):
+        found = launches("norm_backward", M, D, type, D + 8, D + 16, D + 24, 0)
+        consecutive(found, M, {"x": (D + 8) * size, "dy": (D + 16) * size, "dx": (D + 24) * size, "mean": 4, "rstd": 4})
+        launches("norm_backward", M, D, type, D + 8, D + 16, D + 24, 1)
