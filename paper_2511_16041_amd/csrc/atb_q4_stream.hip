@@ -285,11 +285,19 @@ hipError_t launch_zeros(const StreamParams &p, hipStream_t stream)
 
 }  // namespace
 
+// A launch has at most 65535 workgroups in y, of 16 rows each.
 hipError_t launch_q4_stream(const StreamParams &p, hipStream_t stream)
 {
-    if (p.group == 32) return launch_zeros<32>(p, stream);
-    if (p.group == 64) return launch_zeros<64>(p, stream);
-    return launch_zeros<128>(p, stream);
+    constexpr int MOST = 65535 * 16;
+    for (int row = 0; row < p.M; row += MOST) {
+        StreamParams part = p;
+        part.M = p.M - row < MOST ? p.M - row : MOST;
+        part.x = p.x + row * p.ldx;
+        part.y = static_cast<char *>(p.y) + row * p.ldy * (p.y_type == ATB_TYPE_F32 ? 4 : 2);
+        const hipError_t e = p.group == 32 ? launch_zeros<32>(part, stream) : p.group == 64 ? launch_zeros<64>(part, stream) : launch_zeros<128>(part, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace atb

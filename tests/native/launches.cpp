@@ -44,6 +44,9 @@ extern "C" hipError_t hipLaunchKernel(const void *, dim3 grid, dim3 block, void 
     } else if (g_operator == "norm_backward") {
         const auto &p = *static_cast<const atb::NormParams *>(args[0]);
         std::printf(" rows %lld x %lld dy %lld dx %lld mean %lld rstd %lld", (long long)p.M, off(p.x, kX), off(p.dy, kY), off(p.dx, kZ), off(p.mean, kMean), off(p.rstd, kRstd));
+    } else if (g_operator == "q4" || g_operator == "q4_gated") {
+        const auto &p = *static_cast<const atb::StreamParams *>(args[0]);
+        std::printf(" rows %lld x %lld y %lld", (long long)p.M, off(p.x, kX), off(p.y, kY));
     }
     std::printf("\n");
     return hipSuccess;
@@ -61,6 +64,13 @@ int main(int argc, char **argv)
     else if (g_operator == "norm_backward")    // M, D, type, pitch of x, pitch of dy, pitch of dx, whether the parameters' gradients are asked for
         st = atb_layer_norm_backward(at(kY), v[4], at(kX), v[3], static_cast<float *>(at(kMean)), static_cast<float *>(at(kRstd)), at(kW), at(kZ), v[5], v[6] ? at(kW) : nullptr,
                                      v[6] ? at(kW) : nullptr, v[6] ? at(kW) : nullptr, v[0], v[1], (atb_type)v[2], (atb_type)v[2], nullptr);
+    else if (g_operator == "q4") {             // M, N, K, group, type of y, pitch of x, pitch of y
+        const atb_q4 w = {at(kW), at(kW), at(kW), v[1], v[2], (int)v[3]};
+        st = atb_q4_matvec(&w, at(kX), v[5], at(kY), v[6], (atb_type)v[4], v[0], nullptr);
+    } else if (g_operator == "q4_gated") {     // M, N, K, group, pitch of x, pitch of h
+        const atb_q4 w = {at(kW), at(kW), nullptr, v[1], v[2], (int)v[3]};
+        st = atb_q4_gated(&w, &w, ATB_ACT_SILU, at(kX), v[4], at(kY), v[5], v[0], nullptr);
+    }
     std::printf("status %d\n", st);
     return 0;
 }

@@ -162,3 +162,9 @@ def test_another_stream():
     again = atb.q4_matvec(x, w, stream=side)
     side.synchronize()
     assert torch.equal(first, again)
+
+
+def test_rows_of_more_than_one_launch():
+    """65535 blocks of 16 rows a launch: every row, on both sides of that."""
+    w, x = random_weight(24, 64, 32, True, 13), rows(65535 * 16 + 5, 64, 14, pad=8)
+    check(atb.q4_matvec(x, w, torch.float32), x, w)

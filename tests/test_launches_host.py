@@ -63,3 +63,14 @@ def test_layer_norm_backward(launches, D, type):
         found = launches("norm_backward", M, D, type, D + 8, D + 16, D + 24, 0)
         consecutive(found, M, {"x": (D + 8) * size, "dy": (D + 16) * size, "dx": (D + 24) * size, "mean": 4, "rstd": 4})
         launches("norm_backward", M, D, type, D + 8, D + 16, D + 24, 1)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N", [1, 4096, 4097, 8192, 8193, 2 ** 24])
+def test_products_with_4_bit_weights(launches, N, group):
+    K = 2 * group
+    for M in (1, 64, 2 ** 20 - 16, 2 ** 20 - 15, 2 ** 20, MOST_ROWS):
+        for type in (0, 1):
+            found = launches("q4", M, N, K, group, type, K + 8, N + 3)
+            consecutive(found, M, {"x": 2 * (K + 8), "y": (4 if type else 2) * (N + 3)})
+        consecutive(launches("q4_gated", M, N, K, group, K + 8, N + 3), M, {"x": 2 * (K + 8), "y": 2 * (N + 3)})
