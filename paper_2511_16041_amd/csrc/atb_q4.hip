@@ -64,14 +64,30 @@ __global__ void __launch_bounds__(256) q4_decode_kernel(const uint8_t *__restric
     for (int e = 0; e < 8; ++e) out[n * K + k + e] = v[e];
 }
 
+// f(first row, rows, workgroups of 256 threads), called with N rows of `threads` threads each: as many at a time as a launch, which has fewer than 2^32 threads, can take.
+template <class F>
+hipError_t by_rows(int64_t N, int64_t threads, F f)
+{
+    const int64_t most = ((int64_t)1 << 31) / threads;                // K <= 2^22: a row has at most 2^20
+    for (int64_t row = 0; row < N; row += most) {
+        const int64_t rows = N - row < most ? N - row : most;
+        f(row, rows, dim3((unsigned)((rows * threads + 255) / 256)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <class X, int G>
 hipError_t quantize(const void *w, int64_t ldw, uint8_t *packed, uint16_t *scales, uint8_t *zeros, int64_t N, int64_t K, hipStream_t stream)
 {
-    const int64_t grid = (N * (K / 4) + 255) / 256;
-    if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-    if (zeros) hipLaunchKernelGGL((q4_quantize_kernel<X, G, true>), dim3((unsigned)grid), dim3(256), 0, stream, static_cast<const X *>(w), ldw, packed, scales, zeros, N, K);
-    else hipLaunchKernelGGL((q4_quantize_kernel<X, G, false>), dim3((unsigned)grid), dim3(256), 0, stream, static_cast<const X *>(w), ldw, packed, scales, zeros, N, K);
-    return hipGetLastError();
+    return by_rows(N, K / 4, [&](int64_t row, int64_t rows, dim3 grid) {
+        const X *from = static_cast<const X *>(w) + row * ldw;
+        uint8_t *codes = packed + row * (K / 2);
+        uint16_t *s = scales + row * (K / G);
+        if (zeros) hipLaunchKernelGGL((q4_quantize_kernel<X, G, true>), grid, dim3(256), 0, stream, from, ldw, codes, s, zeros + row * (K / G), rows, K);
+        else hipLaunchKernelGGL((q4_quantize_kernel<X, G, false>), grid, dim3(256), 0, stream, from, ldw, codes, s, zeros, rows, K);
+    });
 }
 
 template <class X>
@@ -80,6 +96,15 @@ hipError_t quantize(const void *w, int64_t ldw, uint8_t *packed, uint16_t *scale
     if (group == 32) return quantize<X, 32>(w, ldw, packed, scales, zeros, N, K, stream);
     if (group == 64) return quantize<X, 64>(w, ldw, packed, scales, zeros, N, K, stream);
     return quantize<X, 128>(w, ldw, packed, scales, zeros, N, K, stream);
+}
+
+template <class X>
+hipError_t decode(const uint8_t *packed, const uint16_t *scales, const uint8_t *zeros, void *out, int64_t N, int64_t K, int group, hipStream_t stream)
+{
+    return by_rows(N, K / 8, [&](int64_t row, int64_t rows, dim3 grid) {
+        hipLaunchKernelGGL((q4_decode_kernel<X>), grid, dim3(256), 0, stream, packed + row * (K / 2), scales + row * (K / group), zeros ? zeros + row * (K / group) : nullptr,
+                           static_cast<X *>(out) + row * K, rows, K, group);
+    });
 }
 
 }  // namespace
@@ -94,11 +119,8 @@ hipError_t launch_q4_quantize(const void *w, int w_type, int64_t ldw, uint8_t *p
 hipError_t launch_q4_decode(const uint8_t *packed, const uint16_t *scales, const uint8_t *zeros, void *out, int out_type,
                             int64_t N, int64_t K, int group, hipStream_t stream)
 {
-    const int64_t grid = (N * (K / 8) + 255) / 256;
-    if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-    if (out_type == ATB_TYPE_F32) hipLaunchKernelGGL((q4_decode_kernel<float>), dim3((unsigned)grid), dim3(256), 0, stream, packed, scales, zeros, static_cast<float *>(out), N, K, group);
-    else hipLaunchKernelGGL((q4_decode_kernel<__bf16>), dim3((unsigned)grid), dim3(256), 0, stream, packed, scales, zeros, static_cast<__bf16 *>(out), N, K, group);
-    return hipGetLastError();
+    if (out_type == ATB_TYPE_F32) return decode<float>(packed, scales, zeros, out, N, K, group, stream);
+    return decode<__bf16>(packed, scales, zeros, out, N, K, group, stream);
 }
 
 }  // namespace atb

@@ -16,6 +16,7 @@ const int64_t kX = (int64_t)1 << 40, kY = (int64_t)1 << 42, kZ = (int64_t)1 << 4
 
 void *at(int64_t address) { return reinterpret_cast<void *>(address); }
 long long off(const void *p, int64_t base) { return (long long)(reinterpret_cast<int64_t>(p) - base); }
+template <class T> T argument(void **args, int i) { return *static_cast<T *>(args[i]); }
 
 }  // namespace
 
@@ -47,6 +48,12 @@ extern "C" hipError_t hipLaunchKernel(const void *, dim3 grid, dim3 block, void 
     } else if (g_operator == "q4" || g_operator == "q4_gated") {
         const auto &p = *static_cast<const atb::StreamParams *>(args[0]);
         std::printf(" rows %lld x %lld y %lld", (long long)p.M, off(p.x, kX), off(p.y, kY));
+    } else if (g_operator == "q4_quantize") {      // w, ldw, packed, scales, zeros, N, K
+        std::printf(" rows %lld w %lld packed %lld scales %lld zeros %lld", (long long)argument<int64_t>(args, 5), off(argument<void *>(args, 0), kX), off(argument<void *>(args, 2), kY),
+                    off(argument<void *>(args, 3), kZ), off(argument<void *>(args, 4), kW));
+    } else if (g_operator == "q4_decode") {        // packed, scales, zeros, out, N, K, group
+        std::printf(" rows %lld packed %lld scales %lld zeros %lld out %lld", (long long)argument<int64_t>(args, 4), off(argument<void *>(args, 0), kY), off(argument<void *>(args, 1), kZ),
+                    off(argument<void *>(args, 2), kW), off(argument<void *>(args, 3), kX));
     }
     std::printf("\n");
     return hipSuccess;
@@ -70,6 +77,12 @@ int main(int argc, char **argv)
     } else if (g_operator == "q4_gated") {     // M, N, K, group, pitch of x, pitch of h
         const atb_q4 w = {at(kW), at(kW), nullptr, v[1], v[2], (int)v[3]};
         st = atb_q4_gated(&w, &w, ATB_ACT_SILU, at(kX), v[4], at(kY), v[5], v[0], nullptr);
+    }
+    else if (g_operator == "q4_quantize")      // N, K, group, type, pitch
+        st = atb_q4_quantize(at(kX), v[4], (atb_type)v[3], at(kY), at(kZ), at(kW), v[0], v[1], (int)v[2], nullptr);
+    else if (g_operator == "q4_decode") {      // N, K, group, type
+        const atb_q4 w = {at(kY), at(kZ), at(kW), v[0], v[1], (int)v[2]};
+        st = atb_q4_decode(&w, at(kX), (atb_type)v[3], nullptr);
     }
     std::printf("status %d\n", st);
     return 0;

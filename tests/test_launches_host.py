@@ -74,3 +74,12 @@ def test_products_with_4_bit_weights(launches, N, group):
             found = launches("q4", M, N, K, group, type, K + 8, N + 3)
             consecutive(found, M, {"x": 2 * (K + 8), "y": (4 if type else 2) * (N + 3)})
         consecutive(launches("q4_gated", M, N, K, group, K + 8, N + 3), M, {"x": 2 * (K + 8), "y": 2 * (N + 3)})
+
+
+@pytest.mark.parametrize("type", [0, 1])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(1, 128), (1000, 4096), (2 ** 13, 2 ** 20), (2 ** 14 - 1, 2 ** 20), (2 ** 14 + 7, 2 ** 20), (2 ** 24, 128), (2 ** 24, 4224), (2 ** 20 + 3, 2 ** 18), (2 ** 13 + 1, 2 ** 22)])
+def test_quantising_and_decoding(launches, N, K, group, type):
+    size, G = (4 if type else 2), K // group
+    consecutive(launches("q4_quantize", N, K, group, type, K + 3), N, {"w": size * (K + 3), "packed": K // 2, "scales": 2 * G, "zeros": G})
+    consecutive(launches("q4_decode", N, K, group, type), N, {"out": size * K, "packed": K // 2, "scales": 2 * G, "zeros": G})
