@@ -78,11 +78,13 @@ static inline TilePlan tile_plan(int64_t M, int64_t N, int tile, bool gated)
 // Large tiles in shares / small ones: D 4096, F 14336, M 640 276 / 348 and 538 / 689, M 1024 318 / 370 and 692 / 799, M 2048 593 / 659 and 1259 / 1404; D 2048, F 5504,
 // M 2048 148 / 145 and 340 / 374.  With shares of 24 K-steps D 5120, F 1536, M 1500 takes 199 backward instead of 174.
 // Two workgroups per CU with small tiles write twice the sums and are slower from M = 128 on (D 8192, F 2048, M 128: 48 forward, 98 backward; with one 40 and 87).
+// Without room for shares (`room`) what is left takes their place.
 struct TileChoice { bool large; int parts; };
-static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated)
+static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated, bool room)
 {
     const TilePlan large = tile_plan(M, N, 256, gated), small = tile_plan(M, N, 128, gated);
     if ((int64_t)large.tiles_m * large.tiles_n * problems >= 192) return {true, 1};
+    if (!room) return {false, 1};
     const int64_t steps = (K + 63) / 64 * segments, tiles = (int64_t)small.tiles_m * small.tiles_n * problems;
     const int64_t few = (int64_t)large.tiles_m * large.tiles_n * problems, each = 256 / std::max<int64_t>(few, 1);
     if (!gated && M > 128 && few > 0 && few * each >= 192 && steps >= 28 * each) return {true, (int)each};
@@ -91,7 +93,7 @@ static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segme
 }
 static inline int64_t tile_shares(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated)
 {
-    const TileChoice c = choose_tiles(M, N, K, segments, problems, gated);
+    const TileChoice c = choose_tiles(M, N, K, segments, problems, gated, true);
     return c.parts > 1 ? c.parts * (gated ? 2 : problems) * M * N : 0;
 }
 // The products of the forward pass (A and B with K contiguous): epilogue kStore, kGated or kGatedKeep.

@@ -694,10 +694,10 @@ hipError_t launch_shape(TileParams &p, hipStream_t stream)
 template <bool AT, bool BROWS, int EPI>
 hipError_t launch_tiles(TileParams &p, hipStream_t stream)
 {
-    const TileChoice how = choose_tiles(p.M, p.N, p.K, p.segments, p.problems, is_gated(EPI));
+    const TileChoice how = choose_tiles(p.M, p.N, p.K, p.segments, p.problems, is_gated(EPI), p.shares != nullptr);
     p.steps = (p.K + 63) / 64;
     p.planes = is_gated(EPI) ? 2 : p.problems;
-    p.parts = p.shares ? how.parts : 1;
+    p.parts = how.parts;
     constexpr int SHARE = is_gated(EPI) ? kGatedShare : kShare;
     if (p.parts == 1) return how.large ? launch_shape<Tile256, AT, BROWS, EPI>(p, stream) : launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
     const hipError_t e = how.large ? launch_shape<Tile256, AT, BROWS, SHARE>(p, stream) : launch_shape<Tile128, AT, BROWS, SHARE>(p, stream);

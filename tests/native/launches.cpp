@@ -48,6 +48,9 @@ extern "C" hipError_t hipLaunchKernel(const void *, dim3 grid, dim3 block, void 
     } else if (g_operator == "q4" || g_operator == "q4_gated") {
         const auto &p = *static_cast<const atb::StreamParams *>(args[0]);
         std::printf(" rows %lld x %lld y %lld", (long long)p.M, off(p.x, kX), off(p.y, kY));
+    } else if (g_operator == "ffn" || g_operator == "ffn_backward") {
+        const auto &p = *static_cast<const atb::TileParams *>(args[0]);
+        std::printf(" m %d n %d k %d parts %d planes %d", p.M, p.N, p.K * p.segments, p.parts, p.planes);
     } else if (g_operator == "q4_quantize") {      // w, ldw, packed, scales, zeros, N, K
         std::printf(" rows %lld w %lld packed %lld scales %lld zeros %lld", (long long)argument<int64_t>(args, 5), off(argument<void *>(args, 0), kX), off(argument<void *>(args, 2), kY),
                     off(argument<void *>(args, 3), kZ), off(argument<void *>(args, 4), kW));
@@ -83,6 +86,11 @@ int main(int argc, char **argv)
     else if (g_operator == "q4_decode") {      // N, K, group, type
         const atb_q4 w = {at(kY), at(kZ), at(kW), v[0], v[1], (int)v[2]};
         st = atb_q4_decode(&w, at(kX), (atb_type)v[3], nullptr);
+    }
+    else if (g_operator == "ffn" || g_operator == "ffn_backward") {      // M, D, F, whether there is a workspace, whether the forward pass keeps what the backward pass needs
+        const atb_ffn f = {at(kX), at(kW), at(kW), at(kW), v[1], v[1], v[1], v[2], v[0], v[1], v[2], ATB_ACT_SILU, v[3] ? at(kZ) : nullptr};
+        if (g_operator == "ffn") st = atb_ffn_forward(&f, at(kY), v[4] ? at(kMean) : nullptr, at(kY), v[1], nullptr);
+        else st = atb_ffn_backward(&f, at(kY), at(kMean), at(kY), v[1], at(kW), at(kW), at(kX), v[1], at(kW), at(kW), at(kW), nullptr);
     }
     std::printf("status %d\n", st);
     return 0;

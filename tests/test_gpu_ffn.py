@@ -230,3 +230,20 @@ def test_shares_of_rows_that_are_not_finite():
     rows = [i for i in range(70) if i != 3]
     assert not y[3].isfinite().any()
     close({"y": y[rows]}, {"y": (want[0][rows], want[1][rows])})
+
+
+def test_without_a_workspace_where_it_would_hold_shares_of_large_tiles():
+    """The C entry points without room for shares, at a size whose y and dx are large tiles in shares with it."""
+    import ctypes
+    M, D, F = 2600, 2056, 3592
+    x, wg, wu, wd, dy = make(M, D, F, 12, scale=0.02)
+    want = reference(x, wg, wu, wd, dy, "silu")
+    f = atb.Ffn(x.data_ptr(), wg.data_ptr(), wu.data_ptr(), wd.data_ptr(), D, D, D, F, M, D, F, 0)
+    new = lambda rows, cols: torch.full((rows, cols), float("nan"), dtype=torch.bfloat16, device="cuda")
+    h, y, kept = new(M, F), new(M, D), torch.empty(6 * M * F, dtype=torch.uint8, device="cuda")
+    dg, du, out = new(M, F), new(M, F), {"dx": new(M, D), "dwg": new(F, D), "dwu": new(F, D), "dwd": new(D, F)}
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert atb.lib().atb_ffn_forward(ctypes.byref(f), h.data_ptr(), kept.data_ptr(), y.data_ptr(), D, stream) == 0
+    assert atb.lib().atb_ffn_backward(ctypes.byref(f), h.data_ptr(), kept.data_ptr(), dy.data_ptr(), D, dg.data_ptr(), du.data_ptr(), out["dx"].data_ptr(), D,
+                                      out["dwg"].data_ptr(), out["dwu"].data_ptr(), out["dwd"].data_ptr(), stream) == 0
+    close({"y": y, **out}, want)

@@ -83,3 +83,26 @@ def test_quantising_and_decoding(launches, N, K, group, type):
     size, G = (4 if type else 2), K // group
     consecutive(launches("q4_quantize", N, K, group, type, K + 3), N, {"w": size * (K + 3), "packed": K // 2, "scales": 2 * G, "zeros": G})
     consecutive(launches("q4_decode", N, K, group, type), N, {"out": size * K, "packed": K // 2, "scales": 2 * G, "zeros": G})
+
+
+BLOCKS = [(33, 1032, 1544), (129, 520, 4104), (257, 264, 7176), (500, 4096, 14336), (1000, 2048, 5504), (1500, 2056, 5000), (2000, 136, 72), (2600, 2056, 3592), (2600, 3592, 2056), (3600, 2056, 3080),
+          (8192, 4096, 14336)]
+
+
+@pytest.mark.parametrize("M,D,F", BLOCKS)
+def test_shares_fit_the_workspace_of_a_gated_block(launches, M, D, F):
+    import paper_2511_16041_amd as atb
+    L = atb.lib()
+    for name, size in (("ffn", L.atb_ffn_workspace(M, D, F, 1)), ("ffn_backward", L.atb_ffn_backward_workspace(M, D, F))):
+        found = launches(name, M, D, F, 1, 1)
+        assert max(one["parts"] * one["planes"] * one["m"] * one["n"] * 4 for one in found if one["parts"] > 1) == size if size else all(one["parts"] == 1 for one in found)
+
+
+@pytest.mark.parametrize("M,D,F", BLOCKS)
+def test_without_a_workspace_large_tiles_are_nearly_as_many_as_cus(launches, M, D, F):
+    """Large tiles (512 threads) that are chosen because their shares fill the CUs have no business where there is no room for shares."""
+    for name in ("ffn", "ffn_backward"):
+        found = launches(name, M, D, F, 0, 1)
+        assert all(one["parts"] == 1 for one in found)
+        for one in found:
+            assert one["block"][0] == 256 or one["grid"][0] * one["grid"][1] >= 192, one
