@@ -700,7 +700,9 @@ hipError_t launch_tiles(TileParams &p, hipStream_t stream)
     p.parts = how.parts;
     constexpr int SHARE = is_gated(EPI) ? kGatedShare : kShare;
     if (p.parts == 1) return how.large ? launch_shape<Tile256, AT, BROWS, EPI>(p, stream) : launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
-    const hipError_t e = how.large ? launch_shape<Tile256, AT, BROWS, SHARE>(p, stream) : launch_shape<Tile128, AT, BROWS, SHARE>(p, stream);
+    hipError_t e;
+    if constexpr (is_gated(EPI)) e = launch_shape<Tile128, AT, BROWS, SHARE>(p, stream);           // (their shares are never large tiles)
+    else e = how.large ? launch_shape<Tile256, AT, BROWS, SHARE>(p, stream) : launch_shape<Tile128, AT, BROWS, SHARE>(p, stream);
     if (e != hipSuccess) return e;
     const int64_t threads = (int64_t)p.M * (p.N / 4);          // (few tiles: far below 2^31)
     hipLaunchKernelGGL((join_kernel<EPI>), dim3((unsigned)((threads + 255) / 256), p.problems), dim3(256), 0, stream, p);

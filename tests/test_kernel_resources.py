@@ -84,3 +84,9 @@ def test_nothing_spills_but_in_the_epilogue_of_the_four_wave_tiles(all_kernels, 
     assert all(n <= 10 for n in (spilled.pop(t) for t in four_waves)) and not any(spilled.values()), spilled
     others = {name: k for name, k in all_kernels.items() if "atb_gemm_kernel" not in name}
     assert others and not any(k["vgpr_spill_count"] for k in others.values())
+
+
+def test_no_gated_shares_of_large_tiles(all_kernels):
+    """The gated product's shares are small tiles alone (kGatedShare, the epilogue 5): of large ones there is no kernel that nothing would reach."""
+    shares = [name for name in all_kernels if "tile_kernel" in name and "ELi5EEE" in name]
+    assert len(shares) == 1 and "ILi128ELi128E" in shares[0], shares
