@@ -16,3 +16,16 @@ def test_rows_of_more_than_one_launch(dtype):
     want, got = reference(x, dy, w, b, 1e-5), run(x, dy, w, b, 1e-5)
     for name in ("y", "mean", "rstd", "dx"):
         close(got[name], want[name], name)
+
+
+@pytest.mark.parametrize("D", [2 ** 17 + 3, 2 ** 24])
+def test_sums_along_long_rows(D, monkeypatch):
+    """Rows of two values and the gradient of a mean, all of one value: rounding errors of a sum are all of one sign.  A row's sum is taken in chains of at most 128 additions, of their sums at most D / 2^17 more
+    and a tree of 10: each errs by at most 2^-24 of the sum of the terms' sizes."""
+    monkeypatch.setattr("test_gpu_norm.E", (128 + D / 2 ** 17 + 12) * 2.0 ** -24)
+    x, dy = torch.full((2, D), 0.1, device="cuda"), torch.full((2, D), 0.1, device="cuda")
+    x[:, 1::2] = 0.101
+    x[1, ::4] = -0.2
+    want, got = reference(x, dy, None, None, 1e-5), run(x, dy, None, None, 1e-5)
+    for name in ("y", "mean", "rstd", "dx"):
+        close(got[name], want[name], name)
