@@ -24,7 +24,29 @@ struct NormParams {
 };
 hipError_t launch_norm(const NormParams &p, hipStream_t stream);
 hipError_t launch_norm_backward(const NormParams &p, hipStream_t stream);
-int64_t norm_partials(int64_t M, int64_t D);       // partial sums of the parameters' gradients that the backward pass makes
+
+constexpr int kNormPerThread = 16;                 // elements of a row that a thread holds
+constexpr int kNormGradThreads = 512;              // workgroup of the backward pass: 256 registers per thread
+constexpr int kNormMaxGradRow = kNormGradThreads * kNormPerThread;       // of longer rows the parameters' gradients are a pass of their own
+
+// Threads per row: the power of two, 64 to 1024, that holds it.
+static inline int norm_threads(int64_t D)
+{
+    int t = 64;
+    while (t < 1024 && (int64_t)t * kNormPerThread < D) t *= 2;
+    return t;
+}
+
+// Partial sums of the parameters' gradients that the backward pass makes, one of each of its workgroups: one per CU of the 256 (of longer rows 64, times the column blocks),
+// fewer where there are not as many row groups (a workgroup takes kNormGradThreads / norm_threads(D) rows at a time), and as many times more as it takes for none to
+// add more than 512 of them one after another: every addition may err by 2^-24 of the sum, and where all err one way 4096 of them made it 6e-5.
+static inline int64_t norm_partials(int64_t M, int64_t D)
+{
+    if (M <= 0) return 0;
+    const int64_t rows = D > kNormMaxGradRow ? 1 : kNormGradThreads / norm_threads(D), most = D > kNormMaxGradRow ? 64 : 256;
+    const int64_t groups = (M + rows - 1) / rows;
+    return groups < most ? groups : most * ((groups + most * 512 - 1) / (most * 512));
+}
 
 // ---- bf16 products in tiles (atb_ffn.hip, atb_ffn_grad.hip)
 

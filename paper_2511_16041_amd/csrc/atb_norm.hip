@@ -15,10 +15,8 @@
 namespace atb {
 namespace {
 
-constexpr int kPerThread = 16;                 // elements of a row that a thread holds
+constexpr int kPerThread = kNormPerThread, kGradThreads = kNormGradThreads, kMaxGradRow = kNormMaxGradRow;
 constexpr int kMaxRow = 1024 * kPerThread;     // longer rows are read again for every sum
-constexpr int kGradThreads = 512;              // workgroup of the backward pass: 256 registers per thread
-constexpr int kMaxGradRow = kGradThreads * kPerThread;
 
 template <class T> struct Chunk;               // 16 bytes of a row
 template <> struct Chunk<__bf16> {
@@ -453,8 +451,13 @@ __global__ void __launch_bounds__(1024) norm_params_kernel(const NormParams p, i
     float s = 0.0f;
     if (col < p.D) {
         const float *at = p.partial + ((int64_t)first * 2 + which) * p.D + col;
+        for (int i = first; i < end; i += 64) {               // 64 at a time: shorter chains
+            const int stop = min(end, i + 64);
+            float part = 0.0f;
 #pragma unroll 8
-        for (int i = first; i < end; ++i, at += 2 * p.D) s += *at;
+            for (int n = i; n < stop; ++n, at += 2 * p.D) part += *at;
+            s += part;
+        }
     }
     sums[wave][lane] = s;
     __syncthreads();
@@ -463,14 +466,6 @@ __global__ void __launch_bounds__(1024) norm_params_kernel(const NormParams p, i
         for (int i = 1; i < 16; ++i) s += sums[i][lane];
         out[col] = (P)s;
     }
-}
-
-// Threads per row: the power of two, 64 to 1024, that holds it in 16 elements each.
-int threads_of(int64_t D)
-{
-    int t = 64;
-    while (t < 1024 && (int64_t)t * kPerThread < D) t *= 2;
-    return t;
 }
 
 // Rows of a launch with a workgroup a row: of up to 1024 threads, and a launch has fewer than 2^32.
@@ -512,7 +507,7 @@ hipError_t forward(const NormParams &p, hipStream_t stream)
         hipLaunchKernelGGL((norm_long_kernel<X, P>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
         return hipGetLastError();
     }
-    switch (threads_of(p.D)) {
+    switch (norm_threads(p.D)) {
         case 64: return forward_of<X, P, 64>(p, stream);
         case 128: return forward_of<X, P, 128>(p, stream);
         case 256: return forward_of<X, P, 256>(p, stream);
@@ -567,7 +562,7 @@ hipError_t backward(const NormParams &p, hipStream_t stream)
     hipError_t e = hipSuccess;
     if (p.M > 0 && (p.dx || params)) {
         if (p.D > kMaxGradRow) e = backward_long<X, P>(p, stream);
-        else switch (threads_of(p.D)) {
+        else switch (norm_threads(p.D)) {
             case 64: e = backward_short<X, P, 64>(p, stream); break;
             case 128: e = backward_short<X, P, 128>(p, stream); break;
             case 256: e = backward_short<X, P, 256>(p, stream); break;
@@ -580,15 +575,6 @@ hipError_t backward(const NormParams &p, hipStream_t stream)
 }
 
 }  // namespace
-
-// Workgroups of the backward pass: one per CU of the 256, fewer where there are not as many rows (a workgroup takes kGradThreads / T at a time).
-int64_t norm_partials(int64_t M, int64_t D)
-{
-    if (M <= 0) return 0;
-    if (D > kMaxGradRow) return M < 64 ? M : 64;
-    const int64_t rows = kGradThreads / threads_of(D), n = (M + rows - 1) / rows;
-    return n < 256 ? n : 256;
-}
 
 hipError_t launch_norm(const NormParams &p, hipStream_t stream)
 {

@@ -29,3 +29,26 @@ def test_sums_along_long_rows(D, monkeypatch):
     want, got = reference(x, dy, None, None, 1e-5), run(x, dy, None, None, 1e-5)
     for name in ("y", "mean", "rstd", "dx"):
         close(got[name], want[name], name)
+
+
+@pytest.mark.parametrize("M,D", [(2 ** 20 + 3, 8), (2 ** 23, 8), (2 ** 18 + 1, 1030)])
+def test_sums_over_many_rows(M, D):
+    """The gradients of the parameters where every row adds the same, so that rounding errors have one sign.  A workgroup adds at most 512 rows one after another, then halves of its
+    row groups; the partial sums, M / 4096 at most of these rows, are added 64 at a time in 16 runs: each addition errs by at most 2^-24 of the sum of the terms' sizes."""
+    value, xh = 0.5079958438873291, 0.75                                 # 4096 of them added in fp32: 6e-5 off
+    x, dy = torch.full((M, D), 2.0, device="cuda"), torch.full((M, D), value, device="cuda")
+    mean, rstd = torch.full((M,), 1.0, device="cuda"), torch.full((M,), xh, device="cuda")
+    _, dw, db = atb.layer_norm_backward(dy, x, mean, rstd, torch.ones(D, device="cuda"))
+    chain = 512 + 3 + 64 + M / 4096 / 16 / 64 + 1 + 16 + 1
+    for got, want in ((db, M * value), (dw, M * value * xh)):
+        assert bool(((got.double() - want).abs() <= (chain + 2) * 2.0 ** -24 * want).all()), float((got.double() / want - 1).abs().max())
+
+
+def test_sums_over_many_long_rows():
+    """The same in rows of more than 8192 elements, whose gradients of the parameters are a pass of their own."""
+    M, D, value = 2 ** 17 + 1, 8200, 0.5079958438873291
+    x, dy = torch.full((M, D), 2.0, device="cuda"), torch.full((M, D), value, device="cuda")
+    mean, rstd = torch.ones((M,), device="cuda"), torch.ones((M,), device="cuda")
+    _, dw, db = atb.layer_norm_backward(dy, x, mean, rstd, torch.ones(D, device="cuda"))
+    for got in (dw, db):
+        assert bool(((got.double() - M * value).abs() <= (512 + 64 + 1 + 16 + 3) * 2.0 ** -24 * M * value).all()), float((got.double() / (M * value) - 1).abs().max())
