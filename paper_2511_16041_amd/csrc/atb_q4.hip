@@ -27,7 +27,8 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const X *__restrict__ 
         hi = fmaxf(hi, __shfl_xor(hi, d));
         lo = fminf(lo, __shfl_xor(lo, d));
     }
-    const float step = ZEROS ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f;
+    const float range = hi - lo;                             // may pass fp32's range: then by halves
+    const float step = !ZEROS ? fmaxf(hi, -lo) / 7.0f : range <= 3.402823466e38f ? range / 15.0f : (0.5f * hi - 0.5f * lo) / 7.5f;
     union { __bf16 b; uint16_t w; } s;
     s.b = (__bf16)step;
     const float scale = (float)s.b;

@@ -168,3 +168,16 @@ def test_rows_of_more_than_one_launch():
     """65535 blocks of 16 rows a launch: every row, on both sides of that."""
     w, x = random_weight(24, 64, 32, True, 13), rows(65535 * 16 + 5, 64, 14, pad=8)
     check(atb.q4_matvec(x, w, torch.float32), x, w)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_quantise_the_largest_numbers(zeros):
+    """Finite weights whose range, the largest less the smallest, passes fp32's: scale and codes are still the formula's, taken in 64 bits."""
+    w = torch.tensor([[3.0e38, -2.6e38] * 16, [1.0e38, -3.3e38] * 16, [3.2e38, -0.0] * 16], device="cuda")
+    got = atb.q4_quantize(w, 32, zeros)
+    hi, lo = w.double().amax(1, keepdim=True).clamp(min=0), w.double().amin(1, keepdim=True).clamp(max=0)
+    s = ((hi - lo) / 15 if zeros else torch.maximum(hi, -lo) / 7).bfloat16()
+    z = torch.round(-lo / s.double()).clamp(0, 15) if zeros else torch.full_like(hi, 8)
+    assert torch.equal(got.scales, s)
+    assert torch.equal(codes(got.packed).double(), (torch.round(w.double() / s.double()) + z).clamp(0, 15))
+    assert got.zeros is None or torch.equal(got.zeros.double(), z)
