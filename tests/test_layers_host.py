@@ -214,3 +214,24 @@ def test_workspace_of_a_gated_block():
     for bad in ((-1, 64, 64), (1, 60, 64), (1, 64, 0), (2 ** 23 + 1, 64, 64), (1, 2 ** 22, 64)):
         assert L.atb_ffn_workspace(*bad, 1) == 0 and L.atb_ffn_backward_workspace(*bad) == 0
     assert L.atb_ffn_backward_workspace(0, 64, 64) == 0
+
+
+@pytest.mark.parametrize("mistake", ["g and u in bf16", "dh in bf16"])
+def test_the_bound_on_the_blocks_error_sees_one_more_rounding(mistake):
+    """The bound of test_gpu_ffn_error.py, with the mistake made in the oracle: every gradient that it touches is outside."""
+    import torch
+    from test_gpu_ffn import activation
+    from test_gpu_ffn_error import MARGIN, block, rounded
+    gen = torch.Generator().manual_seed(3)
+    x, wg, wu, wd, dy = ((s * torch.randn(shape, generator=gen)).bfloat16().double() for s, shape in ((1, (200, 264)), (0.05, (520, 264)), (0.05, (520, 264)), (0.05, (264, 520)), (0.1, (200, 264))))
+    exact, model = block(x, wg, wu, wd, dy, "silu", lambda t: t), block(x, wg, wu, wd, dy, "silu", rounded)
+    g, u, dh = x @ wg.t(), x @ wu.t(), dy @ wd
+    if mistake == "dh in bf16":
+        dh = rounded(dh)
+    else:
+        g, u = rounded(g), rounded(u)
+    a, slope = activation("silu", g)
+    dg, du = rounded(dh * u * slope), rounded(dh * a)
+    for name, y in (("dx", dg @ wg + du @ wu), ("dwg", dg.t() @ x), ("dwu", du.t() @ x)):
+        off, allowed = (float((t - exact[name]).norm() / exact[name].norm()) for t in (rounded(y), model[name]))
+        assert off > 1.1 * MARGIN * allowed, name
