@@ -65,3 +65,18 @@ def test_launch_without_a_device_returns_hip_error():
     env = dict(os.environ, HIP_VISIBLE_DEVICES="", ROCR_VISIBLE_DEVICES="", CUDA_VISIBLE_DEVICES="")
     r = subprocess.run([sys.executable, "-c", code], env=env, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "no-device ok" in r.stdout, r.stdout + r.stderr
+
+
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir(ROCM_INC), reason="needs g++ and the HIP headers")
+def test_the_feed_forward_operators_host_code_is_clean_under_asan_and_ubsan(tmp_path):
+    """atb_layers_api.cpp and the rules of atb_layers.h, which decide the sizes of buffers that kernels write."""
+    exe = str(tmp_path / "sanitize_layers")
+    san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-static-libasan", "-static-libubsan", "-fno-omit-frame-pointer", "-g", "-O1"]
+    subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INC, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wno-deprecated-declarations",
+                    os.path.join(NATIVE, "sanitize_layers.cpp"), os.path.join(NATIVE, "stub_device.cpp"), os.path.join(CSRC, "atb_api.cpp"), os.path.join(CSRC, "atb_model.cpp"),
+                    os.path.join(CSRC, "atb_layers_api.cpp"), "-o", exe, "-lm"] + san, check=True)
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([exe], env=env, capture_output=True, text=True, timeout=120)
+    out = r.stdout + r.stderr
+    assert r.returncode == 0 and "sanitize_layers: ok" in r.stdout, out
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out
