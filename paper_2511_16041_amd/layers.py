@@ -2,7 +2,8 @@
 block in bf16 and its gradients, and the gated block's products with 4-bit weights for few tokens.
 
 Results and workspaces are made on the device of the first tensor; a call is launched asynchronously on `stream`, by default that device's current one, and
-memory that it makes belongs to that stream.  Tensors that are not what a kernel takes (type, shape, device, rows whose elements
+memory that it makes belongs to that stream.  The operators are not part of torch's autograd: results never require gradients, whatever the operands do, and a graph ends at
+them; a backward pass is the call of that name, with what the forward call returns for it, and the 4-bit products have none.  Tensors that are not what a kernel takes (type, shape, device, rows whose elements
 do not lie next to each other) raise AssertionError, sizes that no kernel takes AtbError.  A matrix's rows may lie further apart than they are long."""
 from __future__ import annotations
 
@@ -36,7 +37,8 @@ def _activation(name: str) -> int:
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stats: bool = False, stream=None):
     """(x - mean) / sqrt(variance + eps) * weight + bias over the rows of x (M x D, bf16 or fp32), in x's type.  weight, bias: D elements in bf16 or
-    fp32, both of one type, or None.  stats: returns (y, mean, rstd), the statistics in fp32, which the backward pass takes."""
+    fp32, both of one type, or None.  stats: returns (y, mean, rstd), the statistics in fp32, which the backward pass, layer_norm_backward, takes (autograd does not follow
+    this call)."""
     return _call("layer_norm", "atb_layer_norm", stream, _address("atb_layer_norm"), x, weight, bias, eps, stats)
 
 
@@ -58,14 +60,16 @@ class FeedForwardState(NamedTuple):
 
 def feed_forward(x, w_gate, w_up, w_down, act: str = "silu", save: bool = False, stream=None):
     """(act(x w_gate^T) * (x w_up^T)) w_down^T in bf16: x M x D, w_gate and w_up F x D, w_down D x F (as a linear layer's weight is kept), D and F
-    multiples of 8.  act: "silu", "gelu" or "gelu_tanh".  save: returns (y, FeedForwardState)."""
+    multiples of 8; rows 16-byte aligned and a multiple of 8 elements apart.  act: "silu", "gelu" or "gelu_tanh".  The inner activations are rounded to bf16.  save: returns
+    (y, FeedForwardState), which feed_forward_backward takes (autograd does not follow this call)."""
     out = _call("ffn_forward", "atb_ffn_forward", stream, _address("atb_ffn_forward"), _address("atb_ffn_kept_bytes"), _address("atb_ffn_workspace"), x, w_gate, w_up, w_down,
                 _activation(act), save)
     return (out[0], FeedForwardState(*out[1:], act)) if save else out
 
 
 def feed_forward_backward(dy, x, w_gate, w_up, w_down, state: FeedForwardState, stream=None):
-    """(dx, dw_gate, dw_up, dw_down) of feed_forward, in bf16."""
+    """(dx, dw_gate, dw_up, dw_down) of feed_forward, in bf16, all four; inside, the gradients of both first products are rounded to bf16.  (The C entry point takes NULL for those that are not
+    asked for.)"""
     return _call("ffn_backward", "atb_ffn_backward", stream, _address("atb_ffn_backward"), _address("atb_ffn_kept_bytes"), _address("atb_ffn_backward_workspace"), dy, x, w_gate, w_up, w_down,
                  state.h, state.kept, _activation(state.act))
 
@@ -95,7 +99,7 @@ def q4_matvec(x, weight: Tuple, dtype=None, stream=None):
 
 
 def q4_feed_forward(x, w_gate: Tuple, w_up: Tuple, w_down: Tuple, act: str = "silu", stream=None):
-    """feed_forward of few tokens with all three weights in 4 bits; the inner activations are rounded to bf16."""
+    """feed_forward of few tokens with all three weights in 4 bits; the inner activations are rounded to bf16.  Any number of tokens is right, but every 16 read the weights again."""
     return _call("q4_ffn", "atb_q4_gated", stream, _address("atb_q4_gated"), _address("atb_q4_matvec"), x, *Q4Weight(*w_gate), *Q4Weight(*w_up),
                  *Q4Weight(*w_down), _activation(act))
 

@@ -247,3 +247,15 @@ def test_without_a_workspace_where_it_would_hold_shares_of_large_tiles():
     assert atb.lib().atb_ffn_backward(ctypes.byref(f), h.data_ptr(), kept.data_ptr(), dy.data_ptr(), D, dg.data_ptr(), du.data_ptr(), out["dx"].data_ptr(), D,
                                       out["dwg"].data_ptr(), out["dwu"].data_ptr(), out["dwd"].data_ptr(), stream) == 0
     close({"y": y, **out}, want)
+
+
+def test_the_operators_are_not_part_of_autograd():
+    """Operands that require gradients give the same results, which require none: the backward passes are calls of their own."""
+    x, wg, wu, wd, _ = make(40, 72, 136, 13)
+    n = atb.layer_norm(x, wg[0].contiguous())
+    y = atb.feed_forward(n, wg, wu, wd)
+    asked = [t.clone().requires_grad_() for t in (x, wg, wu, wd)]
+    again = atb.layer_norm(asked[0], asked[1][0].contiguous())
+    assert torch.equal(again, n) and not again.requires_grad
+    z = atb.feed_forward(n, *asked[1:])
+    assert torch.equal(y, z) and not z.requires_grad
