@@ -6,9 +6,10 @@
 // workgroup walks rows a grid apart and keeps its share of both sums in registers, 16 columns per thread; a second kernel adds the
 // workgroups' sums in order.  No atomics: the same bits every time.
 // Rows begin anywhere: 16-byte requests at any element, and the elements of the last, incomplete chunk one by one.
-// Measured (a copy reaches 4.9 TB/s here; inputs of this size come partly out of the Infinity Cache): 8192 x 4096 in bf16 forward 29.1 us, 4.6 TB/s, backward
-// 34.0 us, 5.9 TB/s, and the sums of dw and db 4.7 us; 3000 x 5001 in fp32 forward 26.6 us, 4.5 TB/s, backward 44.8 us; 1 x 4096 in bf16 3.3 us; 4096 x 8200 in bf16
-// 40 us and 42 + 28 + 5: half of the 1024 threads have nothing to do.
+// Measured (a copy reaches 4.9 TB/s here; inputs of this size come partly out of the memory-side cache): 8192 x 4096 in bf16 forward 29.0 us, 4.6 TB/s, backward
+// 33.9 us, 5.9 TB/s, and the sums of dw and db 4.7 us; 3000 x 5001 in fp32 forward 26.4 us, 4.5 TB/s, backward 44.1 us; 1 x 4096 in bf16 3.1 us.  In bf16, forward and
+// dx + the share of dw and db + their sum: 4096 x 8200 41 us and 57 + 28 + 5 (half of the 1024 threads have nothing to do, and x and dy are read twice), 2048 x 16384 31 and
+// 44 + 27 + 5, 2048 x 16400 90 and 111 + 29 + 5 (a lane takes single elements).
 #include "atb_device.h"
 #include "atb_layers.h"
 
@@ -536,7 +537,7 @@ hipError_t backward_short(const NormParams &p, hipStream_t stream)
 }
 
 // Rows of more than kMaxGradRow elements: with both sums beside the row a thread would need more registers than it has (16 elements in each of
-// 1024 threads: 38 spilled), so dw and db are a pass of their own over x and dy.
+// 1024 threads: 38 spilled), so dw and db are a pass of their own over x and dy.  (Both sums in LDS, up to 128 KiB of it, have not been tried.)
 template <class X, class P>
 hipError_t backward_long(const NormParams &p, hipStream_t stream)
 {

@@ -1,4 +1,5 @@
-// 4-bit weights with group scales: quantiser and decoder.  Bound: HBM.
+// 4-bit weights with group scales: quantiser and decoder.  Bound: decoding HBM, 8192 x 8192 to bf16 30 us, 5.8 TB/s (what it has just written is in part in a cache); quantising the VALU, 8192
+// x 8192 in bf16 to groups of 32 with zero points 110 to 125 us, 1.4 TB/s: its instructions, 64-bit divisions for a thread's place among them, take 83 % of the cycles.
 // w = s (q - z), q and z in 0 .. 15; a group is G neighbouring k of one row with a scale in bf16 and, if kept, a zero point.
 #include "atb_device.h"
 #include "atb_layers.h"

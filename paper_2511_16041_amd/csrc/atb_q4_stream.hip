@@ -1,16 +1,19 @@
 // Products of few rows with 4-bit weights and group scales, alone or gated: act(x Wg^T) o (x Wu^T).
-// Bound: the bytes of the weights; a small one is its launch.
+// Floor: the bytes of the weights; a small one is its launch.
 //
 // A workgroup has 16 columns of y times a few and 16 rows, as in atb_stream.hip: W waves take the panels of K in turn, and their sums are added in
 // wave order.  A panel is 256 k, one 128-byte line of every row of W.  A lane asks for 16 bytes of its row, 32 codes; the dwords of four lanes are exchanged (a 4 x 4
-// transposition in four lane swaps), so that one MFMA's 32 k lie in one group of 32.  Two panels of a wave are on their way, x comes from a cache when it is
-// needed: with it in registers as well there is room for half as many waves.  Scales and zero points are asked for by 16 lanes, one a column, and handed to the others.
+// transposition in four lane swaps), so that one MFMA's 32 k lie in one group of 32.  The next panel is asked for ahead of the multiplication, and x, out of a cache, in
+// it: with x of a panel in registers as well there is room for half as many waves.  Requests come back in order, so the first MFMA of a panel waits for x and
+// with it for the next panel, and that is what bounds these kernels rather than decoding: of the cycles VALU instructions take 40 % (16 rows, 8192 -> 8192) to 44 % (the gated
+// product below) and MFMAs 7 to 10 %, the rest is waiting.  Scales and zero points are asked for by 16 lanes, one a column, and handed to the others.
 //
 // w = s (q - z).  A code becomes bf16 without a conversion: 0x4180 | q << 3 is the number 16 + q.  The MFMAs of a group sum (16 + q) x; one more,
 // shared by all columns, sums x; then y += s (sum - (16 + z) sum of x), all in fp32.  (With 0x4300 | q, 128 + q, the sum that is subtracted again is
 // 30 times the result's size and not 5, and the error against 64 bits 1.8e-6.)
-// Measured: one row, 4096 -> 4096 in groups of 128 5.0 us; gated 4096 -> 14336 in groups of 64 with zero points 22.2 us, 2.9 TB/s, and back 12.8; 16 rows,
-// 8192 -> 8192 in groups of 32 with zero points 17.5 us, 2.3 TB/s: from there on decoding is what counts.
+// Measured: one row, 4096 -> 4096 in groups of 128 5.0 us; gated 4096 -> 14336 in groups of 64 with zero points 21.9 us, 3.0 TB/s, and back 13.1; 16 rows,
+// 8192 -> 8192 in groups of 32 with zero points 17.6 us, 2.3 TB/s.  Every block of 16 rows is a workgroup that asks for the weights and decodes them again: 32 rows 34.6 us,
+// 64 66.4; 64 rows 4096 -> 4096 23.6, 16 7.1.
 #include "atb_stream.h"
 
 namespace atb {
@@ -265,7 +268,8 @@ hipError_t launch_shape(const StreamParams &p, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Waves and columns of a workgroup: enough workgroups for every CU, then as many columns to a request of x as there are, then 16 waves where a CU has but one workgroup.
+// Waves and columns of a workgroup: 16 columns as long as these are one workgroup per CU at most (N = 4096), 32 beyond; 16 waves where there is at most one workgroup per CU.  (So
+// from N = 4097, 129 workgroups, to 8191 a part of the CUs has none; 16 columns in more workgroups have not been measured there.)
 // us, 16 columns in 8 / 16 waves, 32 columns in 8 / 16 waves: one row 14336 -> 4096 in groups of 64 16.3 / 13.1, 23.3 / 18.8; 8192 -> 8192 in groups of 128 14.7 / 15.0, 13.4 / 12.8,
 // of 32 with 16 rows 25.2 / 25.2, 17.8 / 17.2; 4096 -> 14336 in groups of 64 - / 16.3, 12.6 / 13.6; gated 4096 -> 14336 in 4 / 8 / 16 waves 22.9 / 21.9 / 25.5.
 template <int G, bool ZEROS>

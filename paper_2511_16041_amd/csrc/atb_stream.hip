@@ -8,7 +8,8 @@
 // A wave's panels come straight from memory into two LDS buffers of its own (no barriers: it waits for its own requests), the next one on its way
 // while one is multiplied.  A lane of an MFMA needs 16 bytes of one row, its neighbour of the next row; asked for like that, every lane is an
 // access of the L1 (63 a request, 86 000 a CU for the block of 16 tokens of 4096, 14336: 36 of its 48 us).  Into LDS eight neighbouring lanes ask for one line.
-// Measured, 16 rows: gated 4096 -> 14336 46.7 us, 5.0 TB/s; plain 14336 -> 4096 26.7 us, 4.4 TB/s.
+// Measured, 16 rows, 15 passes over three sets of weights: gated 4096 -> 14336 46.4 us, 5.1 TB/s; plain 14336 -> 4096 26.8 us, 4.4 TB/s.  Among many passes 41.7 and 24.8; one row 39.9
+// and 23.6.
 #include "atb_stream.h"
 
 namespace atb {
@@ -173,7 +174,7 @@ hipError_t launch_rows(const StreamParams &p, hipStream_t stream)
 
 }  // namespace
 
-// Waves and columns of a workgroup, us for 16 rows: gated 4096 -> 14336 in 4 / 8 / 16 waves of 16 + 16 columns 41.7 / 44.1 / 52.5, 14336 -> 4096 in 8 waves of 16 columns
+// Waves and columns of a workgroup, us for 16 rows among many passes: gated 4096 -> 14336 in 4 / 8 / 16 waves of 16 + 16 columns 41.7 / 44.1 / 52.5, 14336 -> 4096 in 8 waves of 16 columns
 // 24.8 and of 32 (half as many workgroups as CUs) 32.2.
 hipError_t launch_stream(const StreamParams &p, hipStream_t stream)
 {

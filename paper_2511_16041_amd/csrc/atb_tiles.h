@@ -12,9 +12,13 @@
 // so no MFMA behind the barrier waits for LDS, and A's tile s + 2 is still on its way at the barrier.
 // Where there are fewer tiles than CUs a workgroup takes a share of the reduction (choose_tiles).
 //
-// Bound: the path by which requests come into a CU (43 to 60 GB/s each; without requests a K-step takes 59 % of its time, without MFMAs 94 %), then power.
-// Measured, M = 8192, D = 4096, F = 14336: gated 1636 us, 1176 TFLOP/s; down 731, 1316; dh with its epilogue 964, 998; dx 1450, 1327; the gradients of
-// the gate and up weights 1500, 1282, of the down weight 884, 1088 (3.5 rounds of tiles).
+// Bound: the path by which requests come into a CU (64 KiB a K-step, 30 to 40 GB/s each in the products below; without requests a K-step takes 59 % of its time, without MFMAs
+// 94 %), then power.
+// Measured, M = 8192, D = 4096, F = 14336: gated 1624 us, 1185 TFLOP/s; down 739, 1302; dh with its epilogue 975, 986; dx 1476, 1304; the gradients of
+// the gate and up weights 1540, 1249, of the down weight 898, 1072 (3.5 rounds of tiles).  (From box to box 2 %.)
+//
+// Rounded to bf16 are, beside the results, the operands of the products that follow: h, dg and du.  Their MFMAs take no other type at this rate; with three terms
+// in the place of one an operand in two halves would keep 16 bits.  y and the gradients are 2.4e-3 off in the 2-norm, 1.7e-3 of it the results' rounding.
 #pragma once
 
 #include "atb_activation.h"
