@@ -296,7 +296,7 @@ atb_status atb_q4_quantize(const void *W, int64_t ldw, atb_type type, void *pack
 /* The values that a 4-bit weight stands for: out, DEVICE, N x K of out_type (in fp32 exact, in bf16 rounded to nearest even). */
 atb_status atb_q4_decode(const atb_q4 *w, void *out, atb_type out_type, void *hip_stream);
 
-/* y = x W^T for few rows: x DEVICE, M x K bf16 (pitch ldx, a multiple of 8; 16-byte aligned), y M x N of y_type (pitch ldy).  Any M up to 2^23
+/* y = x W^T for few rows: x DEVICE, M x K bf16 (pitch ldx, a multiple of 8, at most 2^26; 16-byte aligned), y M x N of y_type (pitch ldy).  Any M up to 2^23
  * is right; weights are read once per 16 rows.  A row with an infinity in x, or whose sums pass fp32's range, is not finite, NaN also where the formula
  * has an infinity: (16 + q) x is summed and (16 + z) x taken off again.  Async on hip_stream. */
 atb_status atb_q4_matvec(const atb_q4 *w, const void *x, int64_t ldx, void *y, int64_t ldy, atb_type y_type, int64_t M, void *hip_stream);

@@ -3,7 +3,7 @@
 
 namespace {
 
-constexpr int64_t kMaxRows = (int64_t)1 << 23, kMaxPitch = (int64_t)1 << 22, kMaxNorm = (int64_t)1 << 24;
+constexpr int64_t kMaxRows = (int64_t)1 << 23, kMaxPitch = (int64_t)1 << 22, kMaxRowsApart = (int64_t)1 << 26, kMaxNorm = (int64_t)1 << 24;
 
 using atb::hip_status;
 
@@ -253,7 +253,8 @@ namespace {
 
 bool q4_operands(const atb_q4 *w, const void *x, int64_t ldx, const void *y, int64_t ldy, atb_type y_type, int64_t M)
 {
-    return is_matrix(x, w->K, ldx) && y && aligned(y, size_of(y_type)) && ldy >= w->N && M <= kMaxRows;
+    // 16 rows of x are within 2^31 bytes
+    return x && aligned(x, 16) && ldx >= w->K && ldx % 8 == 0 && ldx <= kMaxRowsApart && y && aligned(y, size_of(y_type)) && ldy >= w->N && M <= kMaxRows;
 }
 
 atb::StreamParams q4_params(const atb_q4 *w, const void *x, int64_t ldx, void *y, int64_t ldy, atb_type y_type, int64_t M)

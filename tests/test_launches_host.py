@@ -106,3 +106,10 @@ def test_without_a_workspace_large_tiles_are_nearly_as_many_as_cus(launches, M, 
         assert all(one["parts"] == 1 for one in found)
         for one in found:
             assert one["block"][0] == 256 or one["grid"][0] * one["grid"][1] >= 192, one
+
+
+@pytest.mark.parametrize("K,ldx", [(2 ** 22, 2 ** 22), (2 ** 22, 2 ** 26), (128, 2 ** 26), (128, 2 ** 22 + 8)])
+def test_4_bit_weights_of_the_longest_rows(launches, K, ldx):
+    """K up to 2^22 is documented, and with it rows of x at least that far apart."""
+    consecutive(launches("q4", 40, 24, K, 128, 0, ldx, 24), 40, {"x": 2 * ldx, "y": 48})
+    consecutive(launches("q4_gated", 40, 24, K, 128, ldx, 24), 40, {"x": 2 * ldx, "y": 48})
