@@ -265,15 +265,15 @@ size_t atb_ffn_backward_workspace(int64_t M, int64_t D, int64_t F);
 size_t atb_ffn_kept_bytes(int64_t M, int64_t F);
 
 /* h: DEVICE, M x F bf16 (pitch F), the block's inner activations: workspace, and what the backward pass takes.  kept: DEVICE,
- * atb_ffn_kept_bytes(M, F) bytes, 16-byte aligned, or NULL: nothing is kept.  y: DEVICE, bf16, pitch ldy (a multiple of 8).
+ * atb_ffn_kept_bytes(M, F) bytes, 16-byte aligned, or NULL: nothing is kept.  y: DEVICE, bf16, 16-byte aligned, pitch ldy (as ldx).
  * Async on hip_stream. */
 atb_status atb_ffn_forward(const atb_ffn *f, void *h, void *kept, void *y, int64_t ldy, void *hip_stream);
 
-/* Gradients of a loss with dy (M x D bf16, pitch lddy): with g = x Wg^T, u = x Wu^T, dh = dy Wd,
+/* Gradients of a loss with dy (M x D bf16, pitch lddy, as ldx): with g = x Wg^T, u = x Wu^T, dh = dy Wd,
  *     dg = dh o u o act'(g),  du = dh o act(g),
  *     dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h.
  * h, kept: of the forward pass.  dgate, dup: DEVICE, M x F bf16 (pitch F), workspace: dg and du (rounded to bf16; dh is not).  dx: M x D,
- * pitch lddx; dw_gate, dw_up: F x D, dw_down: D x F, contiguous, bf16; each of the four may be NULL: not asked for (dw_gate and
+ * pitch lddx (as ldx); dw_gate, dw_up: F x D, dw_down: D x F, contiguous, bf16; each of the four may be NULL: not asked for (dw_gate and
  * dw_up together).  All 16-byte aligned. */
 atb_status atb_ffn_backward(const atb_ffn *f, const void *h, const void *kept, const void *dy, int64_t lddy, void *dgate, void *dup,
                             void *dx, int64_t lddx, void *dw_gate, void *dw_up, void *dw_down, void *hip_stream);
