@@ -219,7 +219,8 @@ typedef enum atb_type { ATB_TYPE_BF16 = 0, ATB_TYPE_F32 = 1 } atb_type;
 typedef enum atb_activation {
     ATB_ACT_SILU = 0,      /* g / (1 + exp(-g)) */
     ATB_ACT_GELU = 1,      /* g (1 + erf(g / sqrt 2)) / 2, beside fp32's rounding to 2.2e-7; of its own size 1.6e-3 at g = -5, 1e-2 at -8 */
-    ATB_ACT_GELU_TANH = 2  /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+    ATB_ACT_GELU_TANH = 2, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+    ATB_ACT_NONE = 3       /* atb_linear only: g itself */
 } atb_activation;
 
 /* Layer norm of the M rows of x (D elements of `type`, DEVICE):
@@ -304,6 +305,38 @@ atb_status atb_q4_matvec(const atb_q4 *w, const void *x, int64_t ldx, void *y, i
 /* h = act(x Wg^T) o (x Wu^T) in one launch, h M x N bf16: Wg and Wu with the same N, K, group, both with or both without zero points. */
 atb_status atb_q4_gated(const atb_q4 *w_gate, const atb_q4 *w_up, atb_activation act, const void *x, int64_t ldx, void *h, int64_t ldh,
                         int64_t M, void *hip_stream);
+
+/* ------------------------- what a block has around its feed-forward sublayer
+ *
+ * A product with its epilogue and its gradients.  As above: row-major matrices with pitches in elements, sums and statistics in fp32,
+ * no atomics (the same inputs give the same bits), workspaces that the caller owns for the call, M == 0 a valid call, non-finite inputs as the formulas
+ * give them and never outside the rows and columns that depend on them. */
+
+/* y = act(x W^T + bias) + residual in bf16: x M x K, W N x K (the layout in which frameworks keep the weight of a linear layer). */
+typedef struct atb_linear {
+    const void *x, *w;                          /* DEVICE, bf16, 16-byte aligned */
+    int64_t ldx, ldw;                           /* multiples of 8, below 2^22 */
+    const void *bias;                           /* DEVICE, N elements of bias_type, or NULL */
+    int64_t M, N, K;                            /* 0 <= M <= 2^23; N any, 1 .. 2^22 - 8; K a multiple of 8, 8 .. 2^22 - 8 */
+    atb_activation act;                         /* ATB_ACT_NONE too */
+    atb_type bias_type;
+    void *workspace;                            /* DEVICE, 16-byte aligned, of the bytes below for the call; forward also NULL: long reductions of few rows are not shared out */
+} atb_linear;
+
+/* Bytes of the workspace of a forward pass (keeps != 0: one with `slope`) and of a backward pass; 0: none is used, or invalid arguments.  Of a backward pass they
+ * hold act'(z) o dy in bf16 (unless act is ATB_ACT_NONE and N a multiple of 8) and sums of it, or of products, in fp32. */
+size_t atb_linear_workspace(int64_t M, int64_t N, int64_t K, int keeps);
+size_t atb_linear_backward_workspace(int64_t M, int64_t N, int64_t K, atb_activation act);
+
+/* residual: DEVICE, M x N bf16 (pitch ldr), or NULL; may be y.  slope: DEVICE, M x N fp16 (pitch N), written with act'(x W^T + bias) for the backward pass, or NULL; with
+ * ATB_ACT_NONE there is none.  y: DEVICE, M x N bf16 (pitch ldy).  All three at any element.  Async on hip_stream. */
+atb_status atb_linear_forward(const atb_linear *l, const void *residual, int64_t ldr, void *slope, void *y, int64_t ldy, void *hip_stream);
+
+/* Gradients of a loss with dy (M x N bf16, pitch lddy): with dz = dy o act'(z), rounded to bf16 for the products,
+ *     dx = dz W,  dW = dz^T x,  dbias = sum over rows of dz (not rounded);  the residual's gradient is dy itself.
+ * slope: of the forward pass; NULL with ATB_ACT_NONE.  dy: at any element, but with ATB_ACT_NONE and N a multiple of 8 16-byte aligned with a pitch as ldx.  dx: M x K (pitch
+ * lddx, as ldx), dw: N x K contiguous, both bf16 and 16-byte aligned; dbias: N elements of bias_type; each may be NULL: not asked for.  The values of l->bias are not read. */
+atb_status atb_linear_backward(const atb_linear *l, const void *slope, const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dw, void *dbias, void *hip_stream);
 
 /* ------------------------------------------------- model and tile selector */
 

@@ -6,7 +6,8 @@ shared library is missing or a call fails, an exception is raised.
 The calls that launch a GEMM or the quantiser go through a small extension
 module (csrc/atb_binding.cpp), everything else through ctypes.
 The operators of a transformer's feed-forward sublayer (layer norm, the gated
-block, products with 4-bit weights) are in layers.py and reached from here.
+block, products with 4-bit weights) are in layers.py, those of a block around it
+(a product with its epilogue) in block.py; all are reached from here.
 """
 from __future__ import annotations
 
@@ -88,6 +89,12 @@ class Q4(ctypes.Structure):
                 ("group", ctypes.c_int)]
 
 
+class Linear(ctypes.Structure):
+    """atb_linear: the operands of a product with its epilogue."""
+    _fields_ = [("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("bias", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("M", "N", "K")] + [("act", ctypes.c_int), ("bias_type", ctypes.c_int), ("workspace", ctypes.c_void_p)]
+
+
 # every symbol include/atb.h declares
 EXPORTS = [
     "atb_status_string", "atb_last_hip_error", "atb_gemm_create", "atb_gemm_create_fmt", "atb_gemm_run", "atb_gemm_destroy",
@@ -96,6 +103,7 @@ EXPORTS = [
     "atb_model_eval", "atb_select_tiles", "atb_model_microkernel", "atb_instance_geometry", "atb_mfma_probe",
     "atb_layer_norm", "atb_layer_norm_workspace", "atb_layer_norm_backward", "atb_ffn_workspace", "atb_ffn_backward_workspace", "atb_ffn_kept_bytes", "atb_ffn_forward", "atb_ffn_backward",
     "atb_q4_quantize", "atb_q4_decode", "atb_q4_matvec", "atb_q4_gated",
+    "atb_linear_workspace", "atb_linear_backward_workspace", "atb_linear_forward", "atb_linear_backward",
 ]
 
 
@@ -173,6 +181,11 @@ def lib() -> ctypes.CDLL:
     L.atb_q4_matvec.argtypes = [ctypes.POINTER(Q4), vp, i64, vp, i64, ci, i64, vp]
     L.atb_q4_gated.restype = ci
     L.atb_q4_gated.argtypes = [ctypes.POINTER(Q4), ctypes.POINTER(Q4), ci, vp, i64, vp, i64, i64, vp]
+    L.atb_linear_workspace.restype = L.atb_linear_backward_workspace.restype = ctypes.c_size_t
+    L.atb_linear_workspace.argtypes = L.atb_linear_backward_workspace.argtypes = [i64, i64, i64, ci]
+    L.atb_linear_forward.restype = L.atb_linear_backward.restype = ci
+    L.atb_linear_forward.argtypes = [ctypes.POINTER(Linear), vp, i64, vp, vp, i64, vp]
+    L.atb_linear_backward.argtypes = [ctypes.POINTER(Linear), vp, vp, i64, vp, i64, vp, vp, vp]
     _lib = L
     return L
 
@@ -452,3 +465,4 @@ class Gemm:
 
 from .layers import (FeedForwardState, Q4Weight, feed_forward, feed_forward_backward, layer_norm, layer_norm_backward, q4_decode,  # noqa: E402
                      q4_feed_forward, q4_matvec, q4_quantize)
+from .block import linear, linear_backward  # noqa: E402

@@ -24,10 +24,11 @@ ATB_DEV float normal_cdf(float x, float &e)
     return x < 0.0f ? tail : 1.0f - tail;
 }
 
-// act(g).  The activation is a constant of the code around it: a wave-uniform branch per element costs more than the function.
+// act(g), of ATB_ACT_NONE g itself.  The activation is a constant of the code around it: a wave-uniform branch per element costs more than the function.
 template <int act>
 ATB_DEV float activate(float g)
 {
+    if (act == ATB_ACT_NONE) return g;
     if (act == ATB_ACT_SILU) return g * sigmoid(g);
     if (act == ATB_ACT_GELU) {
         float e;
@@ -65,6 +66,13 @@ ATB_DEV void with_activation(int act, F f)
     if (act == ATB_ACT_SILU) f(Activation<ATB_ACT_SILU>());
     else if (act == ATB_ACT_GELU) f(Activation<ATB_ACT_GELU>());
     else f(Activation<ATB_ACT_GELU_TANH>());
+}
+// ... where there may be none
+template <class F>
+ATB_DEV void with_activation_or_none(int act, F f)
+{
+    if (act == ATB_ACT_NONE) f(Activation<ATB_ACT_NONE>());
+    else with_activation(act, f);
 }
 
 }  // namespace atb

@@ -471,9 +471,96 @@ PyObject *q4_decode(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------------------------ what a block has around that sublayer
+
+// x, w and bias of a product with its epilogue; false: not what the kernels take
+bool describe(atb_linear &l, const at::Tensor &x, const at::Tensor &w, const std::optional<at::Tensor> &bias, long act)
+{
+    if (!x.is_cuda() || x.dim() != 2 || w.dim() != 2) return false;
+    const at::Device on = x.device();
+    l.M = x.size(0);
+    l.N = w.size(0);
+    l.K = w.size(1);
+    if (!is_rows(x, at::kBFloat16, l.M, l.K, on) || !is_rows(w, at::kBFloat16, l.N, l.K, on)) return false;
+    if (bias && (!is_float(*bias) || !is_vector(*bias, bias->scalar_type(), l.N, on))) return false;
+    l.x = x.data_ptr(); l.ldx = pitch(x);
+    l.w = w.data_ptr(); l.ldw = pitch(w);
+    l.bias = data<void *>(bias);
+    l.bias_type = bias ? type_of(*bias) : ATB_TYPE_BF16;
+    l.act = static_cast<atb_activation>(act);
+    l.workspace = nullptr;
+    return true;
+}
+// The distance between rows that may begin at any element
+int64_t apart(const at::Tensor &t) { return t.size(0) <= 1 ? t.size(1) : t.stride(0); }
+
+// linear(entry, entry of the workspace's size, x, w, bias, act, residual, save) -> y, or (y, slope or None)
+PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "linear takes 8 arguments");
+    const auto call = reinterpret_cast<decltype(&atb_linear_forward)>(PyLong_AsVoidPtr(args[0]));
+    const auto room = reinterpret_cast<decltype(&atb_linear_workspace)>(PyLong_AsVoidPtr(args[1]));
+    const long act = PyLong_AsLong(args[5]);
+    const int save = PyObject_IsTrue(args[7]);
+    if (PyErr_Occurred() || !tensors(args + 2, 2) || !tensors_or_none(args + 4, 1) || !tensors_or_none(args + 6, 1)) return nullptr;
+    HANDLE_TH_ERRORS
+    const at::Tensor &x = THPVariable_Unpack(args[2]);
+    const auto bias = optional_tensor(args[4]), residual = optional_tensor(args[6]);
+    atb_linear l;
+    if (!describe(l, x, THPVariable_Unpack(args[3]), bias, act) || (residual && !is_rows(*residual, at::kBFloat16, l.M, l.N, x.device()))) return refuse();
+    const c10::DeviceGuard guard(x.device());
+    const at::Tensor y = make({l.M, l.N}, at::kBFloat16, x.device());
+    std::optional<at::Tensor> slope, work;
+    if (save && act != ATB_ACT_NONE) slope = make({l.M, l.N}, at::kHalf, x.device());
+    const int64_t bytes = (int64_t)room(l.M, l.N, l.K, slope.has_value());
+    if (bytes > 0) work = make({bytes}, at::kByte, x.device());
+    l.workspace = data<void *>(work);
+    int st;
+    {
+        WithoutLock unlocked;
+        st = call(&l, data<void *>(residual), residual ? apart(*residual) : 0, data<void *>(slope), y.data_ptr(), l.N, current_stream());
+    }
+    if (st != 0) return PyLong_FromLong(st);
+    return save ? tuple_of({y, slope}) : THPVariable_Wrap(y);
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_backward(entry, entry of the workspace's size, dy, x, w, bias, slope) -> (dx, dw, dbias or None)
+PyObject *linear_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "linear_backward takes 7 arguments");
+    const auto call = reinterpret_cast<decltype(&atb_linear_backward)>(PyLong_AsVoidPtr(args[0]));
+    const auto room = reinterpret_cast<decltype(&atb_linear_backward_workspace)>(PyLong_AsVoidPtr(args[1]));
+    if (PyErr_Occurred() || !tensors(args + 2, 3) || !tensors_or_none(args + 5, 2)) return nullptr;
+    HANDLE_TH_ERRORS
+    const at::Tensor &dy = THPVariable_Unpack(args[2]), &x = THPVariable_Unpack(args[3]);
+    const auto bias = optional_tensor(args[5]), slope = optional_tensor(args[6]);
+    atb_linear l;
+    // (which activation it was no longer matters)
+    if (!describe(l, x, THPVariable_Unpack(args[4]), bias, slope ? ATB_ACT_SILU : ATB_ACT_NONE)) return refuse();
+    const at::Device on = x.device();
+    if (!is_rows(dy, at::kBFloat16, l.M, l.N, on)) return refuse();
+    if (slope && (slope->device() != on || slope->scalar_type() != at::kHalf || slope->dim() != 2 || slope->size(0) != l.M || slope->size(1) != l.N || !slope->is_contiguous())) return refuse();
+    const c10::DeviceGuard guard(on);
+    const at::Tensor dx = make({l.M, l.K}, at::kBFloat16, on), dw = make({l.N, l.K}, at::kBFloat16, on);
+    std::optional<at::Tensor> db, work;
+    if (bias) db = make({l.N}, bias->scalar_type(), on);
+    const int64_t bytes = (int64_t)room(l.M, l.N, l.K, l.act);
+    if (bytes > 0) work = make({bytes}, at::kByte, on);
+    l.workspace = data<void *>(work);
+    int st;
+    {
+        WithoutLock unlocked;
+        st = call(&l, data<void *>(slope), dy.data_ptr(), !slope && l.N % 8 == 0 ? pitch(dy) : apart(dy), dx.data_ptr(), l.K, dw.data_ptr(), data<void *>(db), current_stream());
+    }
+    return st == 0 ? tuple_of({dx, dw, db}) : PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
 #define ATB_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ATB_METHOD(run), ATB_METHOD(quantize), ATB_METHOD(decode), ATB_METHOD(layer_norm), ATB_METHOD(layer_norm_backward), ATB_METHOD(ffn_forward),
-                         ATB_METHOD(ffn_backward), ATB_METHOD(q4_matvec), ATB_METHOD(q4_ffn), ATB_METHOD(q4_quantize), ATB_METHOD(q4_decode), {nullptr, nullptr, 0, nullptr}};
+                         ATB_METHOD(ffn_backward), ATB_METHOD(q4_matvec), ATB_METHOD(q4_ffn), ATB_METHOD(q4_quantize), ATB_METHOD(q4_decode),
+                         ATB_METHOD(linear), ATB_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_launch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

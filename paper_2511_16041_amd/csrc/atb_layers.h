@@ -58,9 +58,12 @@ enum Epilogue {
     kGatedGrad = 3,      // the sum is dh: writes dg = dh u act'(g) and du = dh act(g)
     kShare = 4,          // the sum of a share of the reduction, in fp32; what it is for is done where the shares are joined
     kGatedShare = 5,     // ... of both weights
+    kLinear = 6,         // C = act(sum + bias) + residual
+    kLinearKeep = 7,     // ... and writes act'(sum + bias)
 };
 constexpr bool is_gated(int epilogue) { return epilogue == kGated || epilogue == kGatedKeep || epilogue == kGatedShare; }
 constexpr bool is_share(int epilogue) { return epilogue == kShare || epilogue == kGatedShare; }
+constexpr bool is_linear(int epilogue) { return epilogue == kLinear || epilogue == kLinearKeep; }
 
 struct TileParams {
     // A: M x K, K contiguous, or (transposed) K x M, M contiguous; B: N x K, K contiguous, or (rows) K x N, N contiguous.
@@ -74,6 +77,13 @@ struct TileParams {
     int segments, problems;
     int act;                     // atb_activation
     float *shares;               // room for tile_shares() floats, or null: reductions are not shared out
+    // a product with its epilogue: N is a multiple of 8, of whose columns the first `edge` exist (0: all); C, residual and slope begin at any element
+    int edge;
+    const void *bias;            // edge elements of bias_type, or null
+    int bias_type;               // atb_type
+    const uint16_t *residual;    // M x edge, ldr apart, or null
+    int64_t ldr;
+    uint16_t *slope;             // kLinearKeep: M x edge in fp16
     // set by the launch
     int tiles_m, tiles_n, group_m;
     int steps;                   // K-steps of a segment
@@ -121,6 +131,8 @@ static inline int64_t tile_shares(int64_t M, int64_t N, int64_t K, int segments,
 }
 // The products of the forward pass (A and B with K contiguous): epilogue kStore, kGated or kGatedKeep.
 hipError_t launch_tiles_forward(TileParams p, int epilogue, hipStream_t stream);
+// A product with its epilogue (atb_linear.hip): kLinear or kLinearKeep.
+hipError_t launch_tiles_linear(TileParams p, int epilogue, hipStream_t stream);
 // dh with its epilogue, and dx = dg Wg + du Wu: B in rows.
 hipError_t launch_tiles_dx(TileParams p, int epilogue, hipStream_t stream);
 // Gradients of weights: A transposed, B in rows.
@@ -147,6 +159,12 @@ struct StreamParams {
     int group;                   // 0: bf16 weights
     int gated, act;
     int y_type;                  // atb_type
+    // bf16 weights, not gated: y = act(x W^T + bias) + residual if `linear` is set
+    int linear;
+    const void *bias;            // N elements of bias_type, or null
+    int bias_type;
+    const uint16_t *residual;    // M x N, ldr apart, or null
+    int64_t ldr;
 };
 hipError_t launch_stream(const StreamParams &p, hipStream_t stream);
 hipError_t launch_q4_stream(const StreamParams &p, hipStream_t stream);      // 4 bits; launch_stream calls it

@@ -1,0 +1,113 @@
+// A product with its epilogue, y = act(x W^T + b) + residual, and what its gradients need beside products: dz = dy o act'(z) with its column sums, the bias's gradient.
+// The product and dx = dz W, dW = dz^T x are tiles (atb_tiles.h), of few rows without a backward pass atb_stream.hip.
+//
+// For the backward pass act'(z) is kept in fp16: it lies in -0.17 .. 1.13, so 11 bits of mantissa err by at most 2^-11 of it, an eighth of the rounding of dz that follows (dz is an
+// operand of two products, whose matrix instructions take bf16), and 2 bytes are what z in bf16 would take, with eight times the error.
+// The column sums take dz before it is rounded, in fp32, in runs of rows that are added in order: the same bits every time.
+#include "atb_block.h"
+#include "atb_tiles.h"
+
+namespace atb {
+
+hipError_t launch_tiles_linear(TileParams p, int epilogue, hipStream_t stream)
+{
+    if (epilogue == kLinearKeep) return launch_tiles<false, false, kLinearKeep>(p, stream);
+    return launch_tiles<false, false, kLinear>(p, stream);
+}
+
+namespace {
+
+template <class T>
+ATB_DEV void load_eight(const T *row, int at, int N, float (&v)[8])
+{
+    typedef T vec __attribute__((ext_vector_type(8)));
+    typedef vec any __attribute__((aligned(2)));
+    if (at + 8 <= N) {
+        const vec w = *reinterpret_cast<const any *>(row + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)w[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = at + e < N ? (float)row[at + e] : 0.0f;
+    }
+}
+
+// Eight columns per thread, a run of rows per workgroup.  Bound: HBM.
+template <bool SLOPE>
+__global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradParams p, int parts)
+{
+    const int pitch = (p.N + 7) / 8 * 8, col = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= pitch) return;
+    const int64_t first = p.M * blockIdx.y / parts, end = p.M * (blockIdx.y + 1) / parts;
+    float sum[8] = {};
+#pragma unroll 4
+    for (int64_t row = first; row < end; ++row) {
+        float d[8];
+        load_eight(reinterpret_cast<const __bf16 *>(p.dy) + row * p.lddy, col, p.N, d);
+        if constexpr (SLOPE) {
+            float s[8];
+            load_eight(reinterpret_cast<const _Float16 *>(p.slope) + row * p.N, col, p.N, s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] *= s[e];
+        }
+        if (p.dz) {
+            bf16x8 w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (__bf16)d[e];
+            *reinterpret_cast<bf16x8 *>(p.dz + row * pitch + col) = w;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += d[e];
+    }
+    if (!p.partial) return;
+    float *to = p.partial + (int64_t)blockIdx.y * p.N + col;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (col + e < p.N) to[e] = sum[e];
+}
+
+// The runs' column sums added in order: 64 columns per workgroup, 16 waves with some of the runs each, 64 at a time (shorter chains).
+__global__ void __launch_bounds__(1024) linear_bias_kernel(const LinearGradParams p, int parts)
+{
+    __shared__ float sums[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane;
+    const int run = (parts + 15) / 16, first = wave * run, end = min(first + run, parts);
+    float s = 0.0f;
+    if (col < p.N) {
+        const float *at = p.partial + (int64_t)first * p.N + col;
+        for (int i = first; i < end; i += 64) {
+            const int stop = min(end, i + 64);
+            float part = 0.0f;
+#pragma unroll 8
+            for (int n = i; n < stop; ++n, at += p.N) part += *at;
+            s += part;
+        }
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && col < p.N) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += sums[i][lane];
+        if (p.bias_type == ATB_TYPE_F32) static_cast<float *>(p.dbias)[col] = s;
+        else static_cast<__bf16 *>(p.dbias)[col] = (__bf16)s;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_linear_grad(const LinearGradParams &p, hipStream_t stream)
+{
+    const int parts = (int)linear_parts(p.M, p.N);                 // at most 2^14
+    if (p.M > 0 && (p.dz || p.dbias)) {
+        const dim3 grid((unsigned)((p.N + 2047) / 2048), (unsigned)parts);
+        if (p.slope) hipLaunchKernelGGL(linear_grad_kernel<true>, grid, dim3(256), 0, stream, p, parts);
+        else hipLaunchKernelGGL(linear_grad_kernel<false>, grid, dim3(256), 0, stream, p, parts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!p.dbias) return hipSuccess;
+    hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)((p.N + 63) / 64)), dim3(1024), 0, stream, p, parts);      // no rows: zeros
+    return hipGetLastError();
+}
+
+}  // namespace atb

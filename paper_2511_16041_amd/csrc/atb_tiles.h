@@ -1,4 +1,4 @@
-// bf16 products in tiles: the kernel behind the gated block and its gradients (atb_ffn.hip, atb_ffn_grad.hip).
+// bf16 products in tiles: the kernel behind the gated block and its gradients (atb_ffn.hip, atb_ffn_grad.hip), and behind products with an epilogue (atb_linear.hip).
 //
 // C tile = A tile x B tile with fp32 accumulation in MFMA accumulators, in K-steps of 64.  The tiles of a K-step come straight from memory into
 // LDS: three buffers for A and two for B, all of a CU's 160 KiB.  An operand whose reduction index is contiguous lies in LDS as rows of 64 k (128
@@ -157,7 +157,8 @@ struct Tile {
     // ---- requests
 
     // Bytes from an operand's element (row, col) to its end; rows of `cols` elements, ld apart.
-    static ATB_DEV int64_t bytes_left(int64_t rows, int64_t cols, int64_t ld, int64_t row, int64_t col) { return ((rows - 1 - row) * ld + cols - col) * 2; }
+    // (in whole dwords, as a request checks them: what is odd here has rows that are padded to multiples of 8)
+    static ATB_DEV int64_t bytes_left(int64_t rows, int64_t cols, int64_t ld, int64_t row, int64_t col) { return (((rows - 1 - row) * ld + cols - col) * 2 + 3) & ~(int64_t)3; }
 
     // The operands s: a segment of the reduction, or a problem; K-steps first .. end - 1 of it.
     ATB_DEV void open(int s, int first, int end)
@@ -179,7 +180,7 @@ struct Tile {
             b2_off.place(tid, p.ldb[1]);
         } else {
             if constexpr (BROWS) b = {reinterpret_cast<const char *>(p.B[s] + k0 * p.ldb[s] + n0), bytes_left(p.K, p.N, p.ldb[s], k0, n0)};
-            else b = {reinterpret_cast<const char *>(p.B[s] + n0 * p.ldb[s] + k0), bytes_left(p.N, p.K, p.ldb[s], n0, k0)};
+            else b = {reinterpret_cast<const char *>(p.B[s] + n0 * p.ldb[s] + k0), bytes_left(p.edge, p.K, p.ldb[s], n0, k0)};
             b_off.place(tid, p.ldb[s]);
         }
         a_src = a;
@@ -562,6 +563,109 @@ struct Tile {
         }
     }
 
+    // ---- the epilogue of a product: act(sum + bias) + residual.  Pieces of eight columns, the residual's AHEAD of them on their way.  Of C, residual and slope the
+    // rows begin at any element, and the last piece of a row may be cut.
+
+    // Columns col .. col + 7 of a row of p.edge; 0 past its end
+    template <class T>
+    ATB_DEV void load_eight(const T *row, int col, float (&v)[8]) const
+    {
+        typedef T vec __attribute__((ext_vector_type(8)));
+        typedef vec any __attribute__((aligned(sizeof(T))));
+        if (col + 8 <= p.edge) {
+            const vec w = *reinterpret_cast<const any *>(row + col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)w[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = col + e < p.edge ? (float)row[col + e] : 0.0f;
+        }
+    }
+    typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+    ATB_DEV bf16x8 load_residual(int row, int col) const
+    {
+        bf16x8 w = {};
+        const __bf16 *at = reinterpret_cast<const __bf16 *>(p.residual) + min(row, p.M - 1) * p.ldr;
+        if (col + 8 <= p.edge) {
+            w = *reinterpret_cast<const bf16x8_any *>(at + col);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < p.edge) w[e] = at[col + e];
+        }
+        return w;
+    }
+    template <class T>
+    ATB_DEV void store_eight(T *row, int col, const float (&v)[8]) const
+    {
+        typedef T vec __attribute__((ext_vector_type(8)));
+        typedef vec any __attribute__((aligned(2)));
+        if (col + 8 <= p.edge) {
+            vec w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (T)v[e];
+            *reinterpret_cast<any *>(row + col) = w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < p.edge) row[col + e] = (T)v[e];
+        }
+    }
+
+    ATB_DEV void finish_linear()
+    {
+        constexpr int PIECES = S::MI * S::NI / 2, AHEAD = 4;
+        const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), col0 = n0 + wn * 64 + piece_col();
+        float bias[S::NI / 2][8] = {};
+        if (p.bias) {
+#pragma unroll
+            for (int j = 0; j < S::NI / 2; ++j) {
+                if (p.bias_type == ATB_TYPE_F32) load_eight(static_cast<const float *>(p.bias), col0 + 32 * j, bias[j]);
+                else load_eight(static_cast<const __bf16 *>(p.bias), col0 + 32 * j, bias[j]);
+            }
+        }
+        bf16x8 res[AHEAD] = {};
+        if (p.residual) {
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) res[n] = load_residual(row0 + 16 * (n / (S::NI / 2)), col0 + 32 * (n % (S::NI / 2)));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < PIECES; ++n) {
+            const int i = n / (S::NI / 2), j = n % (S::NI / 2);
+            const int row = here(row0 + 16 * i), col = col0 + 32 * j;
+            float v[8], slope[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                unsigned x = bits(acc[i][2 * j][e]), y = bits(acc[i][2 * j + 1][e]);
+                swap_halves(x, y);
+                v[e] = __uint_as_float(x) + bias[j][e];
+                v[4 + e] = __uint_as_float(y) + bias[j][4 + e];
+            }
+            if constexpr (EPI == kLinearKeep) {
+                with_activation(p.act, [&](auto act) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) activate_grad<decltype(act)::value>(v[e], v[e], slope[e]);
+                });
+            } else {
+                with_activation_or_none(p.act, [&](auto act) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = activate<decltype(act)::value>(v[e]);
+                });
+            }
+            if (p.residual) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += (float)res[n % AHEAD][e];
+            }
+            if (row < p.M) {
+                store_eight(reinterpret_cast<__bf16 *>(p.C[0]) + (int64_t)row * p.ldc, col, v);
+                if constexpr (EPI == kLinearKeep) store_eight(reinterpret_cast<_Float16 *>(p.slope) + (int64_t)row * p.edge, col, slope);
+            }
+            if (n + AHEAD < PIECES && p.residual) res[n % AHEAD] = load_residual(here(row0 + 16 * ((n + AHEAD) / (S::NI / 2))), col0 + 32 * ((n + AHEAD) % (S::NI / 2)));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
     // A share of the sums, in fp32: plane 0 has the gate's or the (first problem's) sums, plane 1 the up projection's or the second problem's
     ATB_DEV void finish_share(int share)
     {
@@ -583,6 +687,7 @@ struct Tile {
     {
         if constexpr (is_share(EPI)) finish_share(share);
         else if constexpr (EPI == kStore) finish_plain();
+        else if constexpr (is_linear(EPI)) finish_linear();
         else if constexpr (EPI == kGatedGrad) finish_grad();
         else finish_gated();
     }
@@ -634,7 +739,33 @@ __global__ void __launch_bounds__(256) join_kernel(const TileParams p)
 #pragma unroll
         for (int n = 0; n < PLANES; ++n) sum[n] += *reinterpret_cast<const floatx4 *>(from + n * plane);
     const int64_t to = (int64_t)row * p.ldc + col;
-    if constexpr (EPI == kStore) {
+    if constexpr (is_linear(EPI)) {
+        const int cols = min(4, p.edge - col);                 // (none or fewer where N is not a multiple of 8)
+        float v[4], slope[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = sum[0][e];
+            if (p.bias && e < cols) v[e] += p.bias_type == ATB_TYPE_F32 ? static_cast<const float *>(p.bias)[col + e] : (float)static_cast<const __bf16 *>(p.bias)[col + e];
+        }
+        if constexpr (EPI == kLinearKeep) {
+            with_activation(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) activate_grad<decltype(act)::value>(v[e], v[e], slope[e]);
+            });
+        } else {
+            with_activation_or_none(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = activate<decltype(act)::value>(v[e]);
+            });
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < cols) {
+                if (p.residual) v[e] += (float)reinterpret_cast<const __bf16 *>(p.residual)[row * p.ldr + col + e];
+                reinterpret_cast<__bf16 *>(p.C[0])[to + e] = (__bf16)v[e];
+                if constexpr (EPI == kLinearKeep) reinterpret_cast<_Float16 *>(p.slope)[(int64_t)row * p.edge + col + e] = (_Float16)slope[e];
+            }
+    } else if constexpr (EPI == kStore) {
         bf16x4 c;
 #pragma unroll
         for (int e = 0; e < 4; ++e) c[e] = (__bf16)sum[0][e];
@@ -701,6 +832,7 @@ hipError_t launch_tiles(TileParams &p, hipStream_t stream)
     const TileChoice how = choose_tiles(p.M, p.N, p.K, p.segments, p.problems, is_gated(EPI), p.shares != nullptr);
     p.steps = (p.K + 63) / 64;
     p.planes = is_gated(EPI) ? 2 : p.problems;
+    if (p.edge == 0) p.edge = p.N;
     p.parts = how.parts;
     constexpr int SHARE = is_gated(EPI) ? kGatedShare : kShare;
     if (p.parts == 1) return how.large ? launch_shape<Tile256, AT, BROWS, EPI>(p, stream) : launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
