@@ -308,7 +308,7 @@ atb_status atb_q4_gated(const atb_q4 *w_gate, const atb_q4 *w_up, atb_activation
 
 /* ------------------------- what a block has around its feed-forward sublayer
  *
- * A product with its epilogue and its gradients.  As above: row-major matrices with pitches in elements, sums and statistics in fp32,
+ * A product with its epilogue and its gradients; norms on both sides of a residual sum, and theirs.  As above: row-major matrices with pitches in elements, sums and statistics in fp32,
  * no atomics (the same inputs give the same bits), workspaces that the caller owns for the call, M == 0 a valid call, non-finite inputs as the formulas
  * give them and never outside the rows and columns that depend on them. */
 
@@ -337,6 +337,46 @@ atb_status atb_linear_forward(const atb_linear *l, const void *residual, int64_t
  * slope: of the forward pass; NULL with ATB_ACT_NONE.  dy: at any element, but with ATB_ACT_NONE and N a multiple of 8 16-byte aligned with a pitch as ldx.  dx: M x K (pitch
  * lddx, as ldx), dw: N x K contiguous, both bf16 and 16-byte aligned; dbias: N elements of bias_type; each may be NULL: not asked for.  The values of l->bias are not read. */
 atb_status atb_linear_backward(const atb_linear *l, const void *slope, const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dw, void *dbias, void *hip_stream);
+
+/* What lies between two blocks: the first one's result z is normed, gated and added to the residual stream x, and the sum is normed for the next one:
+ *     r = scale x + gate o N1(z),  h = N2(r),
+ * N a layer norm, (v - mu) / sqrt(sum((v - mu)^2) / D + eps) weight + bias, a root-mean-square norm, v / sqrt(sum(v^2) / D + eps) weight + bias, or nothing: N1(z) = z, no h. */
+typedef enum atb_norm_kind { ATB_NORM_NONE = 0, ATB_NORM_RMS = 1, ATB_NORM_LAYER = 2 } atb_norm_kind;
+typedef struct atb_norm {
+    const void *weight, *bias;                  /* DEVICE, D elements of param_type, or NULL for 1 and 0 */
+    double eps;                                 /* >= 0 */
+    atb_norm_kind kind;                         /* ATB_NORM_NONE: the rest is not looked at */
+} atb_norm;
+typedef struct atb_residual_norm {
+    const void *x, *z;                          /* DEVICE, M x D of stream_type and of block_type, at any element */
+    int64_t ldx, ldz;
+    atb_norm post, pre;                         /* N1, N2 */
+    const void *gate;                           /* DEVICE, groups x D of param_type, contiguous, or NULL for 1 */
+    int64_t groups;                             /* 1 .. 65535, M a multiple: row i is gated by row i / (M / groups) of gate; 1 without a gate */
+    double scale;                               /* finite */
+    int64_t M, D;                               /* 0 <= M <= 2^23, 1 <= D <= 2^24 */
+    atb_type stream_type, block_type, param_type;       /* of x, r and their gradients; of z, h and theirs, not wider than the first; of gate, weights and biases */
+} atb_residual_norm;
+
+/* r: DEVICE, M x D of stream_type (pitch ldr); may be x.  h: M x D of block_type (pitch ldh), with a norm `pre`; may be z.  Both at any element.  h is the norm of the sum before it is
+ * rounded to stream_type.  stats: DEVICE, 4 x M floats, what the backward pass takes of both norms, or NULL.  Async on hip_stream. */
+atb_status atb_residual_norm_forward(const atb_residual_norm *p, void *r, int64_t ldr, void *h, int64_t ldh, float *stats, void *hip_stream);
+
+/* Where the gradients go: dx M x D of stream_type, dz of block_type, the others as what they are gradients of; each may be NULL: not asked for. */
+typedef struct atb_residual_norm_grads {
+    void *dx, *dz;
+    int64_t lddx, lddz;
+    void *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+} atb_residual_norm_grads;
+
+/* Bytes of the workspace of a backward pass that one of the last five is asked of; 0 on invalid arguments. */
+size_t atb_residual_norm_workspace(int64_t M, int64_t D, int64_t groups);
+
+/* dr: DEVICE, M x D of stream_type (pitch lddr), the gradient of r by all that follows but h, or NULL for 0; dh: of block_type (pitch lddh), with a norm `pre`.  x and z as in the forward pass (r is
+ * computed again: rounded to bf16 it would cost the gradients digits, and x is no longer to read).  stats: of the forward pass.  workspace: DEVICE, 16-byte aligned.  The sums over rows are taken in an order
+ * that M, D and groups alone decide. */
+atb_status atb_residual_norm_backward(const atb_residual_norm *p, const float *stats, const void *dr, int64_t lddr, const void *dh, int64_t lddh,
+                                      const atb_residual_norm_grads *grads, void *workspace, void *hip_stream);
 
 /* ------------------------------------------------- model and tile selector */
 

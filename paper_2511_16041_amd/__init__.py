@@ -7,7 +7,8 @@ The calls that launch a GEMM or the quantiser go through a small extension
 module (csrc/atb_binding.cpp), everything else through ctypes.
 The operators of a transformer's feed-forward sublayer (layer norm, the gated
 block, products with 4-bit weights) are in layers.py, those of a block around it
-(a product with its epilogue) in block.py; all are reached from here.
+(a product with its epilogue, norms on both sides of a residual sum) in block.py;
+all are reached from here.
 """
 from __future__ import annotations
 
@@ -95,6 +96,24 @@ class Linear(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("M", "N", "K")] + [("act", ctypes.c_int), ("bias_type", ctypes.c_int), ("workspace", ctypes.c_void_p)]
 
 
+class NormArgs(ctypes.Structure):
+    """atb_norm"""
+    _fields_ = [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("eps", ctypes.c_double), ("kind", ctypes.c_int)]
+
+
+class ResidualNorm(ctypes.Structure):
+    """atb_residual_norm: the operands of norms on both sides of a residual sum."""
+    _fields_ = [("x", ctypes.c_void_p), ("z", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("ldz", ctypes.c_int64), ("post", NormArgs), ("pre", NormArgs), ("gate", ctypes.c_void_p),
+                ("groups", ctypes.c_int64), ("scale", ctypes.c_double), ("M", ctypes.c_int64), ("D", ctypes.c_int64), ("stream_type", ctypes.c_int), ("block_type", ctypes.c_int),
+                ("param_type", ctypes.c_int)]
+
+
+class ResidualNormGradArgs(ctypes.Structure):
+    """atb_residual_norm_grads"""
+    _fields_ = [("dx", ctypes.c_void_p), ("dz", ctypes.c_void_p), ("lddx", ctypes.c_int64), ("lddz", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("dgate", "dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")]
+
+
 # every symbol include/atb.h declares
 EXPORTS = [
     "atb_status_string", "atb_last_hip_error", "atb_gemm_create", "atb_gemm_create_fmt", "atb_gemm_run", "atb_gemm_destroy",
@@ -104,6 +123,7 @@ EXPORTS = [
     "atb_layer_norm", "atb_layer_norm_workspace", "atb_layer_norm_backward", "atb_ffn_workspace", "atb_ffn_backward_workspace", "atb_ffn_kept_bytes", "atb_ffn_forward", "atb_ffn_backward",
     "atb_q4_quantize", "atb_q4_decode", "atb_q4_matvec", "atb_q4_gated",
     "atb_linear_workspace", "atb_linear_backward_workspace", "atb_linear_forward", "atb_linear_backward",
+    "atb_residual_norm_workspace", "atb_residual_norm_forward", "atb_residual_norm_backward",
 ]
 
 
@@ -186,6 +206,11 @@ def lib() -> ctypes.CDLL:
     L.atb_linear_forward.restype = L.atb_linear_backward.restype = ci
     L.atb_linear_forward.argtypes = [ctypes.POINTER(Linear), vp, i64, vp, vp, i64, vp]
     L.atb_linear_backward.argtypes = [ctypes.POINTER(Linear), vp, vp, i64, vp, i64, vp, vp, vp]
+    L.atb_residual_norm_workspace.restype = ctypes.c_size_t
+    L.atb_residual_norm_workspace.argtypes = [i64, i64, i64]
+    L.atb_residual_norm_forward.restype = L.atb_residual_norm_backward.restype = ci
+    L.atb_residual_norm_forward.argtypes = [ctypes.POINTER(ResidualNorm), vp, i64, vp, i64, vp, vp]
+    L.atb_residual_norm_backward.argtypes = [ctypes.POINTER(ResidualNorm), vp, vp, i64, vp, i64, ctypes.POINTER(ResidualNormGradArgs), vp, vp]
     _lib = L
     return L
 
@@ -465,4 +490,4 @@ class Gemm:
 
 from .layers import (FeedForwardState, Q4Weight, feed_forward, feed_forward_backward, layer_norm, layer_norm_backward, q4_decode,  # noqa: E402
                      q4_feed_forward, q4_matvec, q4_quantize)
-from .block import linear, linear_backward  # noqa: E402
+from .block import Norm, ResidualNormGrads, linear, linear_backward, residual_norm, residual_norm_backward  # noqa: E402

@@ -557,10 +557,119 @@ PyObject *linear_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// A norm of four arguments: kind (atb_norm_kind), weight, bias, eps.  Parameters in `type`, which the first one sets (-1: none yet); false: not what the kernels take
+bool describe(atb_norm &norm, PyObject *const *args, int64_t D, int &type, const at::Device &on)
+{
+    norm = {};
+    norm.kind = static_cast<atb_norm_kind>(PyLong_AsLong(args[0]));
+    norm.eps = PyFloat_AsDouble(args[3]);
+    const void **to[2] = {&norm.weight, &norm.bias};
+    for (int i = 0; i < 2; ++i) {
+        const auto t = optional_tensor(args[1 + i]);
+        if (!t) continue;
+        if (type < 0 && is_float(*t)) type = type_of(*t);
+        if (!is_float(*t) || type_of(*t) != type || !is_vector(*t, t->scalar_type(), D, on)) return false;
+        *to[i] = t->data_ptr();
+    }
+    return true;
+}
+
+// x, z, and of 10 arguments the norms, gate and scale: post (4), gate, scale, pre (4)
+bool describe(atb_residual_norm &p, const at::Tensor &x, const at::Tensor &z, PyObject *const *args)
+{
+    if (!x.is_cuda() || !is_float(x) || x.dim() != 2 || (z.scalar_type() != x.scalar_type() && z.scalar_type() != at::kBFloat16)) return false;
+    const at::Device on = x.device();
+    p = {};
+    p.M = x.size(0);
+    p.D = x.size(1);
+    if (!is_rows(x, x.scalar_type(), p.M, p.D, on) || !is_rows(z, z.scalar_type(), p.M, p.D, on)) return false;
+    p.x = x.data_ptr(); p.ldx = apart(x);
+    p.z = z.data_ptr(); p.ldz = apart(z);
+    p.stream_type = type_of(x);
+    p.block_type = type_of(z);
+    int type = -1;
+    const auto gate = optional_tensor(args[4]);
+    p.groups = 1;
+    if (gate) {
+        if (!is_float(*gate) || gate->device() != on || !gate->is_contiguous() || gate->dim() < 1 || gate->dim() > 2 || gate->size(-1) != p.D) return false;
+        type = type_of(*gate);
+        p.gate = gate->data_ptr();
+        if (gate->dim() == 2) p.groups = gate->size(0);
+        if (p.groups < 1 || p.M % p.groups != 0) return false;
+    }
+    if (!describe(p.post, args, p.D, type, on) || !describe(p.pre, args + 6, p.D, type, on)) return false;
+    p.param_type = type < 0 ? p.block_type : static_cast<atb_type>(type);
+    p.scale = PyFloat_AsDouble(args[5]);
+    return !PyErr_Occurred();
+}
+
+// residual_norm(entry, x, z, post's kind, weight, bias, eps, gate, scale, pre's kind, weight, bias, eps, save) -> (r, h or None), or (r, h, stats)
+PyObject *residual_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 14) return PyErr_Format(PyExc_TypeError, "residual_norm takes 14 arguments");
+    const auto call = reinterpret_cast<decltype(&atb_residual_norm_forward)>(PyLong_AsVoidPtr(args[0]));
+    const int save = PyObject_IsTrue(args[13]);
+    if (PyErr_Occurred() || !tensors(args + 1, 2) || !tensors_or_none(args + 4, 2) || !tensors_or_none(args + 7, 1) || !tensors_or_none(args + 10, 2)) return nullptr;
+    HANDLE_TH_ERRORS
+    const at::Tensor &x = THPVariable_Unpack(args[1]), &z = THPVariable_Unpack(args[2]);
+    atb_residual_norm p;
+    if (!describe(p, x, z, args + 3)) return PyErr_Occurred() ? nullptr : refuse();
+    const at::Device on = x.device();
+    const c10::DeviceGuard guard(on);
+    const at::Tensor r = make({p.M, p.D}, x.scalar_type(), on);
+    std::optional<at::Tensor> h, stats;
+    if (p.pre.kind != ATB_NORM_NONE) h = make({p.M, p.D}, z.scalar_type(), on);
+    if (save) stats = make({4, p.M}, at::kFloat, on);
+    int st;
+    {
+        WithoutLock unlocked;
+        st = call(&p, r.data_ptr(), p.D, data<void *>(h), p.D, data<float *>(stats), current_stream());
+    }
+    if (st != 0) return PyLong_FromLong(st);
+    return save ? tuple_of({r, h, stats}) : tuple_of({r, h});
+    END_HANDLE_TH_ERRORS
+}
+
+// residual_norm_backward(entry, entry of the workspace's size, dr, dh, x, z, stats, and the ten arguments of the forward pass from post's kind on)
+// -> (dx, dz, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias), None for what there is not
+PyObject *residual_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 17) return PyErr_Format(PyExc_TypeError, "residual_norm_backward takes 17 arguments");
+    const auto call = reinterpret_cast<decltype(&atb_residual_norm_backward)>(PyLong_AsVoidPtr(args[0]));
+    const auto room = reinterpret_cast<decltype(&atb_residual_norm_workspace)>(PyLong_AsVoidPtr(args[1]));
+    if (PyErr_Occurred() || !tensors_or_none(args + 2, 2) || !tensors(args + 4, 3) || !tensors_or_none(args + 8, 2) || !tensors_or_none(args + 11, 1) || !tensors_or_none(args + 14, 2)) return nullptr;
+    HANDLE_TH_ERRORS
+    const at::Tensor &x = THPVariable_Unpack(args[4]), &z = THPVariable_Unpack(args[5]), &stats = THPVariable_Unpack(args[6]);
+    const auto dr = optional_tensor(args[2]), dh = optional_tensor(args[3]), gate = optional_tensor(args[11]);
+    atb_residual_norm p;
+    if (!describe(p, x, z, args + 7)) return PyErr_Occurred() ? nullptr : refuse();
+    const at::Device on = x.device();
+    if ((dr && !is_rows(*dr, x.scalar_type(), p.M, p.D, on)) || (dh && !is_rows(*dh, z.scalar_type(), p.M, p.D, on)) || dh.has_value() != (p.pre.kind != ATB_NORM_NONE)) return refuse();
+    if (stats.device() != on || stats.scalar_type() != at::kFloat || stats.dim() != 2 || stats.size(0) != 4 || stats.size(1) != p.M || !stats.is_contiguous()) return refuse();
+    const c10::DeviceGuard guard(on);
+    const at::ScalarType type = p.param_type == ATB_TYPE_F32 ? at::kFloat : at::kBFloat16;
+    const at::Tensor dx = make({p.M, p.D}, x.scalar_type(), on), dz = make({p.M, p.D}, z.scalar_type(), on);
+    std::optional<at::Tensor> dgate, params[4], work;
+    if (gate) dgate = make(gate->sizes(), type, on);
+    const void *there[4] = {p.post.weight, p.post.bias, p.pre.weight, p.pre.bias};
+    // (a norm that is none has no parameters)
+    for (int i = 0; i < 4; ++i)
+        if (there[i] && (i < 2 ? p.post : p.pre).kind != ATB_NORM_NONE) params[i] = make({p.D}, type, on);
+    if (dgate || params[0] || params[1] || params[2] || params[3]) work = make({(int64_t)room(p.M, p.D, p.groups)}, at::kByte, on);
+    const atb_residual_norm_grads g = {dx.data_ptr(), dz.data_ptr(), p.D, p.D, data<void *>(dgate), data<void *>(params[0]), data<void *>(params[1]), data<void *>(params[2]), data<void *>(params[3])};
+    int st;
+    {
+        WithoutLock unlocked;
+        st = call(&p, data<const float *>(stats), data<void *>(dr), dr ? apart(*dr) : 0, data<void *>(dh), dh ? apart(*dh) : 0, &g, data<void *>(work), current_stream());
+    }
+    return st == 0 ? tuple_of({dx, dz, dgate, params[0], params[1], params[2], params[3]}) : PyLong_FromLong(st);
+    END_HANDLE_TH_ERRORS
+}
+
 #define ATB_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ATB_METHOD(run), ATB_METHOD(quantize), ATB_METHOD(decode), ATB_METHOD(layer_norm), ATB_METHOD(layer_norm_backward), ATB_METHOD(ffn_forward),
                          ATB_METHOD(ffn_backward), ATB_METHOD(q4_matvec), ATB_METHOD(q4_ffn), ATB_METHOD(q4_quantize), ATB_METHOD(q4_decode),
-                         ATB_METHOD(linear), ATB_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
+                         ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(residual_norm), ATB_METHOD(residual_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_launch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,4 +1,4 @@
-// Internal declarations of what a transformer's block has around its feed-forward sublayer: a product with its epilogue.
+// Internal declarations of what a transformer's block has around its feed-forward sublayer: a product with its epilogue, norms on both sides of a residual sum.
 // Not part of the public C ABI (see include/atb.h).
 #pragma once
 
@@ -29,6 +29,63 @@ static inline int64_t linear_parts(int64_t M, int64_t N)
     if (M <= 0) return 0;
     const int64_t blocks = (N + 2047) / 2048, wanted = std::max<int64_t>(1, std::min(1024 / std::min<int64_t>(blocks, 1024), (M + 15) / 16));
     return std::max(wanted, (M + 511) / 512);
+}
+
+// ---- norms on both sides of a residual sum (atb_residual.hip)
+
+struct NormSpec {
+    int kind;                    // atb_norm_kind
+    const void *weight, *bias;   // null: 1 and 0
+    float eps;
+};
+struct ResidualParams {
+    const void *x, *z;           // M x D: the residual stream and the block's result
+    void *r, *h;                 // the sum, and (a norm `pre`) its norm
+    const void *dr, *dh;         // their gradients (dr may be null: 0)
+    void *dx, *dz;               // null: not asked for
+    int64_t ldx, ldz, ldr, ldh, lddr, lddh, lddx, lddz;
+    NormSpec post, pre;
+    const void *gate;            // groups x D, or null
+    int64_t groups;              // 1 without a gate; M is a multiple
+    float scale;
+    float *stats;                // 4 x M: mean and 1 / size of post, of pre
+    void *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;       // null: not asked for
+    float *workspace;            // residual_room(M, D, groups).total floats, where one of them is asked for
+    int64_t M;
+    int D;
+    int x_type, z_type, w_type;  // atb_type
+    int parts;                   // set by the launch: workgroups that share the sums over a group's rows
+};
+hipError_t launch_residual(const ResidualParams &p, hipStream_t stream);
+hipError_t launch_residual_backward(const ResidualParams &p, hipStream_t stream);
+
+constexpr int kResidualPerThread = 8;              // elements of a row that a thread holds, of long rows a few times as many
+constexpr int kResidualThreads = 512;              // workgroup of the backward pass: 256 registers per thread
+constexpr int kResidualMaxGradRow = 2 * kResidualThreads * kResidualPerThread;       // longer rows are read again for every sum
+
+// Threads per row: the power of two, 64 to 512, that holds it.
+static inline int residual_threads(int64_t D)
+{
+    int t = 64;
+    while (t < kResidualThreads && (int64_t)t * kResidualPerThread < D) t *= 2;
+    return t;
+}
+
+// The backward pass's workspace in floats.  Sums over the rows of a group are taken by `parts` workgroups, one per CU of the 256 in all (of rows longer than
+// kResidualMaxGradRow, whose sums are a pass of their own, 64 times the column blocks), with chains of at most 512 rows as in norm_partials.
+struct ResidualRoom { int64_t parts, sums, totals, rows, total; };
+static inline ResidualRoom residual_room(int64_t M, int64_t D, int64_t groups)
+{
+    ResidualRoom r = {};
+    const bool is_long = D > kResidualMaxGradRow;
+    const int64_t rows = M / groups, at_once = is_long ? 1 : kResidualThreads / residual_threads(D), most = std::max<int64_t>(1, (is_long ? 64 : 256) / groups);
+    const int64_t turns = (rows + at_once - 1) / at_once;
+    r.parts = M == 0 ? 0 : turns < most ? turns : most * ((turns + most * 512 - 1) / (most * 512));
+    r.sums = round_up(groups * r.parts * 4 * D, 4);
+    r.totals = groups > 1 ? round_up(groups * 4 * D, 4) : 0;
+    r.rows = is_long ? round_up(2 * M, 4) : 0;
+    r.total = r.sums + r.totals + r.rows;
+    return r;
 }
 
 }  // namespace atb

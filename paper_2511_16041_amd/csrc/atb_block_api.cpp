@@ -3,7 +3,7 @@
 
 namespace {
 
-constexpr int64_t kMaxRows = (int64_t)1 << 23, kMaxPitch = (int64_t)1 << 22;
+constexpr int64_t kMaxRows = (int64_t)1 << 23, kMaxPitch = (int64_t)1 << 22, kMaxNorm = (int64_t)1 << 24;
 
 using atb::hip_status;
 
@@ -154,4 +154,100 @@ extern "C" atb_status atb_linear_backward(const atb_linear *l, const void *slope
         st = hip_status(atb::launch_tiles_dw(p, stream));
     }
     return st;
+}
+
+// ------------------------------------------------------------------ norms on both sides of a residual sum
+
+namespace {
+
+bool residual_lengths(int64_t M, int64_t D, int64_t groups)
+{
+    return M >= 0 && M <= kMaxRows && D >= 1 && D <= kMaxNorm && groups >= 1 && groups <= 65535 && M % groups == 0;
+}
+bool is_norm(const atb_norm &n, atb_type type)
+{
+    if (n.kind == ATB_NORM_NONE) return true;
+    return (n.kind == ATB_NORM_RMS || n.kind == ATB_NORM_LAYER) && n.eps >= 0.0 && aligned(n.weight, size_of(type)) && aligned(n.bias, size_of(type));
+}
+bool is_residual(const atb_residual_norm *p)
+{
+    if (!p || !residual_lengths(p->M, p->D, p->groups) || !is_type(p->stream_type) || !is_type(p->block_type) || !is_type(p->param_type)) return false;
+    if (p->block_type == ATB_TYPE_F32 && p->stream_type != ATB_TYPE_F32) return false;
+    if (!is_norm(p->post, p->param_type) || !is_norm(p->pre, p->param_type) || !aligned(p->gate, size_of(p->param_type)) || (!p->gate && p->groups != 1)) return false;
+    if (!(p->scale - p->scale == 0.0)) return false;
+    return p->M == 0 || (is_rows(p->x, p->D, p->ldx, size_of(p->stream_type)) && is_rows(p->z, p->D, p->ldz, size_of(p->block_type)));
+}
+atb::NormSpec spec(const atb_norm &n)
+{
+    if (n.kind == ATB_NORM_NONE) return {ATB_NORM_NONE, nullptr, nullptr, 0.0f};
+    return {n.kind, n.weight, n.bias, (float)n.eps};
+}
+atb::ResidualParams residual(const atb_residual_norm *p)
+{
+    atb::ResidualParams r = {};
+    r.x = p->x; r.ldx = p->ldx;
+    r.z = p->z; r.ldz = p->ldz;
+    r.post = spec(p->post);
+    r.pre = spec(p->pre);
+    r.gate = p->gate;
+    r.groups = p->groups;
+    r.scale = (float)p->scale;
+    r.M = p->M;
+    r.D = (int)p->D;
+    r.x_type = p->stream_type;
+    r.z_type = p->block_type;
+    r.w_type = p->param_type;
+    return r;
+}
+
+}  // namespace
+
+extern "C" atb_status atb_residual_norm_forward(const atb_residual_norm *p, void *r, int64_t ldr, void *h, int64_t ldh, float *stats, void *hip_stream)
+{
+    if (!is_residual(p) || !aligned(stats, 4)) return ATB_ERR_INVALID_ARG;
+    if (p->M == 0) return ATB_OK;
+    if (!is_rows(r, p->D, ldr, size_of(p->stream_type))) return ATB_ERR_INVALID_ARG;
+    if (p->pre.kind == ATB_NORM_NONE ? h != nullptr : !is_rows(h, p->D, ldh, size_of(p->block_type))) return ATB_ERR_INVALID_ARG;
+    atb::ResidualParams q = residual(p);
+    q.r = r; q.ldr = ldr;
+    q.h = h; q.ldh = ldh;
+    q.stats = stats;
+    return hip_status(atb::launch_residual(q, static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" size_t atb_residual_norm_workspace(int64_t M, int64_t D, int64_t groups)
+{
+    return residual_lengths(M, D, groups) ? sizeof(float) * (size_t)atb::residual_room(M, D, groups).total : 0;
+}
+
+extern "C" atb_status atb_residual_norm_backward(const atb_residual_norm *p, const float *stats, const void *dr, int64_t lddr, const void *dh, int64_t lddh,
+                                                 const atb_residual_norm_grads *grads, void *workspace, void *hip_stream)
+{
+    if (!is_residual(p) || !grads) return ATB_ERR_INVALID_ARG;
+    const uintptr_t es = size_of(p->stream_type), eb = size_of(p->block_type), ep = size_of(p->param_type);
+    const atb_residual_norm_grads &g = *grads;
+    for (const void *d : {g.dgate, g.dpost_weight, g.dpost_bias, g.dpre_weight, g.dpre_bias})
+        if (!aligned(d, ep)) return ATB_ERR_INVALID_ARG;
+    // a gradient of what there is not
+    if (((g.dpost_weight || g.dpost_bias) && p->post.kind == ATB_NORM_NONE) || ((g.dpre_weight || g.dpre_bias) && p->pre.kind == ATB_NORM_NONE) || (g.dgate && !p->gate)) return ATB_ERR_INVALID_ARG;
+    const bool asked = g.dgate || g.dpost_weight || g.dpost_bias || g.dpre_weight || g.dpre_bias;
+    if (asked && atb::residual_room(p->M, p->D, p->groups).total > 0 && (!workspace || !aligned(workspace, 16))) return ATB_ERR_INVALID_ARG;
+    if (p->M > 0) {
+        if (!stats || !aligned(stats, 4) || (dr && !is_rows(dr, p->D, lddr, es))) return ATB_ERR_INVALID_ARG;
+        if (p->pre.kind == ATB_NORM_NONE ? dh != nullptr : !is_rows(dh, p->D, lddh, eb)) return ATB_ERR_INVALID_ARG;
+        if ((g.dx && !is_rows(g.dx, p->D, g.lddx, es)) || (g.dz && !is_rows(g.dz, p->D, g.lddz, eb))) return ATB_ERR_INVALID_ARG;
+    }
+    atb::ResidualParams q = residual(p);
+    q.stats = const_cast<float *>(stats);
+    q.dr = dr; q.lddr = lddr;
+    q.dh = dh; q.lddh = lddh;
+    q.dx = g.dx; q.lddx = g.lddx;
+    q.dz = g.dz; q.lddz = g.lddz;
+    q.dgate = g.dgate;
+    q.dpost_weight = g.dpost_weight;
+    q.dpost_bias = g.dpost_bias;
+    q.dpre_weight = g.dpre_weight;
+    q.dpre_bias = g.dpre_bias;
+    q.workspace = static_cast<float *>(workspace);
+    return hip_status(atb::launch_residual_backward(q, static_cast<hipStream_t>(hip_stream)));
 }

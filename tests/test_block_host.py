@@ -89,3 +89,94 @@ def test_linear_gradients_against_differences(act):
         v = torch.randn((x, w, b)[at].shape, generator=g, dtype=torch.float64)
         grad = float((want[name][0] * v).sum())
         assert abs(_slope(loss, (x, w, b), at, v) - grad) < 1e-6 * (1 + abs(grad))
+
+
+# ------------------------------------------------------------------ norms on both sides of a residual sum
+
+def test_residual_norm_refuses():
+    L = atb.lib()
+    keep, a = aligned_address()
+    rms, nothing = atb.NormArgs(a, a, 1e-5, 1), atb.NormArgs(None, None, 0.0, 0)
+    good = dict(x=a, z=a, ldx=8, ldz=8, post=rms, pre=rms, gate=a, groups=2, scale=1.0, M=4, D=8, stream_type=0, block_type=0, param_type=0)
+
+    def forward(r=a, ldr=8, h=a, ldh=8, stats=a, **kw):
+        return L.atb_residual_norm_forward(ctypes.byref(atb.ResidualNorm(**{**good, **kw})), r, ldr, h, ldh, stats, None)
+
+    def backward(stats=a, dr=a, lddr=8, dh=a, lddh=8, grads=None, work=a, **kw):
+        g = atb.ResidualNormGradArgs(**{**dict(dx=a, dz=a, lddx=8, lddz=8, dgate=a, dpost_weight=a, dpost_bias=a, dpre_weight=a, dpre_bias=a), **(grads or {})})
+        return L.atb_residual_norm_backward(ctypes.byref(atb.ResidualNorm(**{**good, **kw})), stats, dr, lddr, dh, lddh, ctypes.byref(g), work, None)
+    shared = [dict(x=None), dict(z=None), dict(x=a + 1), dict(z=a + 1), dict(x=a + 2, stream_type=1), dict(ldx=7), dict(ldz=7), dict(gate=a + 1), dict(gate=None), dict(groups=0), dict(groups=3), dict(groups=65536, M=65536),
+              dict(M=-2), dict(M=2 ** 23 + 2), dict(D=0), dict(D=2 ** 24 + 1, ldx=2 ** 25, ldz=2 ** 25), dict(stream_type=2), dict(block_type=-1), dict(param_type=2), dict(block_type=1), dict(scale=float("nan")),
+              dict(scale=float("inf"))]
+    for side in ("post", "pre"):
+        shared += [{side: atb.NormArgs(a, a, 1e-5, 3)}, {side: atb.NormArgs(a, a, -1.0, 1)}, {side: atb.NormArgs(a, a, float("nan"), 2)}, {side: atb.NormArgs(a + 1, a, 0.0, 1)}, {side: atb.NormArgs(a, a + 1, 0.0, 2)}]
+    for bad in shared + [dict(r=None), dict(r=a + 1), dict(ldr=7), dict(h=None), dict(ldh=7), dict(h=a + 1), dict(stats=a + 2), dict(pre=nothing)]:
+        assert forward(**bad) == INVALID, bad
+    for bad in shared + [dict(stats=None), dict(stats=a + 2), dict(dr=a + 1), dict(lddr=7), dict(dh=None), dict(lddh=7), dict(work=None), dict(work=a + 8), dict(pre=nothing), dict(post=nothing), dict(gate=None, groups=1),
+                         dict(grads=dict(dx=a + 1)), dict(grads=dict(lddx=7)), dict(grads=dict(dz=a + 1)), dict(grads=dict(lddz=0)), dict(grads=dict(dgate=a + 1)), dict(grads=dict(dpre_bias=a + 1))]:
+        assert backward(**bad) == INVALID, bad
+    assert L.atb_residual_norm_forward(None, a, 8, a, 8, a, None) == INVALID
+    assert L.atb_residual_norm_backward(ctypes.byref(atb.ResidualNorm(**good)), a, a, 8, a, 8, None, a, None) == INVALID
+    assert forward(M=0, x=None, z=None, r=None, h=None) == 0
+    assert backward(M=0, x=None, z=None, dh=None, stats=None, grads={k: None for k in ("dgate", "dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")}) == 0
+    if not __import__("torch").cuda.is_available():
+        assert forward() == forward(pre=nothing, h=None) == forward(post=nothing, gate=None, groups=1) == forward(D=20000, ldx=20000, ldz=20000, ldr=20000, ldh=20000) == backward() == backward(dr=None) == 5
+
+
+def test_workspace_of_a_residual_norm():
+    L = atb.lib()
+    for M in (0, 6, 600, 60000, 2 ** 23 - 2 ** 23 % 6):
+        for D in (1, 4096, 8193, 2 ** 24):
+            for groups in (1, 2, 6):
+                assert L.atb_residual_norm_workspace(M, D, groups) >= (16 * D * groups if M else 0) and L.atb_residual_norm_workspace(M, D, groups) % 16 == 0
+    assert L.atb_residual_norm_workspace(8192, 4096, 1) <= 32 << 20
+    for bad in ((-1, 8, 1), (4, 0, 1), (4, 8, 0), (4, 8, 3), (2 ** 23 + 1, 8, 1), (4, 2 ** 24 + 1, 1), (65536, 8, 65536)):
+        assert L.atb_residual_norm_workspace(*bad) == 0
+
+
+def test_residual_norm_refuses_tensors_that_a_kernel_would_read_or_store_past():
+    import torch
+    bf, f32 = torch.bfloat16, torch.float32
+    x, v = _on_device((4, 64), bf), _on_device((64,), bf)
+    wide = _on_device((4, 64), f32)
+    for args in [(torch.zeros(4, 64, dtype=bf), x), (x, _on_device((4, 63), bf)), (x, _on_device((3, 64), bf)), (_on_device((4, 64), torch.float16), x), (x, _on_device((4, 64), bf, (1, 4))),
+                 (x, x, atb.Norm("rms", _on_device((63,), bf))), (x, x, atb.Norm("rms", v, _on_device((64,), f32))), (x, x, atb.Norm("rms", v), _on_device((64,), f32)), (x, x, atb.Norm("rms", torch.zeros(64, dtype=bf))),
+                 (x, x, None, _on_device((2, 64), bf, (128, 1))), (x, x, None, _on_device((2, 63), bf)), (x, x, None, _on_device((1, 1, 64), bf)), (x, x, None, v, 1.0, atb.Norm("rms", _on_device((64,), bf, (2,))))]:
+        with pytest.raises(AssertionError):
+            atb.residual_norm(*args)
+    for args in [(x, x, None, _on_device((3, 64), bf)), (x, x, None, _on_device((0, 64), bf)), (x, wide)]:       # 4 rows in 3 groups, in none, a block wider than the stream
+        with pytest.raises(AssertionError):
+            atb.residual_norm(*args)
+    with pytest.raises(ValueError, match="rms"):
+        atb.residual_norm(x, x, atb.Norm("batch"))
+    stats = _on_device((4, 4), f32)
+    pre = atb.Norm("rms", v)
+    for dr, dh, st, norm in [(_on_device((4, 63), bf), x, stats, pre), (wide, x, stats, pre), (x, None, stats, pre), (x, x, stats, None), (x, wide, stats, pre), (x, x, _on_device((4, 3), f32), pre),
+                             (x, x, _on_device((4, 4), bf), pre), (x, x, _on_device((4, 4), f32, (1, 4)), pre)]:
+        with pytest.raises(AssertionError):
+            atb.residual_norm_backward(dr, dh, x, x, st, None, None, 1.0, norm)
+
+
+@pytest.mark.parametrize("post,pre,groups", [("rms", "rms", 1), ("layer", "layer", 2), (None, "rms", 0), ("layer", None, 4)])
+def test_residual_norm_gradients_against_differences(post, pre, groups):
+    """The formulas that the GPU tests compare with."""
+    import torch
+    from test_gpu_residual import inputs, reference
+    a = inputs(4, 10, torch.float64, torch.float64, torch.float64, post, pre, groups=groups, seed=2, device="cpu")
+    want = reference(a)
+
+    def loss(b):
+        out = reference(b)
+        return (out["r"][0] * a["dr"]).sum() + ((out["h"][0] * a["dh"]).sum() if pre else 0)
+    names = ["dx", "dz"] + ["dgate"] * (groups > 0) + [f"d{s}_{w}" for s, n in (("post", post), ("pre", pre)) if n for w in ("weight", "bias")]
+    g = torch.Generator().manual_seed(3)
+    for name in names:
+        side, _, which = name[1:].partition("_")
+        here = getattr(a[side], which) if which else a[side]
+        v = torch.randn(here.shape, generator=g, dtype=torch.float64)
+
+        def moved(t):
+            return loss({**a, side: a[side]._replace(**{which: t}) if which else t})
+        slope = _slope(moved, (here,), 0, v)
+        grad = float((want[name][0].reshape(here.shape) * v).sum())
+        assert abs(slope - grad) < 1e-6 * (1 + abs(grad)), name
