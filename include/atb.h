@@ -308,7 +308,7 @@ atb_status atb_q4_gated(const atb_q4 *w_gate, const atb_q4 *w_up, atb_activation
 
 /* ------------------------- what a block has around its feed-forward sublayer
  *
- * A product with its epilogue and its gradients; norms on both sides of a residual sum, and theirs.  As above: row-major matrices with pitches in elements, sums and statistics in fp32,
+ * A product with its epilogue and its gradients; norms on both sides of a residual sum, and theirs; a mixture of experts for few tokens.  As above: row-major matrices with pitches in elements, sums and statistics in fp32,
  * no atomics (the same inputs give the same bits), workspaces that the caller owns for the call, M == 0 a valid call, non-finite inputs as the formulas
  * give them and never outside the rows and columns that depend on them. */
 
@@ -377,6 +377,32 @@ size_t atb_residual_norm_workspace(int64_t M, int64_t D, int64_t groups);
  * that M, D and groups alone decide. */
 atb_status atb_residual_norm_backward(const atb_residual_norm *p, const float *stats, const void *dr, int64_t lddr, const void *dh, int64_t lddh,
                                       const atb_residual_norm_grads *grads, void *workspace, void *hip_stream);
+
+/* A mixture of E experts, each a gated block, for few tokens: with l = x R^T, every token's k largest l (of equal ones the lowest expert), p = softmax(l) (renormalize != 0: of the chosen l alone),
+ *     y = sum over the chosen experts e of p_e (act(x Wg_e^T) o (x Wu_e^T)) Wd_e^T,
+ * weights in bf16 or all three in 4 bits.  l is summed in fp64, the products, p and the sum over the experts are fp32; the inner activations are rounded to bf16.  Only the chosen experts' weights are read, once for every 16 tokens
+ * (32 where an expert has more than 12 on average; 4 bits: 16) that chose them.  A NaN among a token's l is behind all numbers, and its p as softmax gives it; 4-bit weights: see atb_q4_matvec. */
+typedef struct atb_moe_weight {                 /* of all experts, one expert's rows after the other's, contiguous; DEVICE */
+    const void *w;                              /* bf16, or codes as atb_q4's; 16-byte aligned */
+    const void *scales, *zeros;                 /* 4 bits: as atb_q4's; all three weights with zero points or none */
+} atb_moe_weight;
+typedef struct atb_moe {
+    const void *x, *router;                     /* DEVICE, bf16, 16-byte aligned: M x D, and E x D */
+    int64_t ldx, ld_router;                     /* multiples of 8, below 2^22 */
+    atb_moe_weight w_gate, w_up, w_down;        /* E x F x D, E x F x D, E x D x F */
+    int64_t M, D, F;                            /* 0 <= M <= 64; D, F multiples of 8 (4 bits: of group), below 2^22 */
+    int experts, top_k;                         /* 1 <= E <= 256, 1 <= k <= min(E, 16) */
+    int group;                                  /* 0: bf16; 32, 64 or 128 */
+    atb_activation act;
+    int renormalize;
+    void *workspace;                            /* DEVICE, 16-byte aligned, of the bytes below for the call */
+} atb_moe;
+
+/* Bytes of the workspace: the l, the plan of the call, the inner activations; 0 on invalid arguments. */
+size_t atb_moe_workspace(int64_t M, int64_t F, int experts, int top_k);
+
+/* y: DEVICE, M x D bf16 (pitch ldy), at any element.  chosen, p: DEVICE, M x k int32 and fp32, or NULL: the experts of every token from its largest l on, and their p.  Async on hip_stream. */
+atb_status atb_moe_forward(const atb_moe *m, void *y, int64_t ldy, int32_t *chosen, float *p, void *hip_stream);
 
 /* ------------------------------------------------- model and tile selector */
 

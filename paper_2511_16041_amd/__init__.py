@@ -7,8 +7,8 @@ The calls that launch a GEMM or the quantiser go through a small extension
 module (csrc/atb_binding.cpp), everything else through ctypes.
 The operators of a transformer's feed-forward sublayer (layer norm, the gated
 block, products with 4-bit weights) are in layers.py, those of a block around it
-(a product with its epilogue, norms on both sides of a residual sum) in block.py;
-all are reached from here.
+(a product with its epilogue, norms on both sides of a residual sum, a mixture of
+experts for few tokens) in block.py; all are reached from here.
 """
 from __future__ import annotations
 
@@ -114,6 +114,17 @@ class ResidualNormGradArgs(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("dgate", "dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")]
 
 
+class MoeWeight(ctypes.Structure):
+    """atb_moe_weight"""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "scales", "zeros")]
+
+
+class Moe(ctypes.Structure):
+    """atb_moe: the operands of a mixture of experts."""
+    _fields_ = [("x", ctypes.c_void_p), ("router", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("ld_router", ctypes.c_int64), ("w_gate", MoeWeight), ("w_up", MoeWeight), ("w_down", MoeWeight)] + \
+               [(n, ctypes.c_int64) for n in ("M", "D", "F")] + [(n, ctypes.c_int) for n in ("experts", "top_k", "group", "act", "renormalize")] + [("workspace", ctypes.c_void_p)]
+
+
 # every symbol include/atb.h declares
 EXPORTS = [
     "atb_status_string", "atb_last_hip_error", "atb_gemm_create", "atb_gemm_create_fmt", "atb_gemm_run", "atb_gemm_destroy",
@@ -124,6 +135,7 @@ EXPORTS = [
     "atb_q4_quantize", "atb_q4_decode", "atb_q4_matvec", "atb_q4_gated",
     "atb_linear_workspace", "atb_linear_backward_workspace", "atb_linear_forward", "atb_linear_backward",
     "atb_residual_norm_workspace", "atb_residual_norm_forward", "atb_residual_norm_backward",
+    "atb_moe_workspace", "atb_moe_forward",
 ]
 
 
@@ -211,6 +223,10 @@ def lib() -> ctypes.CDLL:
     L.atb_residual_norm_forward.restype = L.atb_residual_norm_backward.restype = ci
     L.atb_residual_norm_forward.argtypes = [ctypes.POINTER(ResidualNorm), vp, i64, vp, i64, vp, vp]
     L.atb_residual_norm_backward.argtypes = [ctypes.POINTER(ResidualNorm), vp, vp, i64, vp, i64, ctypes.POINTER(ResidualNormGradArgs), vp, vp]
+    L.atb_moe_workspace.restype = ctypes.c_size_t
+    L.atb_moe_workspace.argtypes = [i64, i64, ci, ci]
+    L.atb_moe_forward.restype = ci
+    L.atb_moe_forward.argtypes = [ctypes.POINTER(Moe), vp, i64, vp, vp, vp]
     _lib = L
     return L
 
@@ -490,4 +506,4 @@ class Gemm:
 
 from .layers import (FeedForwardState, Q4Weight, feed_forward, feed_forward_backward, layer_norm, layer_norm_backward, q4_decode,  # noqa: E402
                      q4_feed_forward, q4_matvec, q4_quantize)
-from .block import Norm, ResidualNormGrads, linear, linear_backward, residual_norm, residual_norm_backward  # noqa: E402
+from .block import Norm, ResidualNormGrads, linear, linear_backward, moe_feed_forward, residual_norm, residual_norm_backward  # noqa: E402

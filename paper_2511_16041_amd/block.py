@@ -1,4 +1,5 @@
-"""What a transformer's block has around and in place of its feed-forward sublayer: a product with its epilogue, norms on both sides of a residual sum, and their gradients.
+"""What a transformer's block has around and in place of its feed-forward sublayer: a product with its epilogue, norms on both sides of a residual sum, and their gradients; and for few
+tokens a mixture of experts.
 
 As in layers.py: results and workspaces are made on the device of the first tensor, calls are launched asynchronously on `stream`, by default that device's current one, autograd does
 not follow them, tensors that are not what a kernel takes raise AssertionError and sizes that no kernel takes AtbError.  A matrix's rows may lie further apart than they are long."""
@@ -7,7 +8,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional, Tuple
 
 from . import _address
-from .layers import ACTIVATIONS, _activation, _call
+from .layers import ACTIVATIONS, Q4Weight, _activation, _call
 
 NO_ACTIVATION = len(ACTIVATIONS)       # ATB_ACT_NONE
 
@@ -72,3 +73,18 @@ def residual_norm_backward(dr, dh, x, z, stats, post: Optional[Norm] = None, gat
     """The gradients of residual_norm from those of r (by all but h; None: 0) and of h (None without a norm `pre`), each in its operand's type.  The same inputs give the same bits."""
     return ResidualNormGrads(*_call("residual_norm_backward", "atb_residual_norm_backward", stream, _address("atb_residual_norm_backward"), _address("atb_residual_norm_workspace"),
                                     dr, dh, x, z, stats, *_norm(post), gate, scale, *_norm(pre)))
+
+
+# ------------------------------------------------------------------ a mixture of experts for few tokens
+
+def _expert_weight(weight) -> Tuple:
+    return Q4Weight(*weight) if isinstance(weight, tuple) else (weight, None, None)
+
+
+def moe_feed_forward(x, router, w_gate, w_up, w_down, top_k: int = 2, act: str = "silu", renormalize: bool = True, routing: bool = False, stream=None):
+    """A mixture of E gated blocks for up to 64 tokens: x M x D, router E x D, both in bf16; every token goes through the top_k (16 at most) experts with the largest x router^T (of equal ones the
+    lowest), and y, M x D in bf16, is the sum of (act(x w_gate[e]^T) * (x w_up[e]^T)) w_down[e]^T times softmax(x router^T)[e] (renormalize: the softmax of the chosen ones alone).  w_gate and w_up: E x F x D in bf16,
+    w_down E x D x F, contiguous, D and F multiples of 8; or all three 4-bit weights (a Q4Weight or a tuple like one, as of q4_quantize) of E F, E F and E D outputs, one expert's after the other's.
+    The inner activations are rounded to bf16.  routing: returns (y, experts, weights), M x top_k in int32 and fp32, from the largest on."""
+    return _call("moe", "atb_moe_forward", stream, _address("atb_moe_forward"), _address("atb_moe_workspace"), x, router, *_expert_weight(w_gate), *_expert_weight(w_up), *_expert_weight(w_down),
+                 top_k, _activation(act), renormalize, routing)

@@ -11,6 +11,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <optional>
 
@@ -666,10 +667,79 @@ PyObject *residual_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n
     END_HANDLE_TH_ERRORS
 }
 
+// One of the three weights of all experts, of three arguments: E x rows x cols in bf16 and two None, or a 4-bit weight of E rows outputs.  group: what the first one has (-1: none yet)
+bool describe(atb_moe_weight &w, PyObject *const *args, int64_t E, int64_t rows, int64_t cols, int &group, const at::Device &on)
+{
+    const at::Tensor &t = THPVariable_Unpack(args[0]);
+    w = {t.data_ptr(), nullptr, nullptr};
+    if (args[1] == Py_None) {
+        if (group < 0) group = 0;
+        return group == 0 && args[2] == Py_None && t.device() == on && t.scalar_type() == at::kBFloat16 && t.dim() == 3 && t.size(0) == E && t.size(1) == rows && t.size(2) == cols && t.is_contiguous();
+    }
+    atb_q4 q;
+    if (!tensors(args + 1, 1) || !describe(q, args, on) || q.N != E * rows || q.K != cols || q.group == 0) return false;
+    if (group < 0) group = q.group;
+    w.scales = q.scales;
+    w.zeros = q.zeros;
+    return q.group == group;
+}
+
+// moe(entry, entry of the workspace's size, x, router, three weights of three arguments each, k, act, renormalize, routing) -> y, or (y, experts, weights)
+PyObject *moe(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 17) return PyErr_Format(PyExc_TypeError, "moe takes 17 arguments");
+    const auto call = reinterpret_cast<decltype(&atb_moe_forward)>(PyLong_AsVoidPtr(args[0]));
+    const auto room = reinterpret_cast<decltype(&atb_moe_workspace)>(PyLong_AsVoidPtr(args[1]));
+    const long k = PyLong_AsLong(args[13]), act = PyLong_AsLong(args[14]);
+    const int renormalize = PyObject_IsTrue(args[15]), routing = PyObject_IsTrue(args[16]);
+    if (PyErr_Occurred() || !tensors(args + 2, 3) || !tensors(args + 7, 1) || !tensors(args + 10, 1)) return nullptr;
+    for (int i = 4; i < 13; i += 3)
+        if (!tensors_or_none(args + i + 1, 2)) return nullptr;
+    HANDLE_TH_ERRORS
+    const at::Tensor &x = THPVariable_Unpack(args[2]), &router = THPVariable_Unpack(args[3]), &gate = THPVariable_Unpack(args[4]);
+    if (!x.is_cuda() || x.dim() != 2 || router.dim() != 2 || gate.dim() < 2) return refuse();
+    const at::Device on = x.device();
+    const int64_t M = x.size(0), D = x.size(1), E = router.size(0);
+    if (E < 1 || k < 1 || k > E || !is_rows(x, at::kBFloat16, M, D, on) || !is_rows(router, at::kBFloat16, E, D, on)) return refuse();
+    const int64_t F = args[5] == Py_None ? gate.size(1) : gate.size(0) / E;
+    atb_moe m = {};
+    int group = -1;
+    if (!describe(m.w_gate, args + 4, E, F, D, group, on) || !describe(m.w_up, args + 7, E, F, D, group, on) || !describe(m.w_down, args + 10, E, D, F, group, on)) return PyErr_Occurred() ? nullptr : refuse();
+    if ((args[6] == Py_None) != (args[9] == Py_None) || (args[6] == Py_None) != (args[12] == Py_None)) return refuse();        // zero points
+    m.x = x.data_ptr(); m.ldx = pitch(x);
+    m.router = router.data_ptr(); m.ld_router = pitch(router);
+    m.M = M;
+    m.D = D;
+    m.F = F;
+    m.experts = (int)std::min<int64_t>(E, INT32_MAX);
+    m.top_k = (int)std::min<int64_t>(k, INT32_MAX);
+    m.group = group;
+    m.act = static_cast<atb_activation>(act);
+    m.renormalize = renormalize;
+    const c10::DeviceGuard guard(on);
+    const at::Tensor y = make({M, D}, at::kBFloat16, on);
+    std::optional<at::Tensor> experts, weights, work;
+    if (routing) {
+        experts = make({M, k}, at::kInt, on);
+        weights = make({M, k}, at::kFloat, on);
+    }
+    const int64_t bytes = (int64_t)room(M, F, m.experts, m.top_k);       // 0: the call below says why
+    if (bytes > 0) work = make({bytes}, at::kByte, on);
+    m.workspace = data<void *>(work);
+    int st;
+    {
+        WithoutLock unlocked;
+        st = call(&m, y.data_ptr(), D, data<int32_t *>(experts), data<float *>(weights), current_stream());
+    }
+    if (st != 0) return PyLong_FromLong(st);
+    return routing ? tuple_of({y, experts, weights}) : THPVariable_Wrap(y);
+    END_HANDLE_TH_ERRORS
+}
+
 #define ATB_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ATB_METHOD(run), ATB_METHOD(quantize), ATB_METHOD(decode), ATB_METHOD(layer_norm), ATB_METHOD(layer_norm_backward), ATB_METHOD(ffn_forward),
                          ATB_METHOD(ffn_backward), ATB_METHOD(q4_matvec), ATB_METHOD(q4_ffn), ATB_METHOD(q4_quantize), ATB_METHOD(q4_decode),
-                         ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(residual_norm), ATB_METHOD(residual_norm_backward), {nullptr, nullptr, 0, nullptr}};
+                         ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(residual_norm), ATB_METHOD(residual_norm_backward), ATB_METHOD(moe), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_launch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

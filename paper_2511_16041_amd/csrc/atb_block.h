@@ -1,4 +1,5 @@
-// Internal declarations of what a transformer's block has around its feed-forward sublayer: a product with its epilogue, norms on both sides of a residual sum.
+// Internal declarations of what a transformer's block has around its feed-forward sublayer: a product with its epilogue, norms on both sides of a residual sum, a mixture of experts
+// for few tokens.
 // Not part of the public C ABI (see include/atb.h).
 #pragma once
 
@@ -87,5 +88,55 @@ static inline ResidualRoom residual_room(int64_t M, int64_t D, int64_t groups)
     r.total = r.sums + r.totals + r.rows;
     return r;
 }
+
+// ---- a mixture of experts for few tokens (atb_moe.hip, atb_moe_q4.hip)
+
+constexpr int kMoeTokens = 64, kMoeExperts = 256, kMoeTopK = 16, kMoePlaces = kMoeTokens * kMoeTopK;
+constexpr int kMoeSegments = kMoeExperts + kMoePlaces / 16;
+
+// What the tokens chose, in device memory.  A place is a token's choice; places are sorted by expert, of one expert by token.  A segment is a run of places of one expert that a workgroup takes at a
+// time: at most 16 or 32.
+struct MoePlan {
+    int segments;
+    int expert[kMoeSegments], first[kMoeSegments], rows[kMoeSegments];
+    int token[kMoePlaces];
+    float weight[kMoePlaces];
+};
+
+struct MoeParams {
+    const uint16_t *x, *router;  // bf16, M x D and E x D
+    int64_t ldx, ld_router;
+    StreamWeight gate, up, down; // of all experts, one after the other's: E F x D, E F x D, E D x F, contiguous
+    uint16_t *y;                 // bf16 M x D
+    int64_t ldy;
+    int *experts;                // M x k, or null
+    float *weights;              // M x k, or null
+    int M, D, F, E, k;
+    int group;                   // 0: bf16 weights
+    int act, renormalize;
+    // workspace
+    double *logits;              // M x E
+    MoePlan *plan;
+    uint16_t *h;                 // M k x F: the inner activations, by place
+};
+hipError_t launch_moe(const MoeParams &p, hipStream_t stream);
+hipError_t launch_moe_q4(const MoeParams &p, hipStream_t stream);        // the products, with weights in 4 bits; launch_moe calls it
+
+// The workspace, in bytes
+struct MoeRoom { int64_t logits, plan, h, total; };
+static inline MoeRoom moe_room(int64_t M, int64_t F, int64_t E, int64_t k)
+{
+    MoeRoom r;
+    r.logits = round_up(M * E * (int64_t)sizeof(double), 256);
+    r.plan = round_up((int64_t)sizeof(MoePlan), 256);
+    r.h = round_up(M * k * F * 2, 256);
+    r.total = r.logits + r.plan + r.h;
+    return r;
+}
+
+// Rows of x that a workgroup of the products takes: 32 where an expert gets more than 12 on average, so that few get more than 16 and read their weights twice.
+static inline int moe_rows(int64_t M, int64_t E, int64_t k) { return M > 16 && M * k > 12 * E ? 32 : 16; }
+// The most segments that the choices can have
+static inline int moe_segments(int64_t M, int64_t E, int64_t k, int rows) { return (int)(std::min(E, M * k) + M * k / rows); }
 
 }  // namespace atb

@@ -1,0 +1,262 @@
+// A mixture of experts for few tokens: l = x R^T, the k experts with the largest l and their shares of softmax(l), y = sum over them of share * Wd (act(Wg x) o (Wu x)).
+// Floor: the bytes of the chosen experts' weights.
+//
+// Four launches.  (1) The router's products in fp64, a wave for one expert and a few tokens: which experts are taken hangs on the order of the l, and in fp32 two that lie close could change places.
+// (2) One workgroup: every token's experts by counting how many are ahead of each (of equal ones the lower index is), their shares, and the plan, the choices sorted by expert.  (3) Gate and up
+// products of every expert and its tokens, as the kernel for few rows does them, with the rows of x gathered by the plan; h by place.  (4) The down product: a workgroup has 16 columns of y and
+// all experts in turn; its waves take the panels of all of them as one long reduction, and at an expert's end each adds its sums, times the tokens' shares, to its own part of y in LDS.  So every expert's weights
+// are read once, those of no token not at all, the sum over a token's experts is in fp32, in the order of the experts, without atomics, and no token's values meet another's.
+#include "atb_moe.h"
+#include "atb_stream_rows.h"
+
+namespace atb {
+namespace {
+
+// ---- the router
+
+// A wave for one expert and T tokens, four waves to a workgroup
+template <int T>
+__global__ void __launch_bounds__(256) moe_logits_kernel(const MoeParams p)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.x, m0 = (blockIdx.y * 4 + wave) * T;
+    if (m0 >= p.M) return;
+    const __bf16 *r = reinterpret_cast<const __bf16 *>(p.router) + e * p.ld_router, *x[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) x[t] = reinterpret_cast<const __bf16 *>(p.x) + min(m0 + t, p.M - 1) * p.ldx;
+    double sum[T] = {};
+#pragma unroll 2
+    for (int at = lane * 8; at < p.D; at += 512) {                 // D is a multiple of 8
+        const bf16x8 w = *reinterpret_cast<const bf16x8 *>(r + at);
+        bf16x8 v[T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) v[t] = *reinterpret_cast<const bf16x8 *>(x[t] + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int t = 0; t < T; ++t) sum[t] = fma((double)(float)w[i], (double)(float)v[t][i], sum[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum[t] += __shfl_xor(sum[t], d);
+        if (lane == 0 && m0 + t < p.M) p.logits[(int64_t)(m0 + t) * p.E + e] = sum[t];
+    }
+}
+
+// Every token's choice and the plan.  `rows`: of a segment at most.
+__global__ void __launch_bounds__(1024) moe_plan_kernel(const MoeParams p, int rows)
+{
+    __shared__ double logits[16][kMoeExperts];
+    __shared__ unsigned long long tokens[kMoeExperts];             // of an expert, a bit each
+    __shared__ int first[kMoeExperts + 1], segment[kMoeExperts + 1];
+    __shared__ int chosen[kMoeTokens][kMoeTopK];
+    __shared__ float share[kMoeTokens][kMoeTopK];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x < kMoeExperts) tokens[threadIdx.x] = 0;
+    __syncthreads();
+    for (int t0 = 0; t0 < p.M; t0 += 16) {                         // a wave takes a token
+        const int t = t0 + wave;
+        constexpr int PER = kMoeExperts / 64;
+        double mine[PER], key[PER];
+        if (t < p.M) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = 64 * i + lane;
+                mine[i] = e < p.E ? p.logits[(int64_t)t * p.E + e] : -INFINITY;
+                key[i] = mine[i] == mine[i] ? mine[i] : -INFINITY;             // NaN is behind all numbers: the ranks are a permutation whatever x holds
+                logits[wave][e] = key[i];
+            }
+        }
+        __syncthreads();
+        if (t < p.M) {
+            int rank[PER] = {};
+            for (int j = 0; j < p.E; ++j) {
+                const double other = logits[wave][j];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) rank[i] += other > key[i] || (other == key[i] && j < 64 * i + lane);
+            }
+            // exp(l - the largest l), summed over all experts or over the chosen ones; a NaN or an infinity among the summands gives what the formula gives
+            double top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) top = fmax(top, key[i]);
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) top = fmax(top, __shfl_xor(top, d));
+            float part[PER], sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const bool live = 64 * i + lane < p.E, taken = live && rank[i] < p.k;
+                part[i] = live ? expf((float)(mine[i] - top)) : 0.0f;
+                if (p.renormalize ? taken : live) sum += part[i];
+            }
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = 64 * i + lane;
+                if (e >= p.E || rank[i] >= p.k) continue;
+                const float s = part[i] / sum;
+                chosen[t][rank[i]] = e;
+                share[t][rank[i]] = s;
+                atomicOr(&tokens[e], 1ull << t);                   // (bits: no order)
+                if (p.experts) p.experts[t * p.k + rank[i]] = e;
+                if (p.weights) p.weights[t * p.k + rank[i]] = s;
+            }
+        }
+        __syncthreads();
+    }
+    // first place and segment of every expert, by a sum over the experts before it
+    if (wave == 0) {
+        int places = 0, segments = 0;
+        for (int e0 = 0; e0 < p.E; e0 += 64) {
+            const int e = e0 + lane, n = e < p.E ? __popcll(tokens[e]) : 0, s = (n + rows - 1) / rows;
+            int at = n, seg = s;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int a = __shfl_up(at, d), b = __shfl_up(seg, d);
+                if (lane >= d) { at += a; seg += b; }
+            }
+            if (e < p.E) {
+                first[e] = places + at - n;
+                segment[e] = segments + seg - s;
+            }
+            places += __shfl(at, 63);
+            segments += __shfl(seg, 63);
+        }
+        if (lane == 0) p.plan->segments = segments;
+    }
+    __syncthreads();
+    if (threadIdx.x < p.E) {
+        const int e = threadIdx.x, n = __popcll(tokens[e]);
+        for (int i = 0; i * rows < n; ++i) {
+            p.plan->expert[segment[e] + i] = e;
+            p.plan->first[segment[e] + i] = first[e] + i * rows;
+            p.plan->rows[segment[e] + i] = min(rows, n - i * rows);
+        }
+    }
+    for (int o = threadIdx.x; o < p.M * p.k; o += 1024) {
+        const int t = o / p.k, c = o - t * p.k, e = chosen[t][c], place = first[e] + __popcll(tokens[e] & ((1ull << t) - 1));
+        p.plan->token[place] = t;
+        p.plan->weight[place] = share[t][c];
+    }
+}
+
+// ---- the products
+
+template <class S>
+__global__ void __launch_bounds__(S::W * 64) moe_gated_kernel(const MoeParams p)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
+    if ((int)blockIdx.y >= p.plan->segments) return;
+    const MoeSegment seg = moe_segment(p.plan, blockIdx.y);
+    const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.F - n0, 16 * S::COLS);
+    const int64_t at = ((int64_t)seg.expert * p.F + n0) * p.D;
+    const StreamView view = {p.x, p.ldx, p.M, seg.rows, {static_cast<const uint16_t *>(p.gate.w) + at, static_cast<const uint16_t *>(p.up.w) + at}, {p.D, p.D}, cols, p.D};
+    const int *tokens = p.plan->token + seg.first;
+    Stream<S> s(view, (unsigned)reinterpret_cast<uintptr_t>(lds), [&](int row) { return tokens[row]; });
+    s.run();
+    finish_rows<S::MB, S::NB, S::W, true>(moe_inner(p, seg), s.acc, reinterpret_cast<float *>(lds), 0, n0, cols);
+}
+
+// MOST: tokens that there is room for
+template <class S, int MOST>
+__global__ void __launch_bounds__(S::W * 64) moe_down_kernel(const MoeParams p)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
+    __shared__ float totals[S::W * MOST * 16 * S::NB];
+    const MoePlan *plan = p.plan;
+    const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.D - n0, 16 * S::COLS);
+    auto view_of = [&](const MoeSegment &seg) {
+        return StreamView{p.h + (int64_t)seg.first * p.F, p.F, seg.rows, seg.rows, {static_cast<const uint16_t *>(p.down.w) + ((int64_t)seg.expert * p.D + n0) * p.F, nullptr}, {p.F, 0}, cols, p.F};
+    };
+    auto row_of = [](int row) { return row; };
+    const int panels = (p.F + S::K - 1) / S::K, segments = __builtin_amdgcn_readfirstlane(plan->segments);
+    Stream<S> s(view_of(moe_segment(plan, 0)), (unsigned)reinterpret_cast<uintptr_t>(lds), row_of);
+    float *mine = totals + s.wave * p.M * 16 * S::NB;
+    for (int i = s.lane; i < p.M * 16 * S::NB; i += 64) mine[i] = 0.0f;
+    // this wave's panels: every W-th of all segments'; `to`: the next one that is asked for
+    struct Place { int segment, panel; };
+    auto settle = [&](Place &at) {
+        while (at.panel >= panels && at.segment < segments) {
+            at.panel -= panels;
+            ++at.segment;
+        }
+    };
+    Place at = {0, s.wave}, to = at;
+    settle(at);
+    settle(to);
+    int opened = 0;
+    auto request = [&](int slot) {
+        if (to.segment != opened) {
+            opened = to.segment;
+            const MoeSegment seg = moe_segment(plan, opened);
+            s.open_rows(view_of(seg), row_of);
+            s.open_weight(view_of(seg), 0);
+        }
+        s.request(to.panel, slot);
+        to.panel += S::W;
+        settle(to);
+    };
+    int summed = at.segment, slot = 0;
+    bool ahead = false;                                            // whether the panel behind the next one has been asked for
+    if (to.segment < segments) {
+        request(0);
+        if (to.segment < segments) {
+            request(1);
+            ahead = true;
+        }
+    }
+    while (at.segment < segments) {
+        if (at.segment != summed) {
+            moe_add(plan, moe_segment(plan, summed), s.acc, mine);
+            s.clear();
+            summed = at.segment;
+        }
+        // (what moe_add reads of the plan is waited for by the compiler, and requests are in order: the wait below is never too short)
+        if (ahead) Stream<S>::template wait<S::REQS>();
+        else Stream<S>::template wait<0>();
+        s.multiply(slot);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the buffer is in registers
+        ahead = to.segment < segments;
+        if (ahead) request(slot);
+        slot ^= 1;
+        at.panel += S::W;
+        settle(at);
+    }
+    if (summed < segments) moe_add(plan, moe_segment(plan, summed), s.acc, mine);
+    __syncthreads();
+    moe_finish<S::NB, S::W>(p, totals, n0, cols);
+}
+
+template <int MB, int XQ, int MOST>
+hipError_t launch_products(const MoeParams &p, hipStream_t stream)
+{
+    typedef StreamShape<MB, 2, XQ, 4, true> Gated;
+    typedef StreamShape<MB, 1, XQ, 8, false> Down;
+    const int segments = moe_segments(p.M, p.E, p.k, 16 * MB);
+    hipLaunchKernelGGL((moe_gated_kernel<Gated>), dim3((unsigned)((p.F + 15) / 16), (unsigned)segments), dim3(Gated::W * 64), 0, stream, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((moe_down_kernel<Down, MOST>), dim3((unsigned)((p.D + 15) / 16)), dim3(Down::W * 64), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_moe(const MoeParams &p, hipStream_t stream)
+{
+    if (p.M == 0) return hipSuccess;
+    if (p.M <= 4) hipLaunchKernelGGL(moe_logits_kernel<1>, dim3((unsigned)p.E), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(moe_logits_kernel<2>, dim3((unsigned)p.E, (unsigned)((p.M + 7) / 8)), dim3(256), 0, stream, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int rows = p.group ? 16 : moe_rows(p.M, p.E, p.k);
+    hipLaunchKernelGGL(moe_plan_kernel, dim3(1), dim3(1024), 0, stream, p, rows);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (p.group) return launch_moe_q4(p, stream);
+    if (rows == 32) return launch_products<2, 4, kMoeTokens>(p, stream);
+    if (p.M <= 8) return launch_products<1, 1, 8>(p, stream);
+    return p.M <= 16 ? launch_products<1, 2, 16>(p, stream) : launch_products<1, 2, kMoeTokens>(p, stream);
+}
+
+}  // namespace atb

@@ -180,3 +180,59 @@ def test_residual_norm_gradients_against_differences(post, pre, groups):
         slope = _slope(moved, (here,), 0, v)
         grad = float((want[name][0].reshape(here.shape) * v).sum())
         assert abs(slope - grad) < 1e-6 * (1 + abs(grad)), name
+
+
+# ------------------------------------------------------------------ a mixture of experts for few tokens
+
+def test_moe_refuses():
+    L = atb.lib()
+    keep, a = aligned_address()
+    bf16, q4, z4 = atb.MoeWeight(a, None, None), atb.MoeWeight(a, a, None), atb.MoeWeight(a, a, a)
+    good = dict(x=a, router=a, ldx=64, ld_router=64, w_gate=bf16, w_up=bf16, w_down=bf16, M=2, D=64, F=64, experts=4, top_k=2, group=0, act=0, renormalize=1, workspace=a)
+
+    def forward(y=a, ldy=64, chosen=a, p=a, **kw):
+        return L.atb_moe_forward(ctypes.byref(atb.Moe(**{**good, **kw})), y, ldy, chosen, p, None)
+    in_4 = dict(w_gate=q4, w_up=q4, w_down=q4)
+    for bad in [dict(x=None), dict(router=None), dict(x=a + 2), dict(router=a + 8), dict(ldx=56), dict(ldx=68), dict(ld_router=63), dict(ld_router=2 ** 22), dict(M=-1), dict(M=65), dict(D=0), dict(D=60), dict(F=4),
+                dict(D=2 ** 22, ldx=2 ** 22, ld_router=2 ** 22), dict(F=2 ** 22), dict(experts=0), dict(experts=257), dict(top_k=0), dict(top_k=5), dict(experts=40, top_k=17), dict(group=16), dict(group=-32), dict(act=3),
+                dict(act=-1), dict(workspace=None), dict(workspace=a + 8), dict(y=None), dict(y=a + 1), dict(ldy=63), dict(chosen=a + 2), dict(p=a + 2), dict(w_gate=atb.MoeWeight(None, None, None)),
+                dict(w_up=atb.MoeWeight(a + 8, None, None)), dict(w_down=atb.MoeWeight(None, a, a)), dict(group=32), dict(group=32, w_gate=q4, w_up=q4), dict(group=32, w_gate=z4, w_up=q4, w_down=q4),
+                dict(group=32, w_gate=q4, w_up=q4, w_down=z4), dict(group=128, **in_4), dict(group=64, F=96, **in_4), dict(group=32, w_gate=atb.MoeWeight(a, a + 1, None), w_up=q4, w_down=q4)]:
+        assert forward(**bad) == INVALID, bad
+    assert L.atb_moe_forward(None, a, 64, a, a, None) == INVALID
+    assert forward(M=0, x=None, y=None, workspace=None) == 0
+    if not __import__("torch").cuda.is_available():
+        assert forward() == forward(chosen=None, p=None) == forward(group=32, **in_4) == forward(group=64, w_gate=z4, w_up=z4, w_down=z4) == forward(M=40, experts=2) == 5
+
+
+def test_workspace_of_a_mixture_of_experts():
+    L = atb.lib()
+    for M, F, E, k in ((0, 8, 1, 1), (1, 8, 1, 1), (64, 14336, 256, 16)):
+        size = L.atb_moe_workspace(M, F, E, k)
+        assert size % 256 == 0 and size >= 8 * M * E + 2 * M * k * F + 8 * 1024
+    for bad in ((-1, 8, 4, 2), (65, 8, 4, 2), (1, 12, 4, 2), (1, 0, 4, 2), (1, 2 ** 22, 4, 2), (1, 8, 0, 1), (1, 8, 257, 1), (1, 8, 4, 0), (1, 8, 4, 5), (1, 8, 40, 17)):
+        assert L.atb_moe_workspace(*bad) == 0
+
+
+def test_moe_refuses_tensors_that_a_kernel_would_read_or_store_past():
+    import torch
+    bf, f32, u8 = torch.bfloat16, torch.float32, torch.uint8
+    x, r = _on_device((3, 64), bf), _on_device((4, 64), bf)
+    up, down = _on_device((4, 128, 64), bf), _on_device((4, 64, 128), bf)
+    for args in [(torch.zeros(3, 64, dtype=bf), r, up, up, down), (_on_device((3, 64), f32), r, up, up, down), (x, _on_device((4, 56), bf), up, up, down), (x, _on_device((4, 64), f32), up, up, down),
+                 (x, _on_device((5, 64), bf), up, up, down), (x, r, up, down, down), (x, r, up, up, up), (x, r, up, _on_device((4, 120, 64), bf), down), (x, r, _on_device((4, 128, 64), f32), up, down),
+                 (x, r, _on_device((4, 128, 64), bf, (16384, 128, 1)), up, down), (x, r, up, up, _on_device((4, 64, 128), bf, (8192, 1, 64))), (x, r, up, up, torch.zeros(4, 64, 128, dtype=bf)),
+                 (x, r, up, up, down, 0), (x, r, up, up, down, 5), (x, r, _on_device((512, 64), bf), up, down)]:
+        with pytest.raises(AssertionError):
+            atb.moe_feed_forward(*args)
+
+    def q4(rows, cols, group=32, zeros=False):
+        return atb.Q4Weight(_on_device((rows, cols // 2), u8), _on_device((rows, cols // group), bf), _on_device((rows, cols // group), u8) if zeros else None)
+    good = (x, r, q4(512, 64), q4(512, 64), q4(256, 128))
+    for at, w in [(2, q4(511, 64)), (2, q4(512, 128)), (3, q4(256, 64)), (4, q4(512, 64)), (4, q4(256, 128, 64)), (3, q4(512, 64, 32, True)), (2, up), (4, down), (2, q4(512, 64)._replace(scales=_on_device((512, 2), f32)))]:
+        with pytest.raises(AssertionError):
+            atb.moe_feed_forward(*good[:at], w, *good[at + 1:])
+    with pytest.raises(ValueError, match="silu"):
+        atb.moe_feed_forward(x, r, up, up, down, 2, "swish")
+    with pytest.raises(TypeError):
+        atb.moe_feed_forward(x, r, up, None, down)
