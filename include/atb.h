@@ -398,8 +398,8 @@ typedef struct atb_moe {
     void *workspace;                            /* DEVICE, 16-byte aligned, of the bytes below for the call */
 } atb_moe;
 
-/* Bytes of the workspace: the l, the plan of the call, the inner activations; 0 on invalid arguments. */
-size_t atb_moe_workspace(int64_t M, int64_t F, int experts, int top_k);
+/* Bytes of the workspace: the l, the plan of the call, the inner activations, partial sums; 0 on invalid arguments. */
+size_t atb_moe_workspace(int64_t M, int64_t D, int64_t F, int experts, int top_k, int group);
 
 /* y: DEVICE, M x D bf16 (pitch ldy), at any element.  chosen, p: DEVICE, M x k int32 and fp32, or NULL: the experts of every token from its largest l on, and their p.  Async on hip_stream. */
 atb_status atb_moe_forward(const atb_moe *m, void *y, int64_t ldy, int32_t *chosen, float *p, void *hip_stream);

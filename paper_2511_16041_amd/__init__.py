@@ -224,7 +224,7 @@ def lib() -> ctypes.CDLL:
     L.atb_residual_norm_forward.argtypes = [ctypes.POINTER(ResidualNorm), vp, i64, vp, i64, vp, vp]
     L.atb_residual_norm_backward.argtypes = [ctypes.POINTER(ResidualNorm), vp, vp, i64, vp, i64, ctypes.POINTER(ResidualNormGradArgs), vp, vp]
     L.atb_moe_workspace.restype = ctypes.c_size_t
-    L.atb_moe_workspace.argtypes = [i64, i64, ci, ci]
+    L.atb_moe_workspace.argtypes = [i64, i64, i64, ci, ci, ci]
     L.atb_moe_forward.restype = ci
     L.atb_moe_forward.argtypes = [ctypes.POINTER(Moe), vp, i64, vp, vp, vp]
     _lib = L

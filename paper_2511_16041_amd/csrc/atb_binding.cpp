@@ -723,7 +723,7 @@ PyObject *moe(PyObject *, PyObject *const *args, Py_ssize_t n)
         experts = make({M, k}, at::kInt, on);
         weights = make({M, k}, at::kFloat, on);
     }
-    const int64_t bytes = (int64_t)room(M, F, m.experts, m.top_k);       // 0: the call below says why
+    const int64_t bytes = (int64_t)room(M, D, F, m.experts, m.top_k, group);       // 0: the call below says why
     if (bytes > 0) work = make({bytes}, at::kByte, on);
     m.workspace = data<void *>(work);
     int st;

@@ -118,25 +118,40 @@ struct MoeParams {
     double *logits;              // M x E
     MoePlan *plan;
     uint16_t *h;                 // M k x F: the inner activations, by place
+    int shares;                  // of the down product's reduction; 1: no partial sums
+    float *partial;              // shares x M x D
 };
 hipError_t launch_moe(const MoeParams &p, hipStream_t stream);
 hipError_t launch_moe_q4(const MoeParams &p, hipStream_t stream);        // the products, with weights in 4 bits; launch_moe calls it
-
-// The workspace, in bytes
-struct MoeRoom { int64_t logits, plan, h, total; };
-static inline MoeRoom moe_room(int64_t M, int64_t F, int64_t E, int64_t k)
-{
-    MoeRoom r;
-    r.logits = round_up(M * E * (int64_t)sizeof(double), 256);
-    r.plan = round_up((int64_t)sizeof(MoePlan), 256);
-    r.h = round_up(M * k * F * 2, 256);
-    r.total = r.logits + r.plan + r.h;
-    return r;
-}
 
 // Rows of x that a workgroup of the products takes: 32 where an expert gets more than 12 on average, so that few get more than 16 and read their weights twice.
 static inline int moe_rows(int64_t M, int64_t E, int64_t k) { return M > 16 && M * k > 12 * E ? 32 : 16; }
 // The most segments that the choices can have
 static inline int moe_segments(int64_t M, int64_t E, int64_t k, int rows) { return (int)(std::min(E, M * k) + M * k / rows); }
+
+// Shares of the down product's reduction, the chosen experts' panels of 64 (4 bits: 256) one after the other, which a third kernel adds: as many as make 512 workgroups of 16 columns (4 bits: 32) where there
+// would be fewer than CUs, and a panel or more for each of their 8 waves (4 bits, whose waves take longer to begin: one and a half).  us, 1 / 2 / 3 / 4 / 6 shares without joining them, which takes 2.5 to 4.8: 21
+// tokens over 60 experts of 2056 x 1416 143 / 108 / 79 / 91 / 79, one token through 2 experts of 4096 x 14336 (256 workgroups) 44 / 44 / 43 / 43 / 43; 4 bits, 4 / 8 shares: one token through 8 of 2048 x 1536 7.5 / 9.7,
+// 2 / 4 / 8: 32 tokens over 8 of 4096 x 14336 81 / 76 / 77.
+static inline int moe_shares(int64_t M, int64_t D, int64_t F, int64_t E, int64_t k, int group)
+{
+    const int64_t blocks = group ? (D + 31) / 32 : (D + 15) / 16, experts = std::min(E, M * k);
+    if (blocks >= 256) return 1;
+    return (int)std::max<int64_t>(1, std::min(512 / blocks, group ? experts * ((F + 255) / 256) / 12 : experts * ((F + 63) / 64) / 8));
+}
+
+// The workspace, in bytes
+struct MoeRoom { int64_t logits, plan, h, partial, total; };
+static inline MoeRoom moe_room(int64_t M, int64_t D, int64_t F, int64_t E, int64_t k, int group)
+{
+    MoeRoom r;
+    const int64_t shares = M > 0 ? moe_shares(M, D, F, E, k, group) : 1;
+    r.logits = round_up(M * E * (int64_t)sizeof(double), 256);
+    r.plan = round_up((int64_t)sizeof(MoePlan), 256);
+    r.h = round_up(M * k * F * 2, 256);
+    r.partial = shares > 1 ? round_up(shares * M * D * (int64_t)sizeof(float), 256) : 0;
+    r.total = r.logits + r.plan + r.h + r.partial;
+    return r;
+}
 
 }  // namespace atb

@@ -260,6 +260,7 @@ bool moe_counts(int64_t M, int experts, int top_k)
 {
     return M >= 0 && M <= atb::kMoeTokens && experts >= 1 && experts <= atb::kMoeExperts && top_k >= 1 && top_k <= atb::kMoeTopK && top_k <= experts;
 }
+bool moe_group(int group) { return group == 0 || group == 32 || group == 64 || group == 128; }
 bool moe_length(int64_t n, int group) { return n >= 8 && n < kMaxPitch && n % (group ? group : 8) == 0; }
 bool is_moe_weight(const atb_moe_weight &w, int group, bool zeros)
 {
@@ -274,23 +275,22 @@ atb::StreamWeight moe_weight(const atb_moe_weight &w, int group)
 
 }  // namespace
 
-extern "C" size_t atb_moe_workspace(int64_t M, int64_t F, int experts, int top_k)
+extern "C" size_t atb_moe_workspace(int64_t M, int64_t D, int64_t F, int experts, int top_k, int group)
 {
-    if (!moe_counts(M, experts, top_k) || !moe_length(F, 0)) return 0;
-    return (size_t)atb::moe_room(M, F, experts, top_k).total;
+    if (!moe_counts(M, experts, top_k) || !moe_group(group) || !moe_length(D, group) || !moe_length(F, group)) return 0;
+    return (size_t)atb::moe_room(M, D, F, experts, top_k, group).total;
 }
 
 extern "C" atb_status atb_moe_forward(const atb_moe *m, void *y, int64_t ldy, int32_t *chosen, float *p, void *hip_stream)
 {
     if (!m || !moe_counts(m->M, m->experts, m->top_k) || !is_activation(m->act)) return ATB_ERR_INVALID_ARG;
-    if (m->group != 0 && m->group != 32 && m->group != 64 && m->group != 128) return ATB_ERR_INVALID_ARG;
-    if (!moe_length(m->D, m->group) || !moe_length(m->F, m->group)) return ATB_ERR_INVALID_ARG;
+    if (!moe_group(m->group) || !moe_length(m->D, m->group) || !moe_length(m->F, m->group)) return ATB_ERR_INVALID_ARG;
     const bool zeros = m->w_gate.zeros != nullptr;
     if (!is_moe_weight(m->w_gate, m->group, zeros) || !is_moe_weight(m->w_up, m->group, zeros) || !is_moe_weight(m->w_down, m->group, zeros)) return ATB_ERR_INVALID_ARG;
     if (!is_matrix(m->router, m->D, m->ld_router) || !aligned(chosen, 4) || !aligned(p, 4)) return ATB_ERR_INVALID_ARG;
     if (m->M == 0) return ATB_OK;
     if (!is_matrix(m->x, m->D, m->ldx) || !is_rows(y, m->D, ldy, 2) || !m->workspace || !aligned(m->workspace, 16)) return ATB_ERR_INVALID_ARG;
-    const atb::MoeRoom room = atb::moe_room(m->M, m->F, m->experts, m->top_k);
+    const atb::MoeRoom room = atb::moe_room(m->M, m->D, m->F, m->experts, m->top_k, m->group);
     char *work = static_cast<char *>(m->workspace);
     atb::MoeParams q = {};
     q.x = u16(m->x); q.ldx = m->ldx;
@@ -308,5 +308,7 @@ extern "C" atb_status atb_moe_forward(const atb_moe *m, void *y, int64_t ldy, in
     q.logits = reinterpret_cast<double *>(work);
     q.plan = reinterpret_cast<atb::MoePlan *>(work + room.logits);
     q.h = reinterpret_cast<uint16_t *>(work + room.logits + room.plan);
+    q.shares = atb::moe_shares(m->M, m->D, m->F, m->experts, m->top_k, m->group);
+    q.partial = reinterpret_cast<float *>(work + room.logits + room.plan + room.h);
     return hip_status(atb::launch_moe(q, static_cast<hipStream_t>(hip_stream)));
 }

@@ -42,17 +42,35 @@ ATB_DEV void moe_add(const MoePlan *plan, const MoeSegment &s, const floatx4 (&a
         }
 }
 
-// The waves' parts of y, added in wave order: `cols` columns from n0 on.
+// A wave's way through its share of the down product: every W-th panel of the segments', one after the other
+template <int W>
+struct MoePlace {
+    int panels, at, segment, panel;            // of a segment; of all; the segment's
+    ATB_DEV MoePlace(int panels_, int first) : panels(panels_), at(first), segment(first / panels_), panel(first - segment * panels_) {}
+    ATB_DEV void next()
+    {
+        at += W;
+        panel += W;
+        while (panel >= panels) {
+            panel -= panels;
+            ++segment;
+        }
+    }
+};
+
+// The waves' parts of y, added in wave order: `cols` columns from n0 on; of a reduction in shares the share's part, in fp32.
 template <int NB, int W>
 ATB_DEV void moe_finish(const MoeParams &p, const float *totals, int n0, int cols)
 {
+    __syncthreads();
     for (int o = threadIdx.x; o < p.M * 16 * NB; o += W * 64) {
         const int token = o / (16 * NB), col = o % (16 * NB);
         if (col >= cols) continue;
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; ++w) v += totals[w * p.M * 16 * NB + o];
-        reinterpret_cast<__bf16 *>(p.y)[token * p.ldy + n0 + col] = (__bf16)v;
+        if (p.shares > 1) p.partial[((int64_t)blockIdx.y * p.M + token) * p.D + n0 + col] = v;
+        else reinterpret_cast<__bf16 *>(p.y)[token * p.ldy + n0 + col] = (__bf16)v;
     }
 }
 

@@ -14,18 +14,18 @@ namespace {
 
 // ---- the router
 
-// A wave for one expert and T tokens, four waves to a workgroup
+// A workgroup for one expert and T tokens, a quarter of every 2048 elements to each wave
 template <int T>
 __global__ void __launch_bounds__(256) moe_logits_kernel(const MoeParams p)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.x, m0 = (blockIdx.y * 4 + wave) * T;
-    if (m0 >= p.M) return;
+    __shared__ double parts[4][T];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.x, m0 = blockIdx.y * T;
     const __bf16 *r = reinterpret_cast<const __bf16 *>(p.router) + e * p.ld_router, *x[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) x[t] = reinterpret_cast<const __bf16 *>(p.x) + min(m0 + t, p.M - 1) * p.ldx;
     double sum[T] = {};
 #pragma unroll 2
-    for (int at = lane * 8; at < p.D; at += 512) {                 // D is a multiple of 8
+    for (int at = threadIdx.x * 8; at < p.D; at += 2048) {         // D is a multiple of 8
         const bf16x8 w = *reinterpret_cast<const bf16x8 *>(r + at);
         bf16x8 v[T];
 #pragma unroll
@@ -39,14 +39,24 @@ __global__ void __launch_bounds__(256) moe_logits_kernel(const MoeParams p)
     for (int t = 0; t < T; ++t) {
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) sum[t] += __shfl_xor(sum[t], d);
-        if (lane == 0 && m0 + t < p.M) p.logits[(int64_t)(m0 + t) * p.E + e] = sum[t];
+        if (lane == 0) parts[wave][t] = sum[t];
     }
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t < T && m0 + t < p.M) p.logits[(int64_t)(m0 + t) * p.E + e] = parts[0][t] + parts[1][t] + parts[2][t] + parts[3][t];
 }
 
-// Every token's choice and the plan.  `rows`: of a segment at most.
+// Lane `from`'s value, the same for all
+ATB_DEV double of_lane(double v, int from)
+{
+    const unsigned lo = __builtin_amdgcn_readlane(__double2loint(v), from), hi = __builtin_amdgcn_readlane(__double2hiint(v), from);
+    return __hiloint2double((int)hi, (int)lo);
+}
+
+// Every token's choice and the plan.  PER: experts of a lane.  `rows`: of a segment at most.
+template <int PER>
 __global__ void __launch_bounds__(1024) moe_plan_kernel(const MoeParams p, int rows)
 {
-    __shared__ double logits[16][kMoeExperts];
     __shared__ unsigned long long tokens[kMoeExperts];             // of an expert, a bit each
     __shared__ int first[kMoeExperts + 1], segment[kMoeExperts + 1];
     __shared__ int chosen[kMoeTokens][kMoeTopK];
@@ -54,56 +64,59 @@ __global__ void __launch_bounds__(1024) moe_plan_kernel(const MoeParams p, int r
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (threadIdx.x < kMoeExperts) tokens[threadIdx.x] = 0;
     __syncthreads();
-    for (int t0 = 0; t0 < p.M; t0 += 16) {                         // a wave takes a token
-        const int t = t0 + wave;
-        constexpr int PER = kMoeExperts / 64;
+    // a wave takes a token, and the next one's products are on their way
+    double next[PER];
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) next[i] = t < p.M && 64 * i + lane < p.E ? p.logits[(int64_t)t * p.E + 64 * i + lane] : -INFINITY;
+    };
+    fetch(wave);
+    for (int t = wave; t < p.M; t += 16) {
         double mine[PER], key[PER];
-        if (t < p.M) {
+        int rank[PER] = {};
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = 64 * i + lane;
-                mine[i] = e < p.E ? p.logits[(int64_t)t * p.E + e] : -INFINITY;
-                key[i] = mine[i] == mine[i] ? mine[i] : -INFINITY;             // NaN is behind all numbers: the ranks are a permutation whatever x holds
-                logits[wave][e] = key[i];
+        for (int i = 0; i < PER; ++i) {
+            mine[i] = next[i];
+            key[i] = mine[i] == mine[i] ? mine[i] : -INFINITY;                 // NaN is behind all numbers: the ranks are a permutation whatever x holds
+        }
+        fetch(t + 16);
+#pragma unroll
+        for (int o = 0; o < PER; ++o) {
+            const int others = min(64, p.E - 64 * o);
+            for (int j = 0; j < others; ++j) {
+                const double other = of_lane(key[o], j);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) rank[i] += other > key[i] || (other == key[i] && 64 * o + j < 64 * i + lane);
             }
         }
-        __syncthreads();
-        if (t < p.M) {
-            int rank[PER] = {};
-            for (int j = 0; j < p.E; ++j) {
-                const double other = logits[wave][j];
+        // exp(l - the largest l), summed over all experts or over the chosen ones; a NaN or an infinity among the summands gives what the formula gives
+        double top = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < PER; ++i) rank[i] += other > key[i] || (other == key[i] && j < 64 * i + lane);
-            }
-            // exp(l - the largest l), summed over all experts or over the chosen ones; a NaN or an infinity among the summands gives what the formula gives
-            double top = -INFINITY;
+        for (int i = 0; i < PER; ++i) top = fmax(top, key[i]);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) top = fmax(top, key[i]);
+        for (int d = 32; d >= 1; d >>= 1) top = fmax(top, __shfl_xor(top, d));
+        float part[PER], sum = 0.0f;
 #pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) top = fmax(top, __shfl_xor(top, d));
-            float part[PER], sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const bool live = 64 * i + lane < p.E, taken = live && rank[i] < p.k;
-                part[i] = live ? expf((float)(mine[i] - top)) : 0.0f;
-                if (p.renormalize ? taken : live) sum += part[i];
-            }
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = 64 * i + lane;
-                if (e >= p.E || rank[i] >= p.k) continue;
-                const float s = part[i] / sum;
-                chosen[t][rank[i]] = e;
-                share[t][rank[i]] = s;
-                atomicOr(&tokens[e], 1ull << t);                   // (bits: no order)
-                if (p.experts) p.experts[t * p.k + rank[i]] = e;
-                if (p.weights) p.weights[t * p.k + rank[i]] = s;
-            }
+        for (int i = 0; i < PER; ++i) {
+            const bool live = 64 * i + lane < p.E, taken = live && rank[i] < p.k;
+            part[i] = live ? expf((float)(mine[i] - top)) : 0.0f;
+            if (p.renormalize ? taken : live) sum += part[i];
         }
-        __syncthreads();
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = 64 * i + lane;
+            if (e >= p.E || rank[i] >= p.k) continue;
+            const float s = part[i] / sum;
+            chosen[t][rank[i]] = e;
+            share[t][rank[i]] = s;
+            atomicOr(&tokens[e], 1ull << t);                   // (bits: no order)
+            if (p.experts) p.experts[t * p.k + rank[i]] = e;
+            if (p.weights) p.weights[t * p.k + rank[i]] = s;
+        }
     }
+    __syncthreads();
     // first place and segment of every expert, by a sum over the experts before it
     if (wave == 0) {
         int places = 0, segments = 0;
@@ -157,77 +170,76 @@ __global__ void __launch_bounds__(S::W * 64) moe_gated_kernel(const MoeParams p)
     finish_rows<S::MB, S::NB, S::W, true>(moe_inner(p, seg), s.acc, reinterpret_cast<float *>(lds), 0, n0, cols);
 }
 
-// MOST: tokens that there is room for
-template <class S, int MOST>
+// Workgroup (x, y): 16 columns of y, share y of the reduction.
+template <class S>
 __global__ void __launch_bounds__(S::W * 64) moe_down_kernel(const MoeParams p)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
-    __shared__ float totals[S::W * MOST * 16 * S::NB];
+    extern __shared__ float totals[];                              // [W][M][16 NB]
     const MoePlan *plan = p.plan;
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.D - n0, 16 * S::COLS);
     auto view_of = [&](const MoeSegment &seg) {
         return StreamView{p.h + (int64_t)seg.first * p.F, p.F, seg.rows, seg.rows, {static_cast<const uint16_t *>(p.down.w) + ((int64_t)seg.expert * p.D + n0) * p.F, nullptr}, {p.F, 0}, cols, p.F};
     };
     auto row_of = [](int row) { return row; };
-    const int panels = (p.F + S::K - 1) / S::K, segments = __builtin_amdgcn_readfirstlane(plan->segments);
+    const int panels = (p.F + S::K - 1) / S::K, all = __builtin_amdgcn_readfirstlane(plan->segments) * panels;
+    const int first = (int)((int64_t)all * blockIdx.y / p.shares), end = (int)((int64_t)all * (blockIdx.y + 1) / p.shares);
     Stream<S> s(view_of(moe_segment(plan, 0)), (unsigned)reinterpret_cast<uintptr_t>(lds), row_of);
     float *mine = totals + s.wave * p.M * 16 * S::NB;
     for (int i = s.lane; i < p.M * 16 * S::NB; i += 64) mine[i] = 0.0f;
-    // this wave's panels: every W-th of all segments'; `to`: the next one that is asked for
-    struct Place { int segment, panel; };
-    auto settle = [&](Place &at) {
-        while (at.panel >= panels && at.segment < segments) {
-            at.panel -= panels;
-            ++at.segment;
-        }
-    };
-    Place at = {0, s.wave}, to = at;
-    settle(at);
-    settle(to);
+    MoePlace<S::W> at(panels, first + s.wave), to = at;             // the panel that is multiplied, the next one that is asked for
     int opened = 0;
     auto request = [&](int slot) {
         if (to.segment != opened) {
             opened = to.segment;
-            const MoeSegment seg = moe_segment(plan, opened);
-            s.open_rows(view_of(seg), row_of);
-            s.open_weight(view_of(seg), 0);
+            const StreamView view = view_of(moe_segment(plan, opened));
+            s.open_rows(view, row_of);
+            s.open_weight(view, 0);
         }
         s.request(to.panel, slot);
-        to.panel += S::W;
-        settle(to);
+        to.next();
     };
     int summed = at.segment, slot = 0;
-    bool ahead = false;                                            // whether the panel behind the next one has been asked for
-    if (to.segment < segments) {
-        request(0);
-        if (to.segment < segments) {
-            request(1);
-            ahead = true;
-        }
-    }
-    while (at.segment < segments) {
+    if (to.at < end) request(0);
+    bool ahead = to.at < end;                                      // whether the panel behind the next one has been asked for
+    if (ahead) request(1);
+    while (at.at < end) {
         if (at.segment != summed) {
             moe_add(plan, moe_segment(plan, summed), s.acc, mine);
             s.clear();
             summed = at.segment;
         }
-        // (what moe_add reads of the plan is waited for by the compiler, and requests are in order: the wait below is never too short)
+        // (what the compiler loads of the plan in between only makes this wait longer)
         if (ahead) Stream<S>::template wait<S::REQS>();
         else Stream<S>::template wait<0>();
         s.multiply(slot);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the buffer is in registers
-        ahead = to.segment < segments;
+        ahead = to.at < end;
         if (ahead) request(slot);
         slot ^= 1;
-        at.panel += S::W;
-        settle(at);
+        at.next();
     }
-    if (summed < segments) moe_add(plan, moe_segment(plan, summed), s.acc, mine);
-    __syncthreads();
+    if (first + s.wave < end) moe_add(plan, moe_segment(plan, summed), s.acc, mine);
     moe_finish<S::NB, S::W>(p, totals, n0, cols);
 }
 
-template <int MB, int XQ, int MOST>
+// The shares of y added in order: four columns per thread.  (The workgroup of a column that is done last could add them, without this launch: the fence that its sight of the others' parts takes writes back
+// an XCD's whole L2, and two shares of 32 tokens over 8 experts of 4096 x 14336 then took 220 us, one 124.)
+__global__ void __launch_bounds__(256) moe_join_kernel(const MoeParams p)
+{
+    const int pieces = p.D / 4, at = blockIdx.x * 256 + threadIdx.x;
+    if (at >= p.M * pieces) return;
+    const int token = at / pieces, col = (at - token * pieces) * 4;
+    const float *from = p.partial + (int64_t)token * p.D + col;
+    floatx4 sum = {};
+#pragma unroll 8
+    for (int s = 0; s < p.shares; ++s, from += (int64_t)p.M * p.D) sum += *reinterpret_cast<const floatx4 *>(from);
+    __bf16 *to = reinterpret_cast<__bf16 *>(p.y) + token * p.ldy + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = (__bf16)sum[e];
+}
+
+template <int MB, int XQ>
 hipError_t launch_products(const MoeParams &p, hipStream_t stream)
 {
     typedef StreamShape<MB, 2, XQ, 4, true> Gated;
@@ -236,7 +248,7 @@ hipError_t launch_products(const MoeParams &p, hipStream_t stream)
     hipLaunchKernelGGL((moe_gated_kernel<Gated>), dim3((unsigned)((p.F + 15) / 16), (unsigned)segments), dim3(Gated::W * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((moe_down_kernel<Down, MOST>), dim3((unsigned)((p.D + 15) / 16)), dim3(Down::W * 64), 0, stream, p);
+    hipLaunchKernelGGL((moe_down_kernel<Down>), dim3((unsigned)((p.D + 15) / 16), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 16 * sizeof(float), stream, p);
     return hipGetLastError();
 }
 
@@ -245,18 +257,22 @@ hipError_t launch_products(const MoeParams &p, hipStream_t stream)
 hipError_t launch_moe(const MoeParams &p, hipStream_t stream)
 {
     if (p.M == 0) return hipSuccess;
-    if (p.M <= 4) hipLaunchKernelGGL(moe_logits_kernel<1>, dim3((unsigned)p.E), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL(moe_logits_kernel<2>, dim3((unsigned)p.E, (unsigned)((p.M + 7) / 8)), dim3(256), 0, stream, p);
+    if (p.M * p.E <= 1024) hipLaunchKernelGGL(moe_logits_kernel<1>, dim3((unsigned)p.E, (unsigned)p.M), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(moe_logits_kernel<4>, dim3((unsigned)p.E, (unsigned)((p.M + 3) / 4)), dim3(256), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int rows = p.group ? 16 : moe_rows(p.M, p.E, p.k);
-    hipLaunchKernelGGL(moe_plan_kernel, dim3(1), dim3(1024), 0, stream, p, rows);
+    if (p.E <= 64) hipLaunchKernelGGL(moe_plan_kernel<1>, dim3(1), dim3(1024), 0, stream, p, rows);
+    else if (p.E <= 128) hipLaunchKernelGGL(moe_plan_kernel<2>, dim3(1), dim3(1024), 0, stream, p, rows);
+    else hipLaunchKernelGGL(moe_plan_kernel<4>, dim3(1), dim3(1024), 0, stream, p, rows);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.group) return launch_moe_q4(p, stream);
-    if (rows == 32) return launch_products<2, 4, kMoeTokens>(p, stream);
-    if (p.M <= 8) return launch_products<1, 1, 8>(p, stream);
-    return p.M <= 16 ? launch_products<1, 2, 16>(p, stream) : launch_products<1, 2, kMoeTokens>(p, stream);
+    if (p.group) e = launch_moe_q4(p, stream);
+    else if (rows == 32) e = launch_products<2, 4>(p, stream);
+    else e = p.M <= 8 ? launch_products<1, 1>(p, stream) : launch_products<1, 2>(p, stream);
+    if (e != hipSuccess || p.shares == 1) return e;
+    hipLaunchKernelGGL(moe_join_kernel, dim3((unsigned)(((int64_t)p.M * (p.D / 4) + 255) / 256)), dim3(256), 0, stream, p);
+    return hipGetLastError();
 }
 
 }  // namespace atb

@@ -48,13 +48,11 @@ struct Q4Stream {
     int x_off;
     floatx4 acc[1][NB];
 
-    // Row i of the workgroup is row row_of(i) of x.
-    template <class F>
-    ATB_DEV Q4Stream(const Q4View &v, F row_of) : lane(threadIdx.x & 63), c(lane & 15), q(lane >> 4), wave(__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)), K(v.K)
+    // (open_rows is the caller's)
+    ATB_DEV Q4Stream(const Q4View &v) : lane(threadIdx.x & 63), c(lane & 15), q(lane >> 4), wave(__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)), K(v.K)
     {
 #pragma unroll
         for (int g = 0; g < (S::GATED ? 2 : 1); ++g) open_weight(v, g);
-        open_rows(v, row_of);
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int col = min(16 * (j % S::COLS) + c, v.cols - 1);
@@ -76,7 +74,7 @@ struct Q4Stream {
         sr[g] = rsrc_of(w.scales, v.cols * groups * 2);
         if (S::ZEROS) zr[g] = rsrc_of(w.zeros, v.cols * groups);
     }
-    // rows >= M and columns >= N repeat the last one: they only feed sums that are never stored
+    // Row i of the workgroup is row row_of(i) of x.  Rows >= M and columns >= N repeat the last one: they only feed sums that are never stored
     template <class F>
     ATB_DEV void open_rows(const Q4View &v, F row_of)
     {
@@ -202,18 +200,40 @@ struct Q4Stream {
         return r;
     }
 
-    ATB_DEV void multiply(const Panel &s, int panel)
+    // x of a panel, asked for ahead of the next panel's weights: requests come back in order, and the first MFMA would wait for these too.  With scales and zero points of 8 groups of two columns there are no
+    // registers for that: half a panel's is asked for where it is multiplied.
+    static constexpr bool ROWS_FIRST = !(GROUPS == 8 && NB > 1);
+    struct Rows { intx4 x[ROWS_FIRST ? 8 : 4]; int panel; };
+    template <int from, int count>
+    ATB_DEV void ask_rows(Rows &r) const
     {
+#pragma unroll
+        for (int e = from; e < from + count; ++e) {
+            const int k = r.panel * kQ4PanelK + 32 * e;                            // K % 32 == 0
+            r.x[e % (ROWS_FIRST ? 8 : 4)] = load16(xr, k < K ? x_off + k * 2 : kOutside);
+        }
+    }
+    ATB_DEV void load_rows(Rows &r, int panel) const
+    {
+        r.panel = panel;
+        if constexpr (ROWS_FIRST) {
+            ask_rows<0, 8>(r);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    ATB_DEV void multiply(const Panel &s, Rows &r)
+    {
+        if constexpr (ROWS_FIRST) __builtin_amdgcn_sched_barrier(0);
         constexpr int PER = G / 32, SCHED = S::ZEROS ? 1 : 2;      // MFMAs of a group, and of what is scheduled together (registers)
         const intx4 ones = {0x3F803F80, 0x3F803F80, 0x3F803F80, 0x3F803F80};
         const floatx4 none = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            intx4 x[4], codes[NB];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int k = panel * kQ4PanelK + 32 * (4 * h + e);                  // K % 32 == 0
-                x[e] = load16(xr, k < K ? x_off + k * 2 : kOutside);
+            intx4 codes[NB];
+            if constexpr (!ROWS_FIRST) {
+                if (h == 0) ask_rows<0, 4>(r);
+                else ask_rows<4, 4>(r);
             }
 #pragma unroll
             for (int j = 0; j < NB; ++j) codes[j] = transpose(s.w[j][h]);
@@ -225,7 +245,7 @@ struct Q4Stream {
                 for (int j = 0; j < NB; ++j) sum[j] = none;
 #pragma unroll
                 for (int e = g * PER; e < (g + 1) * PER; ++e) {
-                    const intx4 now = reorder(x[e % 4]);
+                    const intx4 now = reorder(r.x[e % (ROWS_FIRST ? 8 : 4)]);
                     xs = mfma_rows(now, ones, xs);
 #pragma unroll
                     for (int j = 0; j < NB; ++j) sum[j] = mfma_rows(now, expand((unsigned)codes[j][e % 4]), sum[j]);
@@ -243,19 +263,25 @@ struct Q4Stream {
         }
     }
 
-    ATB_DEV void run()
+    // open: called once the first weights have been asked for; opens the rows
+    template <class F>
+    ATB_DEV void run(F open)
     {
         const int panels = (K + kQ4PanelK - 1) / kQ4PanelK;
         Panel a, b;
+        Rows r;
         int k = wave;
         if (k < panels) load(a, k);
+        open();
         while (k < panels) {
+            load_rows(r, k);
             if (k + S::W < panels) load(b, k + S::W);
-            multiply(a, k);
+            multiply(a, r);
             k += S::W;
             if (k >= panels) break;
+            load_rows(r, k);
             if (k + S::W < panels) load(a, k + S::W);
-            multiply(b, k);
+            multiply(b, r);
             k += S::W;
         }
     }

@@ -25,8 +25,8 @@ __global__ void __launch_bounds__(S::W * 64, 4) q4_stream_kernel(const StreamPar
     __shared__ float lds[S::W * S::NB * 256];
     const int m0 = blockIdx.y * 16, n0 = blockIdx.x * 16 * S::COLS, rows = min(p.M - m0, 16), cols = min(p.N - n0, 16 * S::COLS);
     const Q4View view = {p.x + (int64_t)m0 * p.ldx, p.ldx, rows, rows, {q4_columns(p.w[0], n0, p.K, S::G), q4_columns(p.w[1], S::GATED ? n0 : 0, p.K, S::G)}, cols, p.K};
-    Q4Stream<S> s(view, [](int row) { return row; });
-    s.run();
+    Q4Stream<S> s(view);
+    s.run([&] { s.open_rows(view, [](int row) { return row; }); });
     finish_rows<1, S::NB, S::W, S::GATED>(p, s.acc, lds, m0, n0, cols);
 }
 

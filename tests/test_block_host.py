@@ -207,10 +207,13 @@ def test_moe_refuses():
 
 def test_workspace_of_a_mixture_of_experts():
     L = atb.lib()
-    for M, F, E, k in ((0, 8, 1, 1), (1, 8, 1, 1), (64, 14336, 256, 16)):
-        size = L.atb_moe_workspace(M, F, E, k)
+    for M, D, F, E, k in ((0, 8, 8, 1, 1), (1, 8, 8, 1, 1), (1, 4096, 14336, 8, 2), (64, 2048, 14336, 256, 16)):
+        size = L.atb_moe_workspace(M, D, F, E, k, 0)
         assert size % 256 == 0 and size >= 8 * M * E + 2 * M * k * F + 8 * 1024
-    for bad in ((-1, 8, 4, 2), (65, 8, 4, 2), (1, 12, 4, 2), (1, 0, 4, 2), (1, 2 ** 22, 4, 2), (1, 8, 0, 1), (1, 8, 257, 1), (1, 8, 4, 0), (1, 8, 4, 5), (1, 8, 40, 17)):
+        if D % 128 == 0:
+            assert L.atb_moe_workspace(M, D, F, E, k, 128) >= 8 * M * E + 2 * M * k * F + 8 * 1024
+    for bad in ((-1, 8, 8, 4, 2, 0), (65, 8, 8, 4, 2, 0), (1, 8, 12, 4, 2, 0), (1, 8, 0, 4, 2, 0), (1, 4, 8, 4, 2, 0), (1, 8, 2 ** 22, 4, 2, 0), (1, 8, 8, 0, 1, 0), (1, 8, 8, 257, 1, 0), (1, 8, 8, 4, 0, 0),
+                (1, 8, 8, 4, 5, 0), (1, 8, 8, 40, 17, 0), (1, 64, 64, 4, 2, 16), (1, 64, 96, 4, 2, 64)):
         assert L.atb_moe_workspace(*bad) == 0
 
 

@@ -269,7 +269,7 @@ def test_through_the_c_entry_point():
     want = atb.moe_feed_forward(*args, k)
     L, stream = atb.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     y = torch.full((M, D + 3), 7.0, dtype=BF16, device="cuda")
-    work = torch.empty(L.atb_moe_workspace(M, F, E, k), dtype=torch.uint8, device="cuda")
+    work = torch.empty(L.atb_moe_workspace(M, D, F, E, k, 0), dtype=torch.uint8, device="cuda")
     m = atb.Moe(args[0].data_ptr(), args[1].data_ptr(), D, D, *(atb.MoeWeight(w.data_ptr(), None, None) for w in args[2:]), M, D, F, E, k, 0, 0, 1, work.data_ptr())
     assert L.atb_moe_forward(ctypes.byref(m), y.data_ptr(), D + 3, None, None, stream) == 0
     assert torch.equal(y[:, :D], want) and bool((y[:, D:] == 7.0).all())
