@@ -64,6 +64,9 @@ constexpr int kResidualPerThread = 8;              // elements of a row that a t
 constexpr int kResidualThreads = 512;              // workgroup of the backward pass: 256 registers per thread
 constexpr int kResidualMaxGradRow = 2 * kResidualThreads * kResidualPerThread;       // longer rows are read again for every sum
 
+// ... and rows of less than a chunk with them
+static inline bool residual_is_long(int64_t D) { return D > kResidualMaxGradRow || D < kResidualPerThread; }
+
 // Threads per row: the power of two, 64 to 512, that holds it.
 static inline int residual_threads(int64_t D)
 {
@@ -72,13 +75,13 @@ static inline int residual_threads(int64_t D)
     return t;
 }
 
-// The backward pass's workspace in floats.  Sums over the rows of a group are taken by `parts` workgroups, one per CU of the 256 in all (of rows longer than
-// kResidualMaxGradRow, whose sums are a pass of their own, 64 times the column blocks), with chains of at most 512 rows as in norm_partials.
+// The backward pass's workspace in floats.  Sums over the rows of a group are taken by `parts` workgroups, one per CU of the 256 in all (of rows that
+// residual_is_long, whose sums are a pass of their own, 64 times the column blocks), with chains of at most 512 rows as in norm_partials.
 struct ResidualRoom { int64_t parts, sums, totals, rows, total; };
 static inline ResidualRoom residual_room(int64_t M, int64_t D, int64_t groups)
 {
     ResidualRoom r = {};
-    const bool is_long = D > kResidualMaxGradRow;
+    const bool is_long = residual_is_long(D);
     const int64_t rows = M / groups, at_once = is_long ? 1 : kResidualThreads / residual_threads(D), most = std::max<int64_t>(1, (is_long ? 64 : 256) / groups);
     const int64_t turns = (rows + at_once - 1) / at_once;
     r.parts = M == 0 ? 0 : turns < most ? turns : most * ((turns + most * 512 - 1) / (most * 512));

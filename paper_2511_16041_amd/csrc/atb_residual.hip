@@ -26,6 +26,12 @@ struct Raw {
 #pragma unroll
         for (int n = 0; n < N; ++n) v[n] = load_chunk<T>(row, at + n * Chunk<T>::E, D);
     }
+    // ... of a chunk that lies inside the row
+    ATB_DEV void fetch(const T *chunk)
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = *reinterpret_cast<const typename Chunk<T>::any *>(chunk + n * Chunk<T>::E);
+    }
     ATB_DEV void fill(float x)
     {
 #pragma unroll
@@ -66,20 +72,116 @@ ATB_DEV Raw<P> param(const void *w, int64_t row, int at, int D, float other)
     return v;
 }
 
-// The sums of a row over its T threads; two areas of scratch in turns, so that one barrier is enough
+// Threads of a row: T, or as many of T as the launch asks for where a row has a workgroup to itself.
+template <int T> ATB_DEV int row_threads() { return T >= kResidualThreads ? (int)blockDim.x : T; }
+
+// A thread's chunk c of a row of D >= E elements.  The row's last chunk is moved back to end with the row, and what follows lies in the same place: all chunks are loaded whole, without a branch (a wave in which some
+// lanes load and others do not waits for its loads where the two ways meet: the next row was not on its way then, and 3000 x 5000 took 86 us backward where 3000 x 5120 took 57).  Elements before `first` are another
+// thread's, or none's.
+struct Span {
+    int at, first;
+    ATB_DEV bool own(int e) const { return e >= first; }
+};
+template <int T>
+ATB_DEV Span span(int c, int t, int D)
+{
+    const int from = here((c * row_threads<T>() + t) * E), at = min(from, D - E);
+    return {at, from - at};
+}
+template <class T>
+ATB_DEV void store_span(T *row, const Span &s, const float (&v)[E])
+{
+    constexpr int N = Chunk<T>::E;
+    if (s.first == 0) {
+#pragma unroll
+        for (int n = 0; n < E; n += N) {
+            typename Chunk<T>::vec w;
+#pragma unroll
+            for (int e = 0; e < N; ++e) w[e] = (T)v[n + e];
+            *reinterpret_cast<typename Chunk<T>::any *>(row + s.at + n) = w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (s.own(e)) row[s.at + e] = (T)v[e];
+    }
+}
+// A parameter's chunk: `other` where there is none
+template <class P>
+ATB_DEV Raw<P> param(const void *w, int64_t row, const Span &s, int D, float other)
+{
+    Raw<P> v;
+    if (w) v.fetch(static_cast<const P *>(w) + row * D + s.at);
+    else v.fill(other);
+    return v;
+}
+
+// v summed over the wave, in every lane.  Among the 16 lanes of a row by swaps in the registers themselves: a shuffle goes through LDS, six of them one after the other take 800 cycles, and two such sums in a
+// row of 7000 cycles were a third of the backward pass.
+template <int control>
+ATB_DEV float swapped(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), control, 0xF, 0xF, true)); }
+ATB_DEV float lanes_sum(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    v += swapped<0xB1>(v);           // lanes 1 0 3 2 of every four
+    v += swapped<0x4E>(v);           // 2 3 0 1
+    v += swapped<0x141>(v);          // 7 .. 0 of every eight
+    v += swapped<0x140>(v);          // 15 .. 0 of every row
+    const int w = __float_as_int(v);
+    v = (__int_as_float(__builtin_amdgcn_readlane(w, 0)) + __int_as_float(__builtin_amdgcn_readlane(w, 16))) + (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
+#endif
+    return v;
+}
+
+// The sums of a row over its threads; two areas of scratch in turns, so that one barrier is enough
 template <int T, int NT>
 struct RowSums {
     float (*scratch)[2 * NT / 64];
     int turn = 0;
+    ATB_DEV RowSums(float (*scratch_)[2 * NT / 64]) : scratch(scratch_)
+    {
+        if constexpr (T >= kResidualThreads) {                // waves that are not there add nothing
+            for (int i = threadIdx.x; i < 2 * 2 * NT / 64; i += blockDim.x) scratch[0][i] = 0.0f;
+            __syncthreads();
+        }
+    }
     template <int N>
     ATB_DEV void operator()(float (&v)[N])
     {
-        row_sums<T, N>(v, scratch[turn]);
-        turn ^= 1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
+        if constexpr (T > 64) {
+            constexpr int W = T / 64;
+            const int wave = threadIdx.x >> 6;
+            float *here = scratch[turn];
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i) here[wave * N + i] = v[i];
+            __syncthreads();
+            const float *mine = here + (T >= kResidualThreads ? 0 : wave / W * W * N);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) s += mine[w * N + i];
+                v[i] = s;
+            }
+            turn ^= 1;
+        }
     }
 };
 
-// v becomes the normed row, without weight and bias; past the row's end v is 0 before and anything behind
+// Elements that are not this thread's own, as 0: in the few waves that have any
+ATB_DEV void clear_before(float (&v)[E], int first)
+{
+    if (first > 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < first) v[e] = 0.0f;
+    }
+}
+
+// v becomes the normed row, without weight and bias; what is not this thread's is 0 before and anything behind
 template <int T, int NT, int C>
 ATB_DEV void normalise(float (&v)[C][E], int kind, float eps, int t, int D, RowSums<T, NT> &sums, float &mean, float &rstd)
 {
@@ -96,12 +198,12 @@ ATB_DEV void normalise(float (&v)[C][E], int kind, float eps, int t, int D, RowS
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int at = here((c * T + t) * E);
+        const Span own = span<T>(c, t, D);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[c][e] -= mean;
-            if (at + e < D) s[0] += v[c][e] * v[c][e];
-        }
+        for (int e = 0; e < E; ++e) v[c][e] -= mean;
+        clear_before(v[c], own.first);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[0] += v[c][e] * v[c][e];
     }
     sums(s);
     rstd = 1.0f / sqrtf(s[0] / (float)D + eps);
@@ -111,56 +213,84 @@ ATB_DEV void normalise(float (&v)[C][E], int kind, float eps, int t, int D, RowS
         for (int e = 0; e < E; ++e) v[c][e] *= rstd;
 }
 
-// T threads per row with C chunks each, NT / T rows of a workgroup at a time
+// T threads per row with C chunks each, NT / T rows of a workgroup at a time.  Rows of one chunk: the parameters are held, and the next row is on its way while one is normed.
 template <class X, class Z, class P, int T, int C>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) residual_kernel(const ResidualParams p, int rounds)
 {
     constexpr int NT = T < 256 ? 256 : T, R = NT / T;
+    constexpr bool HOLD = C == 1;
     __shared__ float scratch[2][2 * NT / 64];
-    RowSums<T, NT> sums{scratch};
-    const int t0 = threadIdx.x % T, group = threadIdx.x / T, D = p.D;
+    RowSums<T, NT> sums(scratch);
+    const int t = T >= kResidualThreads ? threadIdx.x : threadIdx.x % T, group = T >= kResidualThreads ? 0 : threadIdx.x / T, D = p.D;
     const int64_t per_gate = p.M / p.groups;
+    Raw<X> next_x[C];
+    Raw<Z> next_z[C];
+    Raw<P> w1[HOLD ? C : 1], b1[HOLD ? C : 1], w2[HOLD ? C : 1], b2[HOLD ? C : 1], next_gate[HOLD ? C : 1];
+    auto fetch = [&](int64_t row) {
+        row = row < p.M ? row : 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const Span own = span<T>(c, t, D);
+            next_z[c].fetch(static_cast<const Z *>(p.z) + row * p.ldz + own.at);
+            next_x[c].fetch(static_cast<const X *>(p.x) + row * p.ldx + own.at);
+        }
+        if (HOLD && p.groups > 1) {
+#pragma unroll
+            for (int c = 0; c < (HOLD ? C : 1); ++c) next_gate[c] = param<P>(p.gate, row / per_gate, span<T>(c, t, D), D, 1.0f);
+        }
+    };
+    if constexpr (HOLD) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) next_gate[c] = param<P>(p.gate, 0, span<T>(c, t, D), D, 1.0f);
+    }
+    fetch((int64_t)blockIdx.x * R + group);
+    if constexpr (HOLD) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const Span own = span<T>(c, t, D);
+            w1[c] = param<P>(p.post.weight, 0, own, D, 1.0f);
+            b1[c] = param<P>(p.post.bias, 0, own, D, 0.0f);
+            w2[c] = param<P>(p.pre.weight, 0, own, D, 1.0f);
+            b2[c] = param<P>(p.pre.bias, 0, own, D, 0.0f);
+        }
+    }
     for (int n = 0; n < rounds; ++n) {                        // the same number for every thread of the workgroup
-        const int64_t row = ((int64_t)n * gridDim.x + blockIdx.x) * R + group, at_row = row < p.M ? row : 0;
-        const int t = here(t0);
+        const int64_t row = ((int64_t)n * gridDim.x + blockIdx.x) * R + group;
         Raw<X> x[C];
+        Raw<P> gate[HOLD ? C : 1];
         float v[C][E];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            Raw<Z> z;
-            z.fetch(static_cast<const Z *>(p.z) + at_row * p.ldz, (c * T + t) * E, D);
-            x[c].fetch(static_cast<const X *>(p.x) + at_row * p.ldx, (c * T + t) * E, D);
+            const Span own = span<T>(c, t, D);
+            x[c] = next_x[c];
+            if constexpr (HOLD) gate[c] = next_gate[c];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[c][e] = z[e];
+            for (int e = 0; e < E; ++e) v[c][e] = next_z[c][e];
+            clear_before(v[c], own.first);
         }
+        if (HOLD && n + 1 < rounds) fetch(row + (int64_t)gridDim.x * R);
         float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f;
         if (p.post.kind != ATB_NORM_NONE) normalise<T, NT, C>(v, p.post.kind, p.post.eps, t, D, sums, mean1, rstd1);
-        const int64_t gate_row = p.gate && p.groups > 1 ? at_row / per_gate : 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int at = here((c * T + t) * E);
-            if (p.post.kind != ATB_NORM_NONE) {
-                const Raw<P> w = param<P>(p.post.weight, 0, at, D, 1.0f);
-                const Raw<P> b = param<P>(p.post.bias, 0, at, D, 0.0f);
+            const Span own = span<T>(c, t, D);
+            const Raw<P> w = HOLD ? w1[HOLD ? c : 0] : param<P>(p.post.weight, 0, own, D, 1.0f), b = HOLD ? b1[HOLD ? c : 0] : param<P>(p.post.bias, 0, own, D, 0.0f);
+            const Raw<P> g = HOLD ? gate[HOLD ? c : 0] : param<P>(p.gate, p.groups > 1 && row < p.M ? row / per_gate : 0, own, D, 1.0f);
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * w[e] + b[e];
-            }
-            const Raw<P> g = param<P>(p.gate, gate_row, at, D, 1.0f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[c][e] = at + e < D ? p.scale * x[c][e] + g[e] * v[c][e] : 0.0f;
-            if (row < p.M) store_row<X>(static_cast<X *>(p.r) + row * p.ldr, at, D, v[c]);
+            for (int e = 0; e < E; ++e) v[c][e] = p.scale * x[c][e] + g[e] * (v[c][e] * w[e] + b[e]);
+            clear_before(v[c], own.first);
+            if (row < p.M) store_span(static_cast<X *>(p.r) + row * p.ldr, own, v[c]);
             if (C > 1) __builtin_amdgcn_sched_barrier(0);     // chunk by chunk: registers
         }
         if (p.pre.kind != ATB_NORM_NONE) {
             normalise<T, NT, C>(v, p.pre.kind, p.pre.eps, t, D, sums, mean2, rstd2);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int at = here((c * T + t) * E);
-                const Raw<P> w = param<P>(p.pre.weight, 0, at, D, 1.0f);
-                const Raw<P> b = param<P>(p.pre.bias, 0, at, D, 0.0f);
+                const Span own = span<T>(c, t, D);
+                const Raw<P> w = HOLD ? w2[HOLD ? c : 0] : param<P>(p.pre.weight, 0, own, D, 1.0f), b = HOLD ? b2[HOLD ? c : 0] : param<P>(p.pre.bias, 0, own, D, 0.0f);
 #pragma unroll
                 for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * w[e] + b[e];
-                if (row < p.M) store_row<Z>(static_cast<Z *>(p.h) + row * p.ldh, at, D, v[c]);
+                if (row < p.M) store_span(static_cast<Z *>(p.h) + row * p.ldh, own, v[c]);
                 if (C > 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -170,6 +300,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) residual_kernel(const Resid
             p.stats[2 * p.M + row] = mean2;
             p.stats[3 * p.M + row] = rstd2;
         }
+        if (!HOLD && n + 1 < rounds) fetch(row + (int64_t)gridDim.x * R);
     }
 }
 
@@ -187,22 +318,23 @@ struct RowStats {
 
 // dx, dz and (SUMS) the workgroup's part of the sums over rows, [group][part][SUMS][D]: S1, dw2's, S0, db2's.  T threads per row with C chunks each.
 template <class X, class Z, class P, int T, int C, int SUMS>
-__global__ void __launch_bounds__(kResidualThreads) residual_grad_kernel(const ResidualParams p, int parts, int rounds)
+__global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) residual_grad_kernel(const ResidualParams p, int parts, int rounds)
 {
-    constexpr int NT = kResidualThreads, R = NT / T;
-    // registers: the next row's operands and the parameters are held unless two chunks of them would not fit
-    constexpr bool AHEAD = C == 1 || (sizeof(X) == 2 && SUMS < 4), HOLD = C == 1 || sizeof(P) == 2;
+    constexpr int NT = T > kResidualThreads ? T : kResidualThreads, R = NT / T;
+    // registers: the next row's operands (dr, which is used last, on its own) and the parameters are held unless they would not fit
+    constexpr bool TIGHT = T > kResidualThreads && sizeof(X) == 4, LARGE = TIGHT && sizeof(Z) == 4;
+    constexpr bool AHEAD = C == 1 ? !LARGE : sizeof(X) == 2 && SUMS < 4, DR_AHEAD = AHEAD && !TIGHT, HOLD = C == 1 ? !TIGHT || sizeof(P) == 2 : sizeof(P) == 2;
     __shared__ float scratch[2][2 * NT / 64];
-    RowSums<T, NT> sums{scratch};
-    const int t = threadIdx.x % T, group = threadIdx.x / T, D = p.D;
+    RowSums<T, NT> sums(scratch);
+    const int t = T >= kResidualThreads ? threadIdx.x : threadIdx.x % T, group = T >= kResidualThreads ? 0 : threadIdx.x / T, D = p.D;
     const int64_t per_gate = p.M / p.groups, gate_row = blockIdx.x / parts, part = blockIdx.x % parts;
     const bool normed1 = p.post.kind != ATB_NORM_NONE, normed2 = p.pre.kind != ATB_NORM_NONE;
     const float inv = 1.0f / (float)D, centre1 = p.post.kind == ATB_NORM_LAYER ? inv : 0.0f, centre2 = p.pre.kind == ATB_NORM_LAYER ? inv : 0.0f;
     struct Params { Raw<P> w1, b1, w2, gate; };
     Params held[HOLD ? C : 1];
     auto params = [&](int c) {
-        const int at = here((c * T + t) * E);
-        return Params{param<P>(p.post.weight, 0, at, D, 1.0f), param<P>(p.post.bias, 0, at, D, 0.0f), param<P>(p.pre.weight, 0, at, D, 1.0f), param<P>(p.gate, gate_row, at, D, 1.0f)};
+        const Span own = span<T>(c, t, D);
+        return Params{param<P>(p.post.weight, 0, own, D, 1.0f), param<P>(p.post.bias, 0, own, D, 0.0f), param<P>(p.pre.weight, 0, own, D, 1.0f), param<P>(p.gate, gate_row, own, D, 1.0f)};
     };
     if constexpr (HOLD) {
 #pragma unroll
@@ -222,41 +354,53 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_kernel(const R
         next.fetch(p, row);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int at = here((c * T + t) * E);
-            next_x[c].fetch(static_cast<const X *>(p.x) + row * p.ldx, at, D);
-            next_z[c].fetch(static_cast<const Z *>(p.z) + row * p.ldz, at, D);
-            if (p.dr) next_dr[c].fetch(static_cast<const X *>(p.dr) + row * p.lddr, at, D);
-            else next_dr[c].fill(0.0f);
-            if (normed2) next_dh[c].fetch(static_cast<const Z *>(p.dh) + row * p.lddh, at, D);
+            const Span own = span<T>(c, t, D);
+            next_x[c].fetch(static_cast<const X *>(p.x) + row * p.ldx + own.at);
+            next_z[c].fetch(static_cast<const Z *>(p.z) + row * p.ldz + own.at);
+            if (normed2) next_dh[c].fetch(static_cast<const Z *>(p.dh) + row * p.lddh + own.at);
             else next_dh[c].fill(0.0f);
+        }
+    };
+    auto fetch_dr = [&](int64_t row) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (p.dr) next_dr[c].fetch(static_cast<const X *>(p.dr) + row * p.lddr + span<T>(c, t, D).at);
+            else next_dr[c].fill(0.0f);
         }
     };
     bool next_live = false;
     int64_t next_row = row_of(0, next_live);
     if (AHEAD) fetch(next_row);
+    if (DR_AHEAD) fetch_dr(next_row);
     for (int n = 0; n < rounds; ++n) {                        // the same number for every thread of the workgroup
         const int64_t row = next_row;
         const bool live = next_live;
         if (!AHEAD) fetch(row);
+        if (!DR_AHEAD) fetch_dr(row);
         const RowStats st = next;
         float xh1[C][E], xh2[C][E], g[C][E], s[2] = {0.0f, 0.0f};
         Raw<X> dr[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const Params k = HOLD ? held[HOLD ? c : 0] : params(c);
+            const Span own = span<T>(c, t, D);
             dr[c] = next_dr[c];
+            float dh[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) dh[e] = next_dh[c][e];
+            clear_before(dh, own.first);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 xh1[c][e] = (next_z[c][e] - st.mean1) * st.rstd1;
-                const float r = p.scale * next_x[c][e] + k.gate[e] * (xh1[c][e] * k.w1[e] + k.b1[e]), dh = next_dh[c][e];
+                const float r = p.scale * next_x[c][e] + k.gate[e] * (xh1[c][e] * k.w1[e] + k.b1[e]);
                 xh2[c][e] = (r - st.mean2) * st.rstd2;
                 if constexpr (SUMS > 0) {
                     if (live) {
-                        sum[1][c][e] += dh * xh2[c][e];       // (dh is 0 past the end)
-                        if constexpr (SUMS > 2) sum[SUMS - 1][c][e] += dh;
+                        sum[1][c][e] += dh[e] * xh2[c][e];
+                        if constexpr (SUMS > 2) sum[SUMS - 1][c][e] += dh[e];
                     }
                 }
-                g[c][e] = dh * k.w2[e];
+                g[c][e] = dh[e] * k.w2[e];
                 s[0] += g[c][e];
                 s[1] += g[c][e] * xh2[c][e];
             }
@@ -265,6 +409,7 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_kernel(const R
         if (n + 1 < rounds) {                                 // the next row is on its way while this one is summed
             next_row = row_of(n + 1, next_live);
             if (AHEAD) fetch(next_row);
+            if (DR_AHEAD) fetch_dr(next_row);
         }
         if (normed2) sums(s);
         const float m0 = s[0] * centre2, m1 = s[1] * inv;
@@ -272,25 +417,28 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_kernel(const R
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const Params k = HOLD ? held[HOLD ? c : 0] : params(c);
-            const int at = here((c * T + t) * E);
-            float out[E];
+            const Span own = span<T>(c, t, D);
+            float d[E], out[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                float d = dr[c][e];
-                if (normed2) d += st.rstd2 * (g[c][e] - m0 - xh2[c][e] * m1);
-                if (at + e >= D) d = 0.0f;
+                d[e] = dr[c][e];
+                if (normed2) d[e] += st.rstd2 * (g[c][e] - m0 - xh2[c][e] * m1);
+            }
+            clear_before(d, own.first);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
                 if constexpr (SUMS > 0) {
                     if (live) {
-                        sum[0][c][e] += d * xh1[c][e];
-                        if constexpr (SUMS > 2) sum[SUMS - 2][c][e] += d;
+                        sum[0][c][e] += d[e] * xh1[c][e];
+                        if constexpr (SUMS > 2) sum[SUMS - 2][c][e] += d[e];
                     }
                 }
-                out[e] = p.scale * d;
-                g[c][e] = d * k.gate[e] * k.w1[e];
+                out[e] = p.scale * d[e];
+                g[c][e] = d[e] * k.gate[e] * k.w1[e];
                 q[0] += g[c][e];
                 q[1] += g[c][e] * xh1[c][e];
             }
-            if (live && p.dx) store_row<X>(static_cast<X *>(p.dx) + row * p.lddx, at, D, out);
+            if (live && p.dx) store_span(static_cast<X *>(p.dx) + row * p.lddx, own, out);
             if (C > 1) __builtin_amdgcn_sched_barrier(0);
         }
         if (normed1) {
@@ -303,7 +451,7 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_kernel(const R
         }
         if (live && p.dz) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) store_row<Z>(static_cast<Z *>(p.dz) + row * p.lddz, here((c * T + t) * E), D, g[c]);
+            for (int c = 0; c < C; ++c) store_span(static_cast<Z *>(p.dz) + row * p.lddz, span<T>(c, t, D), g[c]);
         }
     }
     if constexpr (SUMS > 0) {
@@ -334,11 +482,11 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_kernel(const R
 #pragma unroll
         for (int i = 0; i < SUMS; ++i)
 #pragma unroll
-            for (int c = 0; c < C; ++c) store_row<float>(to + (int64_t)i * D, (c * T + t) * E, D, sum[i][c]);
+            for (int c = 0; c < C; ++c) store_span(to + (int64_t)i * D, span<T>(c, t, D), sum[i][c]);
     }
 }
 
-// ---- rows of more than kResidualMaxGradRow elements: read again for every sum, from the second time on out of a cache
+// ---- rows of more than kResidualMaxGradRow elements, or of less than a chunk: read again for every sum, from the second time on out of a cache
 
 // This thread's share of sums over a row: f(at, sums) adds the chunk at `at`; 16 chunks at a time, so that no chain of additions is longer than 128 and D / 2^16
 template <int N, class F>
@@ -405,7 +553,7 @@ template <class X, class Z, class P>
 __global__ void __launch_bounds__(kResidualThreads) residual_long_kernel(const ResidualParams p)
 {
     __shared__ float scratch[2][2 * kResidualThreads / 64];
-    RowSums<kResidualThreads, kResidualThreads> sums{scratch};
+    RowSums<kResidualThreads, kResidualThreads> sums(scratch);
     const int D = p.D;
     for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
         const int64_t gate_row = row / (p.M / p.groups);
@@ -472,7 +620,7 @@ template <class X, class Z, class P>
 __global__ void __launch_bounds__(kResidualThreads) residual_grad_long_kernel(const ResidualParams p, float *rows)
 {
     __shared__ float scratch[2][2 * kResidualThreads / 64];
-    RowSums<kResidualThreads, kResidualThreads> sums{scratch};
+    RowSums<kResidualThreads, kResidualThreads> sums(scratch);
     const int D = p.D;
     const bool normed1 = p.post.kind != ATB_NORM_NONE, normed2 = p.pre.kind != ATB_NORM_NONE;
     const float inv = 1.0f / (float)D, centre1 = p.post.kind == ATB_NORM_LAYER ? inv : 0.0f, centre2 = p.pre.kind == ATB_NORM_LAYER ? inv : 0.0f;
@@ -580,20 +728,24 @@ __global__ void __launch_bounds__(256) residual_columns_kernel(const ResidualPar
 
 // ---- the sums' parts
 
-// The 16 waves' parts of the sum of `count` rows, `pitch` floats apart from `at` on, 64 rows at a time (shorter chains)
-ATB_DEV float sum_run(const float *at, int64_t pitch, int64_t count, int wave)
+// This wave's part, of 16, of N sums of `count` numbers, `pitch` floats apart from `at` on and `apart` floats from sum to sum; 64 numbers at a time (shorter chains)
+template <int N>
+ATB_DEV void sum_run(const float *at, int64_t pitch, int64_t apart, int64_t count, int wave, float (&s)[N])
 {
     const int64_t run = (count + 15) / 16, first = wave * run, end = min(first + run, count);
-    float s = 0.0f;
     at += first * pitch;
-    for (int64_t i = first; i < end; i += 64) {
-        const int64_t stop = min(end, i + 64);
-        float part = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = 0.0f;
+    for (int64_t from = first; from < end; from += 64) {
+        const int64_t stop = min(end, from + 64);
+        float part[N] = {};
 #pragma unroll 8
-        for (int64_t n = i; n < stop; ++n, at += pitch) part += *at;
-        s += part;
+        for (int64_t n = from; n < stop; ++n, at += pitch)
+#pragma unroll
+            for (int i = 0; i < N; ++i) part[i] += at[i * apart];
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] += part[i];
     }
-    return s;
 }
 
 // The parts of a group's sums added in order, and its gate's gradient; with one group the other parameters' too, else their terms for residual_groups_kernel.  64 columns per workgroup.
@@ -603,8 +755,10 @@ __global__ void __launch_bounds__(1024) residual_params_kernel(const ResidualPar
     __shared__ float sums[16][SUMS][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, D = p.D, col = blockIdx.x * 64 + lane;
     const int64_t g = blockIdx.y;
-    for (int i = 0; i < SUMS; ++i)
-        sums[wave][i][lane] = col < D ? sum_run(p.workspace + (g * p.parts * SUMS + i) * D + col, (int64_t)SUMS * D, p.parts, wave) : 0.0f;
+    float run[SUMS] = {};
+    if (col < D) sum_run<SUMS>(p.workspace + g * p.parts * SUMS * D + col, (int64_t)SUMS * D, D, p.parts, wave, run);
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) sums[wave][i][lane] = run[i];
     __syncthreads();
     if (wave > 0 || col >= D) return;
     float s[4] = {};
@@ -637,11 +791,12 @@ __global__ void __launch_bounds__(1024) residual_groups_kernel(const ResidualPar
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, D = p.D, col = blockIdx.x * 64 + lane, i = blockIdx.y;
     P *out = static_cast<P *>(i == 0 ? p.dpost_weight : i == 1 ? p.dpre_weight : i == 2 ? p.dpost_bias : p.dpre_bias);
     if (!out) return;                                         // the whole workgroup
-    float s = col < D ? sum_run(totals + (int64_t)i * D + col, (int64_t)SUMS * D, p.groups, wave) : 0.0f;
-    sums[wave][lane] = s;
+    float run[1] = {0.0f};
+    if (col < D) sum_run<1>(totals + (int64_t)i * D + col, (int64_t)SUMS * D, 0, p.groups, wave, run);
+    sums[wave][lane] = run[0];
     __syncthreads();
     if (wave > 0 || col >= D) return;
-    s = 0.0f;
+    float s = 0.0f;
 #pragma unroll
     for (int n = 0; n < 16; ++n) s += sums[n][lane];
     out[col] = (P)s;
@@ -651,22 +806,28 @@ __global__ void __launch_bounds__(1024) residual_groups_kernel(const ResidualPar
 
 constexpr int64_t kMostWorkgroups = 1 << 20;        // of a launch; each walks rows a grid apart
 
+// Threads of a workgroup: where a row has it to itself as many waves as the row fills
+template <int T, int C>
+int workgroup(int D, int least) { return T >= kResidualThreads ? (D + C * E * 64 - 1) / (C * E * 64) * 64 : std::max(T, least); }
+
+// Rows of one chunk per thread: workgroups of 16 waves per CU in all walk the rows (8192 x 4096 in bf16, 16 waves 57 us, 8 77, a workgroup for every row 75, as the rest was then).  Of longer rows, with twice the registers for
+// the row alone, one per workgroup (2048 x 8192 in bf16 25 us either way, 3000 x 5001 with an fp32 stream 47, walking with 12 waves 62).
 template <class X, class Z, class P, int T, int C>
 hipError_t forward_of(const ResidualParams &p, hipStream_t stream)
 {
     constexpr int NT = T < 256 ? 256 : T, R = NT / T;
-    const int64_t all = (p.M + R - 1) / R, grid = std::min(all, kMostWorkgroups);
-    hipLaunchKernelGGL((residual_kernel<X, Z, P, T, C>), dim3((unsigned)grid), dim3(NT), 0, stream, p, (int)((all + grid - 1) / grid));
+    const int64_t all = (p.M + R - 1) / R, grid = std::min(all, C == 1 ? (int64_t)256 * (1024 / NT) : kMostWorkgroups);
+    hipLaunchKernelGGL((residual_kernel<X, Z, P, T, C>), dim3((unsigned)grid), dim3(workgroup<T, C>(p.D, 256)), 0, stream, p, (int)((all + grid - 1) / grid));
     return hipGetLastError();
 }
 
 template <class X, class Z, class P, int T, int C, int SUMS>
 hipError_t backward_of(const ResidualParams &p, hipStream_t stream)
 {
-    constexpr int NT = kResidualThreads, R = NT / T;
+    constexpr int NT = T > kResidualThreads ? T : kResidualThreads, R = NT / T;
     const int64_t per_gate = p.M / p.groups, turns = (per_gate + R - 1) / R;
     const int64_t parts = SUMS > 0 ? p.parts : std::min<int64_t>(turns, std::max<int64_t>(1, 2048 / p.groups));
-    hipLaunchKernelGGL((residual_grad_kernel<X, Z, P, T, C, SUMS>), dim3((unsigned)(p.groups * parts)), dim3(NT), 0, stream, p, (int)parts, (int)((turns + parts - 1) / parts));
+    hipLaunchKernelGGL((residual_grad_kernel<X, Z, P, T, C, SUMS>), dim3((unsigned)(p.groups * parts)), dim3(workgroup<T, C>(p.D, NT)), 0, stream, p, (int)parts, (int)((turns + parts - 1) / parts));
     return hipGetLastError();
 }
 
@@ -677,14 +838,16 @@ hipError_t backward_rows(const ResidualParams &p, hipStream_t stream)
         case 64: return backward_of<X, Z, P, 64, 1, SUMS>(p, stream);
         case 128: return backward_of<X, Z, P, 128, 1, SUMS>(p, stream);
         case 256: return backward_of<X, Z, P, 256, 1, SUMS>(p, stream);
-        default: return p.D <= 512 * E ? backward_of<X, Z, P, 512, 1, SUMS>(p, stream) : backward_of<X, Z, P, 512, 2, SUMS>(p, stream);
+        default:
+            if (p.D <= 512 * E) return backward_of<X, Z, P, 512, 1, SUMS>(p, stream);
+            return p.D <= 768 * E ? backward_of<X, Z, P, 768, 1, SUMS>(p, stream) : backward_of<X, Z, P, 512, 2, SUMS>(p, stream);
     }
 }
 
 template <class X, class Z, class P, int SUMS>
 hipError_t sums_of(const ResidualParams &p, float *rows, float *totals, hipStream_t stream)
 {
-    if (p.M > 0 && p.D > kResidualMaxGradRow) {
+    if (p.M > 0 && residual_is_long(p.D)) {
         const int64_t blocks = (p.D + 256 * E - 1) / (256 * E);
         hipLaunchKernelGGL((residual_columns_kernel<X, Z, P, SUMS>), dim3((unsigned)(blocks * p.groups * p.parts)), dim3(256), 0, stream, p, (int)blocks, rows);
         const hipError_t e = hipGetLastError();
@@ -700,7 +863,7 @@ hipError_t sums_of(const ResidualParams &p, float *rows, float *totals, hipStrea
 template <class X, class Z, class P>
 hipError_t forward(const ResidualParams &p, hipStream_t stream)
 {
-    if (p.D > 4 * kResidualThreads * E) {
+    if (p.D > 4 * kResidualThreads * E || p.D < E) {
         hipLaunchKernelGGL((residual_long_kernel<X, Z, P>), dim3((unsigned)std::min(p.M, kMostWorkgroups)), dim3(kResidualThreads), 0, stream, p);
         return hipGetLastError();
     }
@@ -708,14 +871,16 @@ hipError_t forward(const ResidualParams &p, hipStream_t stream)
         case 64: return forward_of<X, Z, P, 64, 1>(p, stream);
         case 128: return forward_of<X, Z, P, 128, 1>(p, stream);
         case 256: return forward_of<X, Z, P, 256, 1>(p, stream);
-        default: return p.D <= 512 * E ? forward_of<X, Z, P, 512, 1>(p, stream) : p.D <= 1024 * E ? forward_of<X, Z, P, 512, 2>(p, stream) : forward_of<X, Z, P, 512, 4>(p, stream);
+        default:
+            if (p.D <= 512 * E) return forward_of<X, Z, P, 512, 1>(p, stream);
+            return p.D <= 1024 * E ? forward_of<X, Z, P, 512, 2>(p, stream) : forward_of<X, Z, P, 512, 4>(p, stream);
     }
 }
 
 template <class X, class Z, class P>
 hipError_t backward(const ResidualParams &p, hipStream_t stream)
 {
-    const bool asked = p.dgate || p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias, is_long = p.D > kResidualMaxGradRow;
+    const bool asked = p.dgate || p.dpost_weight || p.dpost_bias || p.dpre_weight || p.dpre_bias, is_long = residual_is_long(p.D);
     const int sums = !asked ? 0 : p.dpost_bias || p.dpre_bias || (p.dgate && p.post.kind != ATB_NORM_NONE && p.post.bias) ? 4 : 2;
     const ResidualRoom room = residual_room(p.M, p.D, p.groups);
     float *totals = asked && p.groups > 1 ? p.workspace + room.sums : nullptr, *rows = asked && is_long ? p.workspace + room.sums + room.totals : nullptr;
