@@ -15,7 +15,7 @@ struct LinearGradParams {
     int64_t lddy;
     const uint16_t *slope;       // M x N fp16, or null: 1
     uint16_t *dz;                // M x round_up(N, 8) bf16, the padding written as zero, or null: not wanted
-    float *partial;              // linear_parts(M, N) x N column sums, or null
+    float *partial;              // linear_parts(M, N) x N column sums, where dbias is wanted
     void *dbias;                 // N elements of bias_type, or null
     int bias_type;
     int64_t M;
@@ -23,12 +23,12 @@ struct LinearGradParams {
 };
 hipError_t launch_linear_grad(const LinearGradParams &p, hipStream_t stream);
 
-// Runs of rows whose column sums are taken apart: about 1024 workgroups of 2048 columns, runs of 16 rows or more and, for no sum to have a chain of more than 512 additions,
-// of at most 512.
+// Runs of rows whose column sums are taken apart: one of up to 16 rows (which needs no second kernel), else of 4 rows, which are loaded at once, and as many more as it takes for about 1024 workgroups of 2048 columns; for
+// no sum to have a chain of more than 512 additions, of at most 512.
 static inline int64_t linear_parts(int64_t M, int64_t N)
 {
-    if (M <= 0) return 0;
-    const int64_t blocks = (N + 2047) / 2048, wanted = std::max<int64_t>(1, std::min(1024 / std::min<int64_t>(blocks, 1024), (M + 15) / 16));
+    if (M <= 16) return M > 0;
+    const int64_t blocks = (N + 2047) / 2048, wanted = std::max<int64_t>(1, std::min(1024 / std::min<int64_t>(blocks, 1024), (M + 3) / 4));
     return std::max(wanted, (M + 511) / 512);
 }
 
@@ -75,8 +75,8 @@ static inline int residual_threads(int64_t D)
     return t;
 }
 
-// The backward pass's workspace in floats.  Sums over the rows of a group are taken by `parts` workgroups, one per CU of the 256 in all (of rows that
-// residual_is_long, whose sums are a pass of their own, 64 times the column blocks), with chains of at most 512 rows as in norm_partials.
+// The backward pass's workspace in floats.  Sums over the rows of a group are taken by `parts` workgroups, one per CU of the 256 in all (of rows that residual_is_long, whose sums are a pass of their own, 64 times the
+// column blocks), with chains of at most 512 rows as in norm_partials.  (Two per CU, for which 128 registers do in 16 bits and without biases: 8192 x 4096 84 us instead of 81, and twice the parts to add.)
 struct ResidualRoom { int64_t parts, sums, totals, rows, total; };
 static inline ResidualRoom residual_room(int64_t M, int64_t D, int64_t groups)
 {

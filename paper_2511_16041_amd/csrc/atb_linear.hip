@@ -18,52 +18,75 @@ hipError_t launch_tiles_linear(TileParams p, int epilogue, hipStream_t stream)
 namespace {
 
 template <class T>
-ATB_DEV void load_eight(const T *row, int at, int N, float (&v)[8])
-{
+struct Eight {
     typedef T vec __attribute__((ext_vector_type(8)));
     typedef vec any __attribute__((aligned(2)));
-    if (at + 8 <= N) {
-        const vec w = *reinterpret_cast<const any *>(row + at);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)w[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = at + e < N ? (float)row[at + e] : 0.0f;
-    }
-}
+};
 
-// Eight columns per thread, a run of rows per workgroup.  Bound: HBM.
+// Eight columns per thread, a run of rows per workgroup.  Bound: HBM.  The last chunk of a row is moved back to end with it: all are loaded whole, without a branch, at which a wave would wait for its loads (6 x 1654
+// took 12.3 us with one); its elements before `first` are another thread's.  (Rows of fewer than eight elements: one by one.)
 template <bool SLOPE>
 __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradParams p, int parts)
 {
     const int pitch = (p.N + 7) / 8 * 8, col = (blockIdx.x * 256 + threadIdx.x) * 8;
     if (col >= pitch) return;
-    const int64_t first = p.M * blockIdx.y / parts, end = p.M * (blockIdx.y + 1) / parts;
+    const bool narrow = p.N < 8;
+    const int at = narrow ? 0 : min(col, p.N - 8), first = col - at;
+    const int64_t from = p.M * blockIdx.y / parts, end = p.M * (blockIdx.y + 1) / parts;
+    const __bf16 *dy = reinterpret_cast<const __bf16 *>(p.dy) + at;
+    const _Float16 *slope = reinterpret_cast<const _Float16 *>(p.slope) + at;
     float sum[8] = {};
-#pragma unroll 4
-    for (int64_t row = first; row < end; ++row) {
-        float d[8];
-        load_eight(reinterpret_cast<const __bf16 *>(p.dy) + row * p.lddy, col, p.N, d);
-        if constexpr (SLOPE) {
-            float s[8];
-            load_eight(reinterpret_cast<const _Float16 *>(p.slope) + row * p.N, col, p.N, s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[e] *= s[e];
-        }
+    auto add = [&](int64_t row, const float (&d)[8], int left) {              // of d, the elements first .. left - 1
         if (p.dz) {
-            bf16x8 w;
+            if (first == 0 && left == 8) {
+                bf16x8 w;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = (__bf16)d[e];
-            *reinterpret_cast<bf16x8 *>(p.dz + row * pitch + col) = w;
+                for (int e = 0; e < 8; ++e) w[e] = (__bf16)d[e];
+                *reinterpret_cast<bf16x8 *>(p.dz + row * pitch + col) = w;
+            } else {
+                __bf16 *to = reinterpret_cast<__bf16 *>(p.dz) + row * pitch;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (e >= first && e < left) to[at + e] = (__bf16)d[e];
+                    if (col + e >= p.N) to[col + e] = (__bf16)0.0f;
+                }
+            }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += d[e];
-    }
-    if (!p.partial) return;
-    float *to = p.partial + (int64_t)blockIdx.y * p.N + col;
+    };
+    if (narrow) {
+        for (int64_t row = from; row < end; ++row) {
+            float d[8] = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (col + e < p.N) to[e] = sum[e];
+            for (int e = 0; e < 8; ++e)
+                if (e < p.N) d[e] = (float)dy[row * p.lddy + e] * (SLOPE ? (float)slope[row * p.N + e] : 1.0f);
+            add(row, d, p.N);
+        }
+    } else {
+#pragma unroll 4
+        for (int64_t row = from; row < end; ++row) {
+            const bf16x8 g = *reinterpret_cast<const Eight<__bf16>::any *>(dy + row * p.lddy);
+            float d[8];
+            if constexpr (SLOPE) {
+                const Eight<_Float16>::vec s = *reinterpret_cast<const Eight<_Float16>::any *>(slope + row * p.N);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = (float)g[e] * (float)s[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = (float)g[e];
+            }
+            add(row, d, 8);
+        }
+    }
+    if (!p.dbias) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (e < first || at + e >= p.N) continue;
+        if (parts > 1) p.partial[(int64_t)blockIdx.y * p.N + at + e] = sum[e];
+        else if (p.bias_type == ATB_TYPE_F32) static_cast<float *>(p.dbias)[at + e] = sum[e];
+        else static_cast<__bf16 *>(p.dbias)[at + e] = (__bf16)sum[e];
+    }
 }
 
 // The runs' column sums added in order: 64 columns per workgroup, 16 waves with some of the runs each, 64 at a time (shorter chains).
@@ -105,7 +128,7 @@ hipError_t launch_linear_grad(const LinearGradParams &p, hipStream_t stream)
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (!p.dbias) return hipSuccess;
+    if (!p.dbias || parts == 1) return hipSuccess;
     hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)((p.N + 63) / 64)), dim3(1024), 0, stream, p, parts);      // no rows: zeros
     return hipGetLastError();
 }

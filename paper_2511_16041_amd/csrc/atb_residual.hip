@@ -728,44 +728,55 @@ __global__ void __launch_bounds__(256) residual_columns_kernel(const ResidualPar
 
 // ---- the sums' parts
 
-// This wave's part, of 16, of N sums of `count` numbers, `pitch` floats apart from `at` on and `apart` floats from sum to sum; 64 numbers at a time (shorter chains)
-template <int N>
-ATB_DEV void sum_run(const float *at, int64_t pitch, int64_t apart, int64_t count, int wave, float (&s)[N])
+// Sums over `count` numbers that lie `pitch` floats apart, N of them `apart` floats from sum to sum.  A workgroup of 1024 threads has COLS columns, each of its groups of COLS threads a run of the numbers, 64 at a time
+// (shorter chains); the groups' parts are added in order.  What comes back belongs to column threadIdx.x of the first COLS threads.
+template <int COLS, int N>
+ATB_DEV void sum_columns(const float *from, int64_t pitch, int64_t apart, int count, bool live, float (&s)[N], float (*scratch)[N][COLS])
 {
-    const int64_t run = (count + 15) / 16, first = wave * run, end = min(first + run, count);
-    at += first * pitch;
+    constexpr int GROUPS = 1024 / COLS;
+    const int lane = threadIdx.x % COLS, part = threadIdx.x / COLS, run = (count + GROUPS - 1) / GROUPS, first = part * run, end = live ? min(first + run, count) : 0;
+    from += first * pitch;
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = 0.0f;
-    for (int64_t from = first; from < end; from += 64) {
-        const int64_t stop = min(end, from + 64);
-        float part[N] = {};
+    for (int at = first; at < end; at += 64) {
+        const int stop = min(end, at + 64);
+        float chain[N] = {};
 #pragma unroll 8
-        for (int64_t n = from; n < stop; ++n, at += pitch)
+        for (int n = at; n < stop; ++n, from += pitch)
 #pragma unroll
-            for (int i = 0; i < N; ++i) part[i] += at[i * apart];
+            for (int i = 0; i < N; ++i) chain[i] += from[i * apart];
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] += part[i];
+        for (int i = 0; i < N; ++i) s[i] += chain[i];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) scratch[part][i][lane] = s[i];
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        s[i] = 0.0f;
+        for (int from_group = 0; from_group < GROUPS; from_group += 16) {
+            float sixteen = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 16; ++n) sixteen += scratch[from_group + n][i][lane];
+            s[i] += sixteen;
+        }
     }
 }
 
-// The parts of a group's sums added in order, and its gate's gradient; with one group the other parameters' too, else their terms for residual_groups_kernel.  64 columns per workgroup.
-template <class P, int SUMS>
+// The parts of a group's sums, and its gate's gradient; with one group the other parameters' too, else their terms for residual_groups_kernel.
+template <class P, int SUMS, int COLS>
 __global__ void __launch_bounds__(1024) residual_params_kernel(const ResidualParams p, float *totals)
 {
-    __shared__ float sums[16][SUMS][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, D = p.D, col = blockIdx.x * 64 + lane;
+    __shared__ float scratch[1024 / COLS][SUMS][COLS];
+    const int D = p.D, col = blockIdx.x * COLS + threadIdx.x % COLS;
     const int64_t g = blockIdx.y;
-    float run[SUMS] = {};
-    if (col < D) sum_run<SUMS>(p.workspace + g * p.parts * SUMS * D + col, (int64_t)SUMS * D, D, p.parts, wave, run);
-#pragma unroll
-    for (int i = 0; i < SUMS; ++i) sums[wave][i][lane] = run[i];
-    __syncthreads();
-    if (wave > 0 || col >= D) return;
+    float run[SUMS];
+    sum_columns<COLS, SUMS>(p.workspace + g * p.parts * SUMS * D + col, (int64_t)SUMS * D, D, p.parts, col < D, run, scratch);
+    if (threadIdx.x >= COLS || col >= D) return;
     float s[4] = {};
 #pragma unroll
-    for (int i = 0; i < SUMS; ++i)
-#pragma unroll
-        for (int n = 0; n < 16; ++n) s[i] += sums[n][i][lane];
+    for (int i = 0; i < SUMS; ++i) s[i] = run[i];
     const bool normed1 = p.post.kind != ATB_NORM_NONE;
     auto value = [&](const void *w, int64_t at, float other) { return w ? (float)static_cast<const P *>(w)[at] : other; };
     if (p.dgate) static_cast<P *>(p.dgate)[g * D + col] = (P)(value(normed1 ? p.post.weight : nullptr, col, 1.0f) * s[0] + value(normed1 ? p.post.bias : nullptr, col, 0.0f) * s[2]);
@@ -783,23 +794,17 @@ __global__ void __launch_bounds__(1024) residual_params_kernel(const ResidualPar
     if (p.dpre_bias) static_cast<P *>(p.dpre_bias)[col] = (P)s[3];
 }
 
-// The groups' terms added in order.
+// The groups' terms, one sum to a workgroup.
 template <class P, int SUMS>
 __global__ void __launch_bounds__(1024) residual_groups_kernel(const ResidualParams p, const float *totals)
 {
-    __shared__ float sums[16][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, D = p.D, col = blockIdx.x * 64 + lane, i = blockIdx.y;
+    __shared__ float scratch[16][1][64];
+    const int D = p.D, col = blockIdx.x * 64 + threadIdx.x % 64, i = blockIdx.y;
     P *out = static_cast<P *>(i == 0 ? p.dpost_weight : i == 1 ? p.dpre_weight : i == 2 ? p.dpost_bias : p.dpre_bias);
     if (!out) return;                                         // the whole workgroup
-    float run[1] = {0.0f};
-    if (col < D) sum_run<1>(totals + (int64_t)i * D + col, (int64_t)SUMS * D, 0, p.groups, wave, run);
-    sums[wave][lane] = run[0];
-    __syncthreads();
-    if (wave > 0 || col >= D) return;
-    float s = 0.0f;
-#pragma unroll
-    for (int n = 0; n < 16; ++n) s += sums[n][lane];
-    out[col] = (P)s;
+    float s[1];
+    sum_columns<64, 1>(totals + (int64_t)i * D + col, (int64_t)SUMS * D, 0, (int)p.groups, col < D, s, scratch);
+    if (threadIdx.x < 64 && col < D) out[col] = (P)s[0];
 }
 
 // ---- launches
@@ -853,7 +858,11 @@ hipError_t sums_of(const ResidualParams &p, float *rows, float *totals, hipStrea
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((residual_params_kernel<P, SUMS>), dim3((unsigned)((p.D + 63) / 64), (unsigned)p.groups), dim3(1024), 0, stream, p, totals);
+    // 16 columns to a workgroup where there would be fewer than 32 of 64 columns (us, 64 / 16 columns: 256 parts of 4 sums of 706 columns 18.6 / 6.0, of 2 sums of 4096 5.1 / 9.8; six times 42 parts of 4 sums of 5001 8.5 / 35.8)
+    if ((p.D + 63) / 64 * p.groups < 32)
+        hipLaunchKernelGGL((residual_params_kernel<P, SUMS, 16>), dim3((unsigned)((p.D + 15) / 16), (unsigned)p.groups), dim3(1024), 0, stream, p, totals);
+    else
+        hipLaunchKernelGGL((residual_params_kernel<P, SUMS, 64>), dim3((unsigned)((p.D + 63) / 64), (unsigned)p.groups), dim3(1024), 0, stream, p, totals);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !totals) return e;
     hipLaunchKernelGGL((residual_groups_kernel<P, SUMS>), dim3((unsigned)((p.D + 63) / 64), SUMS), dim3(1024), 0, stream, p, totals);
