@@ -323,13 +323,13 @@ typedef struct atb_linear {
     void *workspace;                            /* DEVICE, 16-byte aligned, of the bytes below for the call; forward also NULL: long reductions of few rows are not shared out */
 } atb_linear;
 
-/* Bytes of the workspace of a forward pass (keeps != 0: one with `slope`) and of a backward pass; 0: none is used, or invalid arguments.  Of a backward pass they
+/* Bytes of the workspace of a forward pass and of a backward pass; 0: none is used, or invalid arguments.  Of a backward pass they
  * hold act'(z) o dy in bf16 (unless act is ATB_ACT_NONE and N a multiple of 8) and sums of it, or of products, in fp32. */
-size_t atb_linear_workspace(int64_t M, int64_t N, int64_t K, int keeps);
+size_t atb_linear_workspace(int64_t M, int64_t N, int64_t K);
 size_t atb_linear_backward_workspace(int64_t M, int64_t N, int64_t K, atb_activation act);
 
-/* residual: DEVICE, M x N bf16 (pitch ldr), or NULL; may be y.  slope: DEVICE, M x N fp16 (pitch N), written with act'(x W^T + bias) for the backward pass, or NULL; with
- * ATB_ACT_NONE there is none.  y: DEVICE, M x N bf16 (pitch ldy).  All three at any element.  Async on hip_stream. */
+/* residual: DEVICE, M x N bf16 (pitch ldr), or NULL; may be y.  slope: DEVICE, M rows of round_up(N, 8) fp16, 16-byte aligned, of which N are written with act'(x W^T + bias)
+ * for the backward pass, or NULL; with ATB_ACT_NONE there is none.  y: DEVICE, M x N bf16 (pitch ldy).  y and residual at any element.  Async on hip_stream. */
 atb_status atb_linear_forward(const atb_linear *l, const void *residual, int64_t ldr, void *slope, void *y, int64_t ldy, void *hip_stream);
 
 /* Gradients of a loss with dy (M x N bf16, pitch lddy): with dz = dy o act'(z), rounded to bf16 for the products,

@@ -214,7 +214,8 @@ def lib() -> ctypes.CDLL:
     L.atb_q4_gated.restype = ci
     L.atb_q4_gated.argtypes = [ctypes.POINTER(Q4), ctypes.POINTER(Q4), ci, vp, i64, vp, i64, i64, vp]
     L.atb_linear_workspace.restype = L.atb_linear_backward_workspace.restype = ctypes.c_size_t
-    L.atb_linear_workspace.argtypes = L.atb_linear_backward_workspace.argtypes = [i64, i64, i64, ci]
+    L.atb_linear_workspace.argtypes = [i64, i64, i64]
+    L.atb_linear_backward_workspace.argtypes = [i64, i64, i64, ci]
     L.atb_linear_forward.restype = L.atb_linear_backward.restype = ci
     L.atb_linear_forward.argtypes = [ctypes.POINTER(Linear), vp, i64, vp, vp, i64, vp]
     L.atb_linear_backward.argtypes = [ctypes.POINTER(Linear), vp, vp, i64, vp, i64, vp, vp, vp]

@@ -512,8 +512,8 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n)
     const c10::DeviceGuard guard(x.device());
     const at::Tensor y = make({l.M, l.N}, at::kBFloat16, x.device());
     std::optional<at::Tensor> slope, work;
-    if (save && act != ATB_ACT_NONE) slope = make({l.M, l.N}, at::kHalf, x.device());
-    const int64_t bytes = (int64_t)room(l.M, l.N, l.K, slope.has_value());
+    if (save && act != ATB_ACT_NONE) slope = make({l.M, (l.N + 7) / 8 * 8}, at::kHalf, x.device());
+    const int64_t bytes = (int64_t)room(l.M, l.N, l.K);
     if (bytes > 0) work = make({bytes}, at::kByte, x.device());
     l.workspace = data<void *>(work);
     int st;
@@ -541,7 +541,7 @@ PyObject *linear_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (!describe(l, x, THPVariable_Unpack(args[4]), bias, slope ? ATB_ACT_SILU : ATB_ACT_NONE)) return refuse();
     const at::Device on = x.device();
     if (!is_rows(dy, at::kBFloat16, l.M, l.N, on)) return refuse();
-    if (slope && (slope->device() != on || slope->scalar_type() != at::kHalf || slope->dim() != 2 || slope->size(0) != l.M || slope->size(1) != l.N || !slope->is_contiguous())) return refuse();
+    if (slope && (slope->device() != on || slope->scalar_type() != at::kHalf || slope->dim() != 2 || slope->size(0) != l.M || slope->size(1) != (l.N + 7) / 8 * 8 || !slope->is_contiguous())) return refuse();
     const c10::DeviceGuard guard(on);
     const at::Tensor dx = make({l.M, l.K}, at::kBFloat16, on), dw = make({l.N, l.K}, at::kBFloat16, on);
     std::optional<at::Tensor> db, work;

@@ -13,7 +13,7 @@ namespace atb {
 struct LinearGradParams {
     const uint16_t *dy;          // M x N bf16, lddy apart, at any element
     int64_t lddy;
-    const uint16_t *slope;       // M x N fp16, or null: 1
+    const uint16_t *slope;       // M rows of round_up(N, 8) in fp16, of which N count, or null: 1
     uint16_t *dz;                // M x round_up(N, 8) bf16, the padding written as zero, or null: not wanted
     float *partial;              // linear_parts(M, N) x N column sums, where dbias is wanted
     void *dbias;                 // N elements of bias_type, or null

@@ -61,19 +61,19 @@ atb::TileParams tiles(void *shares, int64_t M, int64_t N, int64_t K)
 
 }  // namespace
 
-extern "C" size_t atb_linear_workspace(int64_t M, int64_t N, int64_t K, int keeps)
+extern "C" size_t atb_linear_workspace(int64_t M, int64_t N, int64_t K)
 {
-    if (!linear_lengths(M, N, K) || (atb::ffn_streams(M) && !keeps)) return 0;
-    return sizeof(float) * (size_t)atb::tile_shares(M, atb::round_up(N, 8), K, 1, 1, false);
+    if (!linear_lengths(M, N, K) || atb::ffn_streams(M)) return 0;
+    return sizeof(float) * (size_t)atb::tile_shares(M, atb::round_up(N, 8), K, 1, 1, false, true);
 }
 
 extern "C" atb_status atb_linear_forward(const atb_linear *l, const void *residual, int64_t ldr, void *slope, void *y, int64_t ldy, void *hip_stream)
 {
     if (!is_linear(l) || (slope && l->act == ATB_ACT_NONE)) return ATB_ERR_INVALID_ARG;
     if (l->M == 0) return ATB_OK;
-    if (!is_rows(y, l->N, ldy, 2) || (residual && !is_rows(residual, l->N, ldr, 2)) || !aligned(slope, 2)) return ATB_ERR_INVALID_ARG;
+    if (!is_rows(y, l->N, ldy, 2) || (residual && !is_rows(residual, l->N, ldr, 2)) || !aligned(slope, 16)) return ATB_ERR_INVALID_ARG;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (atb::ffn_streams(l->M) && !slope) {
+    if (atb::ffn_streams(l->M)) {
         atb::StreamParams s = {};
         s.w[0] = {l->w, nullptr, nullptr, l->ldw};
         s.x = u16(l->x); s.ldx = l->ldx;
@@ -86,6 +86,7 @@ extern "C" atb_status atb_linear_forward(const atb_linear *l, const void *residu
         s.bias_type = l->bias_type;
         s.residual = u16(residual);
         s.ldr = ldr;
+        s.slope = u16(slope);
         return hip_status(atb::launch_stream(s, stream));
     }
     atb::TileParams p = tiles(l->workspace, l->M, atb::round_up(l->N, 8), l->K);
@@ -118,7 +119,7 @@ extern "C" atb_status atb_linear_backward(const atb_linear *l, const void *slope
     const LinearRoom room = linear_room(M, N, K, l->act);
     if (M > 0) {
         if (!(as_it_is ? is_matrix(dy, N, lddy) : is_rows(dy, N, lddy, 2)) || (dx && !is_matrix(dx, K, lddx))) return ATB_ERR_INVALID_ARG;
-        if ((l->act == ATB_ACT_NONE) != !slope || !aligned(slope, 2)) return ATB_ERR_INVALID_ARG;
+        if ((l->act == ATB_ACT_NONE) != !slope || !aligned(slope, 16)) return ATB_ERR_INVALID_ARG;
         if (!l->workspace && (room.dz || room.partial || room.shares)) return ATB_ERR_INVALID_ARG;
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);

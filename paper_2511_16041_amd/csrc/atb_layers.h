@@ -77,13 +77,13 @@ struct TileParams {
     int segments, problems;
     int act;                     // atb_activation
     float *shares;               // room for tile_shares() floats, or null: reductions are not shared out
-    // a product with its epilogue: N is a multiple of 8, of whose columns the first `edge` exist (0: all); C, residual and slope begin at any element
+    // a product with its epilogue: N is a multiple of 8, of whose columns the first `edge` exist (0: all); C and residual begin at any element
     int edge;
     const void *bias;            // edge elements of bias_type, or null
     int bias_type;               // atb_type
     const uint16_t *residual;    // M x edge, ldr apart, or null
     int64_t ldr;
-    uint16_t *slope;             // kLinearKeep: M x edge in fp16
+    uint16_t *slope;             // kLinearKeep: M rows of round_up(edge, 8) in fp16, 16-byte aligned
     // set by the launch
     int tiles_m, tiles_n, group_m;
     int steps;                   // K-steps of a segment
@@ -112,11 +112,14 @@ static inline TilePlan tile_plan(int64_t M, int64_t N, int tile, bool gated)
 // Two workgroups per CU with small tiles write twice the sums and are slower from M = 128 on (D 8192, F 2048, M 128: 48 forward, 98 backward; with one 40 and 87).
 // Without room for shares (`room`) what is left takes their place: M = 500, D = 4096, F = 14336 275 us forward and 650 backward, with whole reductions in
 // the large tiles that their shares would have had 417 and 973.
-struct TileChoice { bool large; int parts; };
-static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated, bool room)
+// Products with an epilogue (`linear`) have tiles of 128 x 256 too, one per CU, where these are no more than CUs and small ones would be two to some of them.  us, these / what the rules above choose: 2048 x 4096 x 4096 62
+// / 80 (large ones in two shares), 1500 x 5008 x 2056 39 / 47, 1100 x 4096 x 4096 54 / 57, 2048 x 3500 x 1024 20.8 / 21.8.
+struct TileChoice { bool large; int parts; bool wide = false; };
+static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated, bool room, bool linear = false)
 {
     const TilePlan large = tile_plan(M, N, 256, gated), small = tile_plan(M, N, 128, gated);
     if ((int64_t)large.tiles_m * large.tiles_n * problems >= 192) return {true, 1};
+    if (linear && (int64_t)small.tiles_m * small.tiles_n > 256 && (int64_t)small.tiles_m * large.tiles_n <= 256) return {false, 1, true};
     if (!room) return {false, 1};
     const int64_t steps = (K + 63) / 64 * segments, tiles = (int64_t)small.tiles_m * small.tiles_n * problems;
     const int64_t few = (int64_t)large.tiles_m * large.tiles_n * problems, each = 256 / std::max<int64_t>(few, 1);
@@ -124,9 +127,9 @@ static inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, int segme
     const int64_t parts = std::min(256 / std::max<int64_t>(tiles, 1), steps / 8);
     return {false, parts > 1 ? (int)parts : 1};
 }
-static inline int64_t tile_shares(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated)
+static inline int64_t tile_shares(int64_t M, int64_t N, int64_t K, int segments, int problems, bool gated, bool linear = false)
 {
-    const TileChoice c = choose_tiles(M, N, K, segments, problems, gated, true);
+    const TileChoice c = choose_tiles(M, N, K, segments, problems, gated, true, linear);
     return c.parts > 1 ? c.parts * (gated ? 2 : problems) * M * N : 0;
 }
 // The products of the forward pass (A and B with K contiguous): epilogue kStore, kGated or kGatedKeep.
@@ -165,6 +168,7 @@ struct StreamParams {
     int bias_type;
     const uint16_t *residual;    // M x N, ldr apart, or null
     int64_t ldr;
+    uint16_t *slope;             // M rows of round_up(N, 8) in fp16: act'(x W^T + bias), or null
 };
 hipError_t launch_stream(const StreamParams &p, hipStream_t stream);
 hipError_t launch_q4_stream(const StreamParams &p, hipStream_t stream);      // 4 bits; launch_stream calls it

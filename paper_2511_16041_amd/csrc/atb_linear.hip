@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradParams
             float d[8] = {};
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e < p.N) d[e] = (float)dy[row * p.lddy + e] * (SLOPE ? (float)slope[row * p.N + e] : 1.0f);
+                if (e < p.N) d[e] = (float)dy[row * p.lddy + e] * (SLOPE ? (float)slope[row * pitch + e] : 1.0f);
             add(row, d, p.N);
         }
     } else {
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradParams
             const bf16x8 g = *reinterpret_cast<const Eight<__bf16>::any *>(dy + row * p.lddy);
             float d[8];
             if constexpr (SLOPE) {
-                const Eight<_Float16>::vec s = *reinterpret_cast<const Eight<_Float16>::any *>(slope + row * p.N);
+                const Eight<_Float16>::vec s = *reinterpret_cast<const Eight<_Float16>::any *>(slope + row * pitch);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) d[e] = (float)g[e] * (float)s[e];
             } else {

@@ -70,7 +70,13 @@ ATB_DEV void finish_rows(const StreamParams &p, const floatx4 (&acc)[MB][NB], fl
         if (!GATED && p.linear) {
             const int n = n0 + col;
             if (p.bias) v += p.bias_type == ATB_TYPE_F32 ? static_cast<const float *>(p.bias)[n] : (float)static_cast<const __bf16 *>(p.bias)[n];
-            with_activation_or_none(p.act, [&](auto a) { v = activate<decltype(a)::value>(v); });
+            if (p.slope) {
+                float slope = 0.0f;
+                with_activation(p.act, [&](auto a) { activate_grad<decltype(a)::value>(v, v, slope); });
+                reinterpret_cast<_Float16 *>(p.slope)[(int64_t)(m0 + row) * ((p.N + 7) & ~7) + n] = (_Float16)slope;
+            } else {
+                with_activation_or_none(p.act, [&](auto a) { v = activate<decltype(a)::value>(v); });
+            }
             if (p.residual) v += (float)reinterpret_cast<const __bf16 *>(p.residual)[(m0 + row) * p.ldr + n];
         }
         const int64_t to = (int64_t)(m0 + row) * p.ldy + n0 + col;

@@ -563,8 +563,8 @@ struct Tile {
         }
     }
 
-    // ---- the epilogue of a product: act(sum + bias) + residual.  Pieces of eight columns, the residual's AHEAD of them on their way.  Of C, residual and slope the
-    // rows begin at any element, and the last piece of a row may be cut.
+    // ---- the epilogue of a product: act(sum + bias) + residual, in pieces of eight columns.  The residual's are all asked for ahead of the first store: a wait for a load is one for the stores before it too (6061 x
+    // 9088 x 440 with residual and slope, four pieces ahead 159 us, where either alone took 102).  Rows of C and residual begin at any element, and their last piece may be cut; the slope's are padded to multiples of 8.
 
     // Columns col .. col + 7 of a row of p.edge; 0 past its end
     template <class T>
@@ -614,8 +614,13 @@ struct Tile {
 
     ATB_DEV void finish_linear()
     {
-        constexpr int PIECES = S::MI * S::NI / 2, AHEAD = 4;
+        constexpr int PIECES = S::MI * S::NI / 2;
         const int row0 = m0 + wm * (S::TM / S::WM) + (lane & 15), col0 = n0 + wn * 64 + piece_col();
+        bf16x8 res[PIECES] = {};
+        if (p.residual) {
+#pragma unroll
+            for (int n = 0; n < PIECES; ++n) res[n] = load_residual(here(row0 + 16 * (n / (S::NI / 2))), col0 + 32 * (n % (S::NI / 2)));
+        }
         float bias[S::NI / 2][8] = {};
         if (p.bias) {
 #pragma unroll
@@ -624,12 +629,8 @@ struct Tile {
                 else load_eight(static_cast<const __bf16 *>(p.bias), col0 + 32 * j, bias[j]);
             }
         }
-        bf16x8 res[AHEAD] = {};
-        if (p.residual) {
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) res[n] = load_residual(row0 + 16 * (n / (S::NI / 2)), col0 + 32 * (n % (S::NI / 2)));
-        }
         __builtin_amdgcn_sched_barrier(0);
+        const int pitch = (p.edge + 7) & ~7;
 #pragma unroll
         for (int n = 0; n < PIECES; ++n) {
             const int i = n / (S::NI / 2), j = n % (S::NI / 2);
@@ -655,13 +656,18 @@ struct Tile {
             }
             if (p.residual) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += (float)res[n % AHEAD][e];
+                for (int e = 0; e < 8; ++e) v[e] += (float)res[n][e];
             }
             if (row < p.M) {
                 store_eight(reinterpret_cast<__bf16 *>(p.C[0]) + (int64_t)row * p.ldc, col, v);
-                if constexpr (EPI == kLinearKeep) store_eight(reinterpret_cast<_Float16 *>(p.slope) + (int64_t)row * p.edge, col, slope);
+                if constexpr (EPI == kLinearKeep) {
+                    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+                    half8 w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = (_Float16)slope[e];
+                    if (col < pitch) *reinterpret_cast<half8 *>(p.slope + (int64_t)row * pitch + col) = w;
+                }
             }
-            if (n + AHEAD < PIECES && p.residual) res[n % AHEAD] = load_residual(here(row0 + 16 * ((n + AHEAD) / (S::NI / 2))), col0 + 32 * ((n + AHEAD) % (S::NI / 2)));
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -763,7 +769,7 @@ __global__ void __launch_bounds__(256) join_kernel(const TileParams p)
             if (e < cols) {
                 if (p.residual) v[e] += (float)reinterpret_cast<const __bf16 *>(p.residual)[row * p.ldr + col + e];
                 reinterpret_cast<__bf16 *>(p.C[0])[to + e] = (__bf16)v[e];
-                if constexpr (EPI == kLinearKeep) reinterpret_cast<_Float16 *>(p.slope)[(int64_t)row * p.edge + col + e] = (_Float16)slope[e];
+                if constexpr (EPI == kLinearKeep) reinterpret_cast<_Float16 *>(p.slope)[(int64_t)row * ((p.edge + 7) & ~7) + col + e] = (_Float16)slope[e];
             }
     } else if constexpr (EPI == kStore) {
         bf16x4 c;
@@ -812,13 +818,13 @@ __global__ void __launch_bounds__(256) join_kernel(const TileParams p)
 
 typedef TileShape<256, 256, 2, 4> Tile256;
 typedef TileShape<128, 128, 2, 2> Tile128;
+typedef TileShape<128, 256, 2, 4> Tile128x256;
 
 template <class S, bool AT, bool BROWS, int EPI>
 hipError_t launch_shape(TileParams &p, hipStream_t stream)
 {
-    const TilePlan plan = tile_plan(p.M, p.N, S::TM, is_gated(EPI));
-    p.tiles_m = plan.tiles_m;
-    p.tiles_n = plan.tiles_n;
+    p.tiles_m = tile_plan(p.M, p.N, S::TM, is_gated(EPI)).tiles_m;
+    p.tiles_n = tile_plan(p.M, p.N, S::TN, is_gated(EPI)).tiles_n;
     p.group_m = 2048 / S::TM;
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n * p.parts;
     if (total > 0x7fffff00) return hipErrorInvalidConfiguration;
@@ -829,12 +835,14 @@ hipError_t launch_shape(TileParams &p, hipStream_t stream)
 template <bool AT, bool BROWS, int EPI>
 hipError_t launch_tiles(TileParams &p, hipStream_t stream)
 {
-    const TileChoice how = choose_tiles(p.M, p.N, p.K, p.segments, p.problems, is_gated(EPI), p.shares != nullptr);
+    const TileChoice how = choose_tiles(p.M, p.N, p.K, p.segments, p.problems, is_gated(EPI), p.shares != nullptr, is_linear(EPI));
     p.steps = (p.K + 63) / 64;
     p.planes = is_gated(EPI) ? 2 : p.problems;
     if (p.edge == 0) p.edge = p.N;
     p.parts = how.parts;
     constexpr int SHARE = is_gated(EPI) ? kGatedShare : kShare;
+    if constexpr (is_linear(EPI))
+        if (how.wide) return launch_shape<Tile128x256, AT, BROWS, EPI>(p, stream);
     if (p.parts == 1) return how.large ? launch_shape<Tile256, AT, BROWS, EPI>(p, stream) : launch_shape<Tile128, AT, BROWS, EPI>(p, stream);
     hipError_t e;
     if constexpr (is_gated(EPI)) e = launch_shape<Tile128, AT, BROWS, SHARE>(p, stream);           // (their shares are never large tiles)

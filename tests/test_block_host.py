@@ -24,9 +24,9 @@ def test_linear_refuses():
         return L.atb_linear_backward(ctypes.byref(l), slope, dy, lddy, dx, lddx, dw, db, None)
     shared = [dict(x=None), dict(w=None), dict(x=a + 2), dict(w=a + 8), dict(ldx=15), dict(ldx=20), dict(ldx=8), dict(ldw=8), dict(ldw=2 ** 22), dict(bias=a + 1), dict(bias=a + 2, bias_type=1), dict(M=-1),
               dict(M=2 ** 23 + 1), dict(N=0), dict(N=-1), dict(N=2 ** 22 - 7), dict(K=0), dict(K=12), dict(K=2 ** 22), dict(act=4), dict(act=-1), dict(bias_type=2), dict(workspace=a + 8)]
-    for bad in shared + [dict(y=None), dict(y=a + 1), dict(ldy=6), dict(residual=a + 1), dict(ldr=6), dict(slope=a + 1), dict(act=3)]:
+    for bad in shared + [dict(y=None), dict(y=a + 1), dict(ldy=6), dict(residual=a + 1), dict(ldr=6), dict(slope=a + 2), dict(act=3)]:
         assert forward(**bad) == INVALID, bad
-    for bad in shared + [dict(dy=None), dict(dy=a + 1), dict(lddy=6), dict(slope=None), dict(act=3), dict(slope=a + 1), dict(dx=a + 2), dict(lddx=15), dict(lddx=8), dict(dw=a + 8), dict(db=a + 1),
+    for bad in shared + [dict(dy=None), dict(dy=a + 1), dict(lddy=6), dict(slope=None), dict(act=3), dict(slope=a + 8), dict(dx=a + 2), dict(lddx=15), dict(lddx=8), dict(dw=a + 8), dict(db=a + 1),
                          dict(db=a + 2, bias_type=1), dict(workspace=None), dict(act=3, slope=None, N=8, lddy=9), dict(act=3, slope=None, N=8, lddy=8, dy=a + 2)]:
         assert backward(**bad) == INVALID, bad
     assert L.atb_linear_forward(None, a, 7, a, a, 7, None) == INVALID and L.atb_linear_backward(None, a, a, 7, a, 16, a, a, None) == INVALID
@@ -43,13 +43,13 @@ def test_workspace_of_a_product_with_its_epilogue():
     for M in (1, 33, 100, 1000, 8192):
         for N in (1, 1031, 14336):
             for K in (8, 1032, 4096):
-                assert L.atb_linear_workspace(M, N, K, 0) <= L.atb_linear_workspace(M, N, K, 1) <= 64 << 20
+                assert L.atb_linear_workspace(M, N, K) <= 64 << 20
                 dz = 2 * M * (N + 7 & -8)
                 assert L.atb_linear_backward_workspace(M, N, K, 0) >= dz + 4 * N
                 assert L.atb_linear_backward_workspace(M, N, K, 3) >= (dz if N % 8 else 0) + 4 * N
     assert L.atb_linear_backward_workspace(8192, 14336, 4096, 3) < 64 << 20
     for bad in ((-1, 64, 64), (1, 0, 64), (1, 64, 60), (2 ** 23 + 1, 64, 64), (1, 64, 2 ** 22), (1, 2 ** 22, 64)):
-        assert L.atb_linear_workspace(*bad, 1) == 0 and L.atb_linear_backward_workspace(*bad, 0) == 0
+        assert L.atb_linear_workspace(*bad) == 0 and L.atb_linear_backward_workspace(*bad, 0) == 0
     assert L.atb_linear_backward_workspace(4, 64, 64, 4) == 0
 
 
