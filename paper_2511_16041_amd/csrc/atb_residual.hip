@@ -854,6 +854,7 @@ hipError_t sums_of(const ResidualParams &p, float *rows, float *totals, hipStrea
 {
     if (p.M > 0 && residual_is_long(p.D)) {
         const int64_t blocks = (p.D + 256 * E - 1) / (256 * E);
+        if (blocks * p.groups * p.parts > 0xffffff) return hipErrorInvalidConfiguration;       // (2^32 threads: operands of 64 GiB each)
         hipLaunchKernelGGL((residual_columns_kernel<X, Z, P, SUMS>), dim3((unsigned)(blocks * p.groups * p.parts)), dim3(256), 0, stream, p, (int)blocks, rows);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -1,5 +1,8 @@
 """The operators of a block around its feed-forward sublayer without a GPU: what their entry points refuse, sizes of workspaces, and the gradients' formulas against differences."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 
@@ -239,3 +242,22 @@ def test_moe_refuses_tensors_that_a_kernel_would_read_or_store_past():
         atb.moe_feed_forward(x, r, up, up, down, 2, "swish")
     with pytest.raises(TypeError):
         atb.moe_feed_forward(x, r, up, None, down)
+
+
+# ------------------------------------------------------------------ the host code under sanitizers
+
+def test_the_host_code_is_clean_under_asan_and_ubsan(tmp_path):
+    """atb_block_api.cpp and the rules of atb_block.h, which decide the sizes of buffers that kernels write."""
+    from test_host_sanitizers import CSRC, NATIVE, ROCM_INC, ROOT
+    if shutil.which("g++") is None or not os.path.isdir(ROCM_INC):
+        pytest.skip("needs g++ and the HIP headers")
+    exe = str(tmp_path / "sanitize_block")
+    san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-static-libasan", "-static-libubsan", "-fno-omit-frame-pointer", "-g", "-O1"]
+    subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I", ROCM_INC, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-Wno-deprecated-declarations",
+                    os.path.join(NATIVE, "sanitize_block.cpp"), os.path.join(NATIVE, "stub_device.cpp"), os.path.join(CSRC, "atb_api.cpp"), os.path.join(CSRC, "atb_model.cpp"),
+                    os.path.join(CSRC, "atb_block_api.cpp"), "-o", exe, "-lm"] + san, check=True)
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([exe], env=env, capture_output=True, text=True, timeout=120)
+    out = r.stdout + r.stderr
+    assert r.returncode == 0 and "sanitize_block: ok" in r.stdout, out
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out
