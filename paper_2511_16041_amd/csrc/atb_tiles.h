@@ -827,7 +827,7 @@ hipError_t launch_shape(TileParams &p, hipStream_t stream)
     p.tiles_n = tile_plan(p.M, p.N, S::TN, is_gated(EPI)).tiles_n;
     p.group_m = 2048 / S::TM;
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n * p.parts;
-    if (total > 0x7fffff00) return hipErrorInvalidConfiguration;
+    if (total > 0xffffff00u / S::NT) return hipErrorInvalidConfiguration;      // 2^32 threads: a result of 2^36 elements or more
     hipLaunchKernelGGL((tile_kernel<S, AT, BROWS, EPI>), dim3((unsigned)((total + 7) / 8 * 8), p.problems), dim3(S::NT), 0, stream, p);
     return hipGetLastError();
 }
