@@ -89,31 +89,17 @@ __global__ void __launch_bounds__(1024) moe_plan_kernel(const MoeParams p, int r
                 for (int i = 0; i < PER; ++i) rank[i] += other > key[i] || (other == key[i] && 64 * o + j < 64 * i + lane);
             }
         }
-        // exp(l - the largest l), summed over all experts or over the chosen ones; a NaN or an infinity among the summands gives what the formula gives
-        double top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) top = fmax(top, key[i]);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) top = fmax(top, __shfl_xor(top, d));
-        float part[PER], sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const bool live = 64 * i + lane < p.E, taken = live && rank[i] < p.k;
-            part[i] = live ? expf((float)(mine[i] - top)) : 0.0f;
-            if (p.renormalize ? taken : live) sum += part[i];
-        }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+        float weight[PER];
+        moe_weights(p, mine, rank, weight);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = 64 * i + lane;
             if (e >= p.E || rank[i] >= p.k) continue;
-            const float s = part[i] / sum;
             chosen[t][rank[i]] = e;
-            share[t][rank[i]] = s;
+            share[t][rank[i]] = weight[i];
             atomicOr(&tokens[e], 1ull << t);                   // (bits: no order)
             if (p.experts) p.experts[t * p.k + rank[i]] = e;
-            if (p.weights) p.weights[t * p.k + rank[i]] = s;
+            if (p.weights) p.weights[t * p.k + rank[i]] = weight[i];
         }
     }
     __syncthreads();
@@ -159,30 +145,32 @@ template <class S>
 __global__ void __launch_bounds__(S::W * 64) moe_gated_kernel(const MoeParams p)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
-    if ((int)blockIdx.y >= p.plan->segments) return;
-    const MoeSegment seg = moe_segment(p.plan, blockIdx.y);
+    static_assert(S::W == 4 && S::LDS_BYTES >= 12 * kMoeExperts, "moe_choose_one");
+    MoeSegment seg;
+    if (!moe_open<S::XQ == 1>(p, lds, seg)) return;
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.F - n0, 16 * S::COLS);
     const int64_t at = ((int64_t)seg.expert * p.F + n0) * p.D;
     const StreamView view = {p.x, p.ldx, p.M, seg.rows, {static_cast<const uint16_t *>(p.gate.w) + at, static_cast<const uint16_t *>(p.up.w) + at}, {p.D, p.D}, cols, p.D};
     const int *tokens = p.plan->token + seg.first;
-    Stream<S> s(view, (unsigned)reinterpret_cast<uintptr_t>(lds), [&](int row) { return tokens[row]; });
+    Stream<S> s(view, (unsigned)reinterpret_cast<uintptr_t>(lds), [&](int row) { return S::XQ == 1 && p.M == 1 ? 0 : tokens[row]; });
     s.run();
     finish_rows<S::MB, S::NB, S::W, true>(moe_inner(p, seg), s.acc, reinterpret_cast<float *>(lds), 0, n0, cols);
 }
 
 // Workgroup (x, y): 16 columns of y, share y of the reduction.
 template <class S>
-__global__ void __launch_bounds__(S::W * 64) moe_down_kernel(const MoeParams p)
+__global__ void __launch_bounds__(S::W * 64) moe_down_kernel(const MoeParams p, int segments)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
-    extern __shared__ float totals[];                              // [W][M][16 NB]
-    const MoePlan *plan = p.plan;
+    extern __shared__ float totals[];                              // [W][M][16 NB], and the plan of at most `segments`
+    const MoeCopy plan = moe_copy(p.plan, reinterpret_cast<int *>(totals + S::W * p.M * 16 * S::NB), segments, p.M * p.k);
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.D - n0, 16 * S::COLS);
     auto view_of = [&](const MoeSegment &seg) {
         return StreamView{p.h + (int64_t)seg.first * p.F, p.F, seg.rows, seg.rows, {static_cast<const uint16_t *>(p.down.w) + ((int64_t)seg.expert * p.D + n0) * p.F, nullptr}, {p.F, 0}, cols, p.F};
     };
     auto row_of = [](int row) { return row; };
-    const int panels = (p.F + S::K - 1) / S::K, all = __builtin_amdgcn_readfirstlane(plan->segments) * panels;
+    const int panels = (p.F + S::K - 1) / S::K, all = __builtin_amdgcn_readfirstlane(p.plan->segments) * panels;
+    __syncthreads();
     const int first = (int)((int64_t)all * blockIdx.y / p.shares), end = (int)((int64_t)all * (blockIdx.y + 1) / p.shares);
     Stream<S> s(view_of(moe_segment(plan, 0)), (unsigned)reinterpret_cast<uintptr_t>(lds), row_of);
     float *mine = totals + s.wave * p.M * 16 * S::NB;
@@ -248,7 +236,7 @@ hipError_t launch_products(const MoeParams &p, hipStream_t stream)
     hipLaunchKernelGGL((moe_gated_kernel<Gated>), dim3((unsigned)((p.F + 15) / 16), (unsigned)segments), dim3(Gated::W * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((moe_down_kernel<Down>), dim3((unsigned)((p.D + 15) / 16), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 16 * sizeof(float), stream, p);
+    hipLaunchKernelGGL((moe_down_kernel<Down>), dim3((unsigned)((p.D + 15) / 16), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 16 * sizeof(float) + moe_copy_bytes(segments, p.M * p.k), stream, p, segments);
     return hipGetLastError();
 }
 
@@ -262,11 +250,13 @@ hipError_t launch_moe(const MoeParams &p, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int rows = p.group ? 16 : moe_rows(p.M, p.E, p.k);
-    if (p.E <= 64) hipLaunchKernelGGL(moe_plan_kernel<1>, dim3(1), dim3(1024), 0, stream, p, rows);
-    else if (p.E <= 128) hipLaunchKernelGGL(moe_plan_kernel<2>, dim3(1), dim3(1024), 0, stream, p, rows);
-    else hipLaunchKernelGGL(moe_plan_kernel<4>, dim3(1), dim3(1024), 0, stream, p, rows);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (p.M > 1) {                                                 // (a single token's choice: moe_choose_one)
+        if (p.E <= 64) hipLaunchKernelGGL(moe_plan_kernel<1>, dim3(1), dim3(1024), 0, stream, p, rows);
+        else if (p.E <= 128) hipLaunchKernelGGL(moe_plan_kernel<2>, dim3(1), dim3(1024), 0, stream, p, rows);
+        else hipLaunchKernelGGL(moe_plan_kernel<4>, dim3(1), dim3(1024), 0, stream, p, rows);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if (p.group) e = launch_moe_q4(p, stream);
     else if (rows == 32) e = launch_products<2, 4>(p, stream);
     else e = p.M <= 8 ? launch_products<1, 1>(p, stream) : launch_products<1, 2>(p, stream);

@@ -8,29 +8,31 @@ namespace {
 template <class S>
 __global__ void __launch_bounds__(S::W * 64, S::NB > 2 ? 2 : 4) moe_q4_gated_kernel(const MoeParams p)
 {
-    __shared__ float lds[S::W * S::NB * 256];
-    if ((int)blockIdx.y >= p.plan->segments) return;
-    const MoeSegment seg = moe_segment(p.plan, blockIdx.y);
+    __shared__ __attribute__((aligned(16))) float lds[S::W * S::NB * 256];
+    static_assert(S::W == 4 && sizeof(lds) >= 12 * kMoeExperts, "moe_choose_one");
+    MoeSegment seg;
+    if (!moe_open<S::NB == 2>(p, reinterpret_cast<char *>(lds), seg)) return;
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.F - n0, 16 * S::COLS);
     const int64_t n = (int64_t)seg.expert * p.F + n0;
     const Q4View view = {p.x, p.ldx, p.M, seg.rows, {q4_columns(p.gate, n, p.D, S::G), q4_columns(p.up, n, p.D, S::G)}, cols, p.D};
     const int *tokens = p.plan->token + seg.first;
     Q4Stream<S> s(view);
-    s.run([&] { s.open_rows(view, [&](int row) { return tokens[row]; }); });
+    s.run([&] { s.open_rows(view, [&](int row) { return S::NB == 2 && p.M == 1 ? 0 : tokens[row]; }); });
     finish_rows<1, S::NB, S::W, true>(moe_inner(p, seg), s.acc, lds, 0, n0, cols);
 }
 
 template <class S>
-__global__ void __launch_bounds__(S::W * 64, 2) moe_q4_down_kernel(const MoeParams p)
+__global__ void __launch_bounds__(S::W * 64, 2) moe_q4_down_kernel(const MoeParams p, int segments)
 {
-    extern __shared__ float totals[];                              // [W][M][16 NB]
-    const MoePlan *plan = p.plan;
+    extern __shared__ float totals[];                              // [W][M][16 NB], and the plan of at most `segments`
+    const MoeCopy plan = moe_copy(p.plan, reinterpret_cast<int *>(totals + S::W * p.M * 16 * S::NB), segments, p.M * p.k);
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.D - n0, 16 * S::COLS);
     auto view_of = [&](const MoeSegment &seg) {
         return Q4View{p.h + (int64_t)seg.first * p.F, p.F, seg.rows, seg.rows, {q4_columns(p.down, (int64_t)seg.expert * p.D + n0, p.F, S::G), {}}, cols, p.F};
     };
     auto row_of = [](int row) { return row; };
-    const int panels = (p.F + kQ4PanelK - 1) / kQ4PanelK, all = __builtin_amdgcn_readfirstlane(plan->segments) * panels;
+    const int panels = (p.F + kQ4PanelK - 1) / kQ4PanelK, all = __builtin_amdgcn_readfirstlane(p.plan->segments) * panels;
+    __syncthreads();
     const int first = (int)((int64_t)all * blockIdx.y / p.shares), end = (int)((int64_t)all * (blockIdx.y + 1) / p.shares);
     Q4Stream<S> s(view_of(moe_segment(plan, 0)));
     float *mine = totals + s.wave * p.M * 16 * S::NB;
@@ -87,7 +89,7 @@ hipError_t launch_group(const MoeParams &p, hipStream_t stream)
     else hipLaunchKernelGGL((moe_q4_gated_kernel<GatedWide>), dim3((unsigned)((p.F + 31) / 32), segments), dim3(GatedWide::W * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((moe_q4_down_kernel<Down>), dim3((unsigned)((p.D + 31) / 32), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 32 * sizeof(float), stream, p);
+    hipLaunchKernelGGL((moe_q4_down_kernel<Down>), dim3((unsigned)((p.D + 31) / 32), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 32 * sizeof(float) + moe_copy_bytes((int)segments, p.M * p.k), stream, p, (int)segments);
     return hipGetLastError();
 }
 
