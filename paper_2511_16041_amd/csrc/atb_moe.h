@@ -2,6 +2,7 @@
 #pragma once
 
 #include "atb_block.h"
+#include "atb_row.h"
 #include "atb_stream.h"
 
 namespace atb {
@@ -43,8 +44,7 @@ ATB_DEV void moe_weights(const MoeParams &p, const double (&mine)[PER], const in
     double top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PER; ++i) top = fmax(top, mine[i]);        // (of a NaN and a number the number)
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = fmax(top, __shfl_xor(top, d));
+    top = lanes_max(top);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -52,8 +52,7 @@ ATB_DEV void moe_weights(const MoeParams &p, const double (&mine)[PER], const in
         weight[i] = live ? expf((float)(mine[i] - top)) : 0.0f;
         if (p.renormalize ? taken : live) sum += weight[i];
     }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    sum = lanes_sum(sum);
 #pragma unroll
     for (int i = 0; i < PER; ++i) weight[i] /= sum;
 }

@@ -116,23 +116,6 @@ ATB_DEV Raw<P> param(const void *w, int64_t row, const Span &s, int D, float oth
     return v;
 }
 
-// v summed over the wave, in every lane.  Among the 16 lanes of a row by swaps in the registers themselves: a shuffle goes through LDS, six of them one after the other take 800 cycles, and two such sums in a
-// row of 7000 cycles were a third of the backward pass.
-template <int control>
-ATB_DEV float swapped(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), control, 0xF, 0xF, true)); }
-ATB_DEV float lanes_sum(float v)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    v += swapped<0xB1>(v);           // lanes 1 0 3 2 of every four
-    v += swapped<0x4E>(v);           // 2 3 0 1
-    v += swapped<0x141>(v);          // 7 .. 0 of every eight
-    v += swapped<0x140>(v);          // 15 .. 0 of every row
-    const int w = __float_as_int(v);
-    v = (__int_as_float(__builtin_amdgcn_readlane(w, 0)) + __int_as_float(__builtin_amdgcn_readlane(w, 16))) + (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
-#endif
-    return v;
-}
-
 // The sums of a row over its threads; two areas of scratch in turns, so that one barrier is enough
 template <int T, int NT>
 struct RowSums {

@@ -1,4 +1,4 @@
-// What the kernels that hold a row in registers share (atb_norm.hip, atb_residual.hip): 16-byte pieces of rows that begin at any element, and sums over the threads of a row.
+// What the kernels that hold a row in registers share (atb_norm.hip, atb_residual.hip): 16-byte pieces of rows that begin at any element, sums over the threads of a row; sums over a wave (also atb_moe.hip).
 #pragma once
 
 #include "atb_device.h"
@@ -109,6 +109,47 @@ ATB_DEV void row_sums(float (&v)[N], float *scratch)
             v[i] = s;
         }
     }
+}
+
+// v summed over the wave, in every lane.  Among the 16 lanes of a row by swaps in the registers themselves: a shuffle goes through LDS, six of them one after the other take 800 cycles, and two such sums in a
+// row of 7000 cycles were a third of the residual norm's backward pass.
+template <int control>
+ATB_DEV float swapped(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), control, 0xF, 0xF, true)); }
+ATB_DEV float lanes_sum(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    v += swapped<0xB1>(v);           // lanes 1 0 3 2 of every four
+    v += swapped<0x4E>(v);           // 2 3 0 1
+    v += swapped<0x141>(v);          // 7 .. 0 of every eight
+    v += swapped<0x140>(v);          // 15 .. 0 of every row
+    const int w = __float_as_int(v);
+    v = (__int_as_float(__builtin_amdgcn_readlane(w, 0)) + __int_as_float(__builtin_amdgcn_readlane(w, 16))) + (__int_as_float(__builtin_amdgcn_readlane(w, 32)) + __int_as_float(__builtin_amdgcn_readlane(w, 48)));
+#endif
+    return v;
+}
+
+// The greatest over the wave, in every lane; the same way.  v: no NaN
+template <int control>
+ATB_DEV double swapped(double v)
+{
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), control, 0xF, 0xF, true), hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), control, 0xF, 0xF, true);
+    return __hiloint2double(hi, lo);
+}
+ATB_DEV double of_lane(double v, int from)
+{
+    const unsigned lo = __builtin_amdgcn_readlane(__double2loint(v), from), hi = __builtin_amdgcn_readlane(__double2hiint(v), from);
+    return __hiloint2double((int)hi, (int)lo);
+}
+ATB_DEV double lanes_max(double v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    v = fmax(v, swapped<0xB1>(v));
+    v = fmax(v, swapped<0x4E>(v));
+    v = fmax(v, swapped<0x141>(v));
+    v = fmax(v, swapped<0x140>(v));
+    v = fmax(fmax(of_lane(v, 0), of_lane(v, 16)), fmax(of_lane(v, 32), of_lane(v, 48)));
+#endif
+    return v;
 }
 
 }  // namespace atb
