@@ -32,6 +32,24 @@ static inline int64_t linear_parts(int64_t M, int64_t N)
     return std::max(wanted, (M + 511) / 512);
 }
 
+// The tiles in which both products of the backward pass of M rows, N columns and K inputs run in one launch (atb_linear_pair.hip), or 0: each in its own.  A launch of tiles takes as long as its longest reduction
+// or as all K-steps of 64 over 256 CUs, us per K-step of a tile of 256 x 256 1.3 and 1.65, of 128 x 128 0.6 and 0.53: the smaller time chooses the tiles.  By themselves the products may have their reductions in
+// shares, and where dx has few tiles and a long reduction that is faster: up to 1.35 times what large tiles take without idle CUs, or 32 K-steps, the pair is.  us, in one launch / by themselves: 1500 x 5000 x 2056
+// 92 / 102, 5000 x 5000 x 1000 116 / 168, 4096 x 4096 x 2048 108 / 152, 2048 x 2048 x 2048 37 / 44, 1000 x 2000 x 1000 21 / 39, 100 x 1000 x 4000 14 / 19, 1024 x 11008 x 4096 183 / 196, 2048 x 8192 x 2048 141 / 133,
+// 4096 x 4096 x 4096 213 / 214; not taken: 1024 x 8192 x 2048 84 / 79, 512 x 14336 x 4096 162 / 156, 64 x 4096 x 4096 36 / 26.
+static inline int linear_pair(int64_t M, int64_t N, int64_t K)
+{
+    const double dx = (double)((N + 63) / 64), dw = (double)((M + 63) / 64), longest = std::max(dx, dw);
+    auto all = [&](int tile) {
+        const TilePlan x = tile_plan(M, K, tile, false), w = tile_plan(N, K, tile, false);
+        return ((double)x.tiles_m * x.tiles_n * dx + (double)w.tiles_m * w.tiles_n * dw) / 256;
+    };
+    const double large = std::max(1.3 * longest, 1.65 * all(256)), small = std::max(0.6 * longest, 0.53 * all(128));
+    if (longest > 32 && std::min(large, small) > 1.35 * 1.65 * all(256)) return 0;
+    return large <= small ? 256 : 128;
+}
+hipError_t launch_tiles_pair(TileParams dx, TileParams dw, int tile, hipStream_t stream);
+
 // ---- norms on both sides of a residual sum (atb_residual.hip)
 
 struct NormSpec {

@@ -138,22 +138,18 @@ extern "C" atb_status atb_linear_backward(const atb_linear *l, const void *slope
     atb_status st = hip_status(atb::launch_linear_grad(g, stream));
     const uint16_t *dz = as_it_is ? u16(dy) : u16(static_cast<const void *>(work));
     const int64_t lddz = M == 0 ? atb::round_up(N, 8) : as_it_is ? lddy : atb::round_up(N, 8);       // (no tokens: no K-steps, and nothing of the operands is read)
-    if (st == ATB_OK && M > 0 && dx) {
-        atb::TileParams p = tiles(shares, M, K, N);
-        p.A[0] = dz; p.lda[0] = lddz;
-        p.B[0] = u16(l->w); p.ldb[0] = l->ldw;
-        p.C[0] = u16(dx);
-        p.ldc = lddx;
-        st = hip_status(atb::launch_tiles_dx(p, atb::kStore, stream));
-    }
-    if (st == ATB_OK && dw) {
-        atb::TileParams p = tiles(shares, N, K, M);
-        p.A[0] = dz; p.lda[0] = lddz;
-        p.B[0] = u16(l->x); p.ldb[0] = M > 0 ? l->ldx : K;
-        p.C[0] = u16(dw);
-        p.ldc = K;
-        st = hip_status(atb::launch_tiles_dw(p, stream));
-    }
+    atb::TileParams px = tiles(shares, M, K, N), pw = tiles(shares, N, K, M);
+    px.A[0] = pw.A[0] = dz; px.lda[0] = pw.lda[0] = lddz;
+    px.B[0] = u16(l->w); px.ldb[0] = l->ldw;
+    px.C[0] = u16(dx);
+    px.ldc = lddx;
+    pw.B[0] = u16(l->x); pw.ldb[0] = M > 0 ? l->ldx : K;
+    pw.C[0] = u16(dw);
+    pw.ldc = K;
+    const int together = M > 0 && dx && dw ? atb::linear_pair(M, N, K) : 0;
+    if (st == ATB_OK && together) return hip_status(atb::launch_tiles_pair(px, pw, together, stream));
+    if (st == ATB_OK && M > 0 && dx) st = hip_status(atb::launch_tiles_dx(px, atb::kStore, stream));
+    if (st == ATB_OK && dw) st = hip_status(atb::launch_tiles_dw(pw, stream));
     return st;
 }
 

@@ -45,6 +45,13 @@ namespace atb {
 hipError_t launch_tiles_linear(TileParams p, int epilogue, hipStream_t) { CHECK(is_linear(epilogue) && (epilogue == kLinearKeep) == (p.slope != nullptr)); return tiles(p, true); }
 hipError_t launch_tiles_dx(TileParams p, int epilogue, hipStream_t) { CHECK(epilogue == kStore); return tiles(p, false); }
 hipError_t launch_tiles_dw(TileParams p, hipStream_t) { return tiles(p, false); }
+hipError_t launch_tiles_pair(TileParams dx, TileParams dw, int tile, hipStream_t)
+{
+    ++g_launches;
+    for (const TileParams &p : {dx, dw}) CHECK(p.M >= 1 && p.N % 8 == 0 && p.K >= 1 && p.edge == 0 && p.segments == 1 && p.problems == 1);
+    CHECK((tile == 128 || tile == 256) && dx.M == dw.K && dx.K == dw.M && dx.N == dw.N);
+    return g_result;
+}
 hipError_t launch_stream(const StreamParams &p, hipStream_t) { ++g_launches; CHECK(p.M >= 1 && p.M <= 32 && p.N >= 1 && p.K >= 8 && p.linear); return g_result; }
 hipError_t launch_linear_grad(const LinearGradParams &p, hipStream_t)
 {

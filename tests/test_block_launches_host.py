@@ -36,7 +36,7 @@ def launches(tmp_path_factory):
 @pytest.mark.parametrize("M", [1, 8, 9, 32, 33, 100, 2048, 65536, MOST_ROWS])
 @pytest.mark.parametrize("N,K", [(1, 8), (33, 64), (4096, 4096), (5001, 2056), (MOST_PITCH, 8), (8, MOST_PITCH)])
 def test_linear(launches, M, N, K):
-    beyond = max(M * N, M * K, N * K) > 2 ** 40
+    beyond = max(M * N, M * K, N * K) > 2 ** 37          # 256 GiB each
     for act in (0, 3):
         for workspace in (0, 1):
             for more in (0, 1):
@@ -60,4 +60,4 @@ def test_residual_norm(launches, M, D, groups):
 def test_moe(launches, M, D, F, experts, k):
     for group in (0, 32, 128):
         if group == 0 or (D % max(group, 8) == 0 and F % max(group, 8) == 0):
-            assert 4 <= len(launches("moe", M, D, F, experts, k, group)) <= 5
+            assert 3 <= len(launches("moe", M, D, F, experts, k, group)) <= 5

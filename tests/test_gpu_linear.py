@@ -72,7 +72,8 @@ def train(x, w, b, res, dy, act, stream=None):
 # one to a few tiles of either size, ends of tiles and of K-steps on both sides, odd N; long reductions of few tiles (shares); enough tiles for the large ones
 SIZES = [(1, 1, 8), (2, 64, 64), (3, 7, 72), (16, 129, 256), (17, 333, 200), (32, 1000, 64), (33, 263, 136), (65, 71, 520), (130, 521, 264), (257, 767, 512), (300, 1001, 1032),
          (70, 4001, 4104), (40, 37, 8200), (1000, 9, 8), (2100, 3081, 136), (3001, 4099, 72), (2600, 2057, 3592),
-         (1100, 3841, 520), (2040, 4096, 200)]                  # (the last two in tiles of 128 x 256)
+         (1100, 3841, 520), (2040, 4096, 200),                  # (in tiles of 128 x 256)
+         (1000, 1011, 16392), (700, 3001, 1544)]                # (both products of the backward pass in one launch, of tiles of 256 x 256 and of 128 x 128)
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
