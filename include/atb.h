@@ -353,7 +353,7 @@ typedef struct atb_residual_norm {
     atb_norm post, pre;                         /* N1, N2 */
     const void *gate;                           /* DEVICE, groups x D of param_type, contiguous, or NULL for 1 */
     int64_t groups;                             /* 1 .. 65535, M a multiple: row i is gated by row i / (M / groups) of gate; 1 without a gate */
-    double scale;                               /* finite */
+    double scale;                               /* finite in fp32 */
     int64_t M, D;                               /* 0 <= M <= 2^23, 1 <= D <= 2^24 */
     atb_type stream_type, block_type, param_type;       /* of x, r and their gradients; of z, h and theirs, not wider than the first; of gate, weights and biases */
 } atb_residual_norm;

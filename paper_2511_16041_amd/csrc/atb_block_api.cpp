@@ -1,6 +1,9 @@
 // C ABI of what a block has around its feed-forward sublayer (see include/atb.h): argument checking and launches.
 #include "atb_block.h"
 
+#include <cmath>
+#include <limits>
+
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 23, kMaxPitch = (int64_t)1 << 22, kMaxNorm = (int64_t)1 << 24;
@@ -171,7 +174,7 @@ bool is_residual(const atb_residual_norm *p)
     if (!p || !residual_lengths(p->M, p->D, p->groups) || !is_type(p->stream_type) || !is_type(p->block_type) || !is_type(p->param_type)) return false;
     if (p->block_type == ATB_TYPE_F32 && p->stream_type != ATB_TYPE_F32) return false;
     if (!is_norm(p->post, p->param_type) || !is_norm(p->pre, p->param_type) || !aligned(p->gate, size_of(p->param_type)) || (!p->gate && p->groups != 1)) return false;
-    if (!(p->scale - p->scale == 0.0)) return false;
+    if (!(std::abs(p->scale) <= std::numeric_limits<float>::max())) return false;          // (the kernels take it in fp32)
     return p->M == 0 || (is_rows(p->x, p->D, p->ldx, size_of(p->stream_type)) && is_rows(p->z, p->D, p->ldz, size_of(p->block_type)));
 }
 atb::NormSpec spec(const atb_norm &n)

@@ -110,7 +110,7 @@ def test_residual_norm_refuses():
         return L.atb_residual_norm_backward(ctypes.byref(atb.ResidualNorm(**{**good, **kw})), stats, dr, lddr, dh, lddh, ctypes.byref(g), work, None)
     shared = [dict(x=None), dict(z=None), dict(x=a + 1), dict(z=a + 1), dict(x=a + 2, stream_type=1), dict(ldx=7), dict(ldz=7), dict(gate=a + 1), dict(gate=None), dict(groups=0), dict(groups=3), dict(groups=65536, M=65536),
               dict(M=-2), dict(M=2 ** 23 + 2), dict(D=0), dict(D=2 ** 24 + 1, ldx=2 ** 25, ldz=2 ** 25), dict(stream_type=2), dict(block_type=-1), dict(param_type=2), dict(block_type=1), dict(scale=float("nan")),
-              dict(scale=float("inf"))]
+              dict(scale=float("inf")), dict(scale=-1e39)]
     for side in ("post", "pre"):
         shared += [{side: atb.NormArgs(a, a, 1e-5, 3)}, {side: atb.NormArgs(a, a, -1.0, 1)}, {side: atb.NormArgs(a, a, float("nan"), 2)}, {side: atb.NormArgs(a + 1, a, 0.0, 1)}, {side: atb.NormArgs(a, a + 1, 0.0, 2)}]
     for bad in shared + [dict(r=None), dict(r=a + 1), dict(ldr=7), dict(h=None), dict(ldh=7), dict(h=a + 1), dict(stats=a + 2), dict(pre=nothing)]:
