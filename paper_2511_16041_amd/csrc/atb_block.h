@@ -36,7 +36,7 @@ static inline int64_t linear_parts(int64_t M, int64_t N)
 // or as all K-steps of 64 over 256 CUs, us per K-step of a tile of 256 x 256 1.3 and 1.65, of 128 x 128 0.6 and 0.53: the smaller time chooses the tiles.  By themselves the products may have their reductions in
 // shares, and where dx has few tiles and a long reduction that is faster: up to 1.35 times what large tiles take without idle CUs, or 32 K-steps, the pair is.  us, in one launch / by themselves: 1500 x 5000 x 2056
 // 92 / 102, 5000 x 5000 x 1000 116 / 168, 4096 x 4096 x 2048 108 / 152, 2048 x 2048 x 2048 37 / 44, 1000 x 2000 x 1000 21 / 39, 100 x 1000 x 4000 14 / 19, 1024 x 11008 x 4096 183 / 196, 2048 x 8192 x 2048 141 / 133,
-// 4096 x 4096 x 4096 213 / 214; not taken: 1024 x 8192 x 2048 84 / 79, 512 x 14336 x 4096 162 / 156, 64 x 4096 x 4096 36 / 26.
+// 5000 x 5000 x 4096 357 / 443, 4096 x 4096 x 4096 205 / 209, 8192 x 14336 x 4096 1566 / 1563; not taken: 1024 x 8192 x 2048 84 / 79, 512 x 14336 x 4096 162 / 156, 64 x 4096 x 4096 36 / 26.
 static inline int linear_pair(int64_t M, int64_t N, int64_t K)
 {
     const double dx = (double)((N + 63) / 64), dw = (double)((M + 63) / 64), longest = std::max(dx, dw);

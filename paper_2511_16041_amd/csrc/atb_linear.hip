@@ -4,6 +4,10 @@
 // For the backward pass act'(z) is kept in fp16: it lies in -0.17 .. 1.13, so 11 bits of mantissa err by at most 2^-11 of it, an eighth of the rounding of dz that follows (dz is an
 // operand of two products, whose matrix instructions take bf16), and 2 bytes are what z in bf16 would take, with eight times the error.
 // The column sums take dz before it is rounded, in fp32, in runs of rows that are added in order: the same bits every time.
+// Bound: as the tiles; dz and its sums HBM.
+// Measured: forward M = 2048, K = 4096, N = 14336 214 us, 1126 TFLOP/s (448 tiles, 1.75 rounds of the CUs), MFMAs busy 49 %; M = 8192 with the slope kept 830 to 875 us, 1100 to 1160, 57 %: a tile's end, which
+// computes tanh and its derivative and writes 4 bytes an element, is not overlapped with products.  dz 161 us, 4.4 TB/s, the bias's gradient 5.  M = 1500, K = 2056, N = 5001: forward 51 to 57 (240 tiles of
+// 128 x 256, one per CU), dz 14, bias 5.4.
 #include "atb_block.h"
 #include "atb_tiles.h"
 

@@ -1,7 +1,8 @@
 // Both products of a linear layer's backward pass in one launch: dx = dz W, and behind it dW = dz^T x.
 //
 // Where each by itself would leave CUs idle at its end, or has fewer tiles than there is room for, the tiles of the second take their place; the ones of dx, whose reductions are the longer ones (of N, not of
-// M), come first.
+// M), come first.  Bound: as the tiles (atb_tiles.h).
+// Measured: M = 8192, N = 14336, K = 4096 1566 us, 1230 TFLOP/s, MFMAs busy 62 % (two launches 1563: level); 1500 x 5001 x 2056 85 to 90, 34 % (99), its tail one long reduction of 79 K-steps per CU.
 #include "atb_block.h"
 #include "atb_tiles.h"
 

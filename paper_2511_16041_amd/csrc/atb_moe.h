@@ -57,7 +57,7 @@ ATB_DEV void moe_weights(const MoeParams &p, const double (&mine)[PER], const in
     for (int i = 0; i < PER; ++i) weight[i] /= sum;
 }
 
-// The choice of a single token, by every workgroup of its gate and up products for itself, without a launch for it (which took 6 of 31 us of one token through 8 of 64 experts of 2048 x 1536 in 4 bits):
+// The choice of a single token, by every workgroup of its gate and up products for itself, without a launch for it (which took 6 us, 5 more than this, of one token through 8 of 64 experts of 2048 x 1536 in 4 bits: 30 / 25.3 in all):
 // the experts ahead of each are counted by all 256 threads.  Returns this workgroup's segment; those of the first columns write their part of the plan.  `lds`: 12 bytes for each of kMoeExperts.
 ATB_DEV MoeSegment moe_choose_one(const MoeParams &p, char *lds)
 {

@@ -3,15 +3,14 @@
 //
 // A workgroup has 16 columns of y times a few and 16 rows, as in atb_stream.hip: W waves take the panels of K in turn, and their sums are added in
 // wave order.  A panel is 256 k, one 128-byte line of every row of W.  A lane asks for 16 bytes of its row, 32 codes; the dwords of four lanes are exchanged (a 4 x 4
-// transposition in four lane swaps), so that one MFMA's 32 k lie in one group of 32.  The next panel is asked for ahead of the multiplication, and x, out of a cache, in
-// it: with x of a panel in registers as well there is room for half as many waves.  Requests come back in order, so the first MFMA of a panel waits for x and
-// with it for the next panel, and that is what bounds these kernels rather than decoding: of the cycles VALU instructions take 40 % (16 rows, 8192 -> 8192) to 44 % (the gated
-// product below) and MFMAs 7 to 10 %, the rest is waiting.  Scales and zero points are asked for by 16 lanes, one a column, and handed to the others.
+// transposition in four lane swaps), so that one MFMA's 32 k lie in one group of 32.  Before the multiplication x of the panel, out of a cache, is asked for and behind it the next panel:
+// requests come back in order, and with x behind the panel the first MFMA would wait for that too (gated 21.9 us, back 13.1 in the products below).  Two columns of 8 groups with zero points a panel have no
+// registers for it: there x is asked for in the multiplication, half a panel at a time, and this wait is what bounds those, with VALU instructions in 40 % of the cycles (16 rows, 8192 -> 8192) and MFMAs in 7 %.  Scales and zero points are asked for by 16 lanes, one a column, and handed to the others.
 //
 // w = s (q - z).  A code becomes bf16 without a conversion: 0x4180 | q << 3 is the number 16 + q.  The MFMAs of a group sum (16 + q) x; one more,
 // shared by all columns, sums x; then y += s (sum - (16 + z) sum of x), all in fp32.  (With 0x4300 | q, 128 + q, the sum that is subtracted again is
 // 30 times the result's size and not 5, and the error against 64 bits 1.8e-6.)
-// Measured: one row, 4096 -> 4096 in groups of 128 5.0 us; gated 4096 -> 14336 in groups of 64 with zero points 21.9 us, 3.0 TB/s, and back 13.1; 16 rows,
+// Measured: one row, 4096 -> 4096 in groups of 128 5.0 us; gated 4096 -> 14336 in groups of 64 with zero points 20.5 us, 3.2 TB/s, and back 11.5; 16 rows,
 // 8192 -> 8192 in groups of 32 with zero points 17.6 us, 2.3 TB/s.  Every block of 16 rows is a workgroup that asks for the weights and decodes them again: 32 rows 34.6 us,
 // 64 66.4; 64 rows 4096 -> 4096 23.6, 16 7.1.
 #include "atb_q4_rows.h"

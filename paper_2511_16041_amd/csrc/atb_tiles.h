@@ -1,4 +1,4 @@
-// bf16 products in tiles: the kernel behind the gated block and its gradients (atb_ffn.hip, atb_ffn_grad.hip), and behind products with an epilogue (atb_linear.hip).
+// bf16 products in tiles: the kernel behind the gated block and its gradients (atb_ffn.hip, atb_ffn_grad.hip), and behind products with an epilogue and their gradients (atb_linear.hip, atb_linear_pair.hip).
 //
 // C tile = A tile x B tile with fp32 accumulation in MFMA accumulators, in K-steps of 64.  The tiles of a K-step come straight from memory into
 // LDS: three buffers for A and two for B, all of a CU's 160 KiB.  An operand whose reduction index is contiguous lies in LDS as rows of 64 k (128
