@@ -135,6 +135,7 @@ struct MoeParams {
     int M, D, F, E, k;
     int group;                   // 0: bf16 weights
     int act, renormalize;
+    int few;                     // moe_is_few
     // workspace
     double *logits;              // M x E
     MoePlan *plan;
@@ -147,6 +148,14 @@ hipError_t launch_moe_q4(const MoeParams &p, hipStream_t stream);        // the 
 
 // Rows of x that a workgroup of the products takes: 32 where an expert gets more than 12 on average, so that few get more than 16 and read their weights twice.
 static inline int moe_rows(int64_t M, int64_t E, int64_t k) { return M > 16 && M * k > 12 * E ? 32 : 16; }
+// Whether the products of up to 8 tokens choose the experts themselves, instead of a launch before them: where there are no more of the router's products than a workgroup has threads, and their workgroups, of 16 columns of
+// an expert, run at once, four per CU, or have little to choose from.  us, with / without that launch, 4 bits: 2 tokens through 8 of 8 experts of 2304 x 1856 40 / 37.5, 4 through one of 41 of 1280 x 640 21.3 / 19.5,
+// 8 through 2 of 8 of 2048 x 1536 30.5 / 28.2, 2 through 8 of 128 of 2048 x 768 30.2 / 28.8, 2 through 2 of 8 of 4096 x 14336 82.7 / 82.7; not taken: 2 through 8 of 64 of 2048 x 1536 38.3 / 40.0, 8 through 2 of 8 of 4096 x 14336
+// 178 / 183, 8 through 2 of 16 of 2048 x 8192 83 / 102.
+static inline bool moe_is_few(int64_t M, int64_t E, int64_t k, int64_t F)
+{
+    return M <= 8 && M * E <= 256 && (M * E <= 16 || std::min(E, M * k) * ((F + 15) / 16) <= 1024);
+}
 // The most segments that the choices can have
 static inline int moe_segments(int64_t M, int64_t E, int64_t k, int rows) { return (int)(std::min(E, M * k) + M * k / rows); }
 

@@ -305,6 +305,7 @@ extern "C" atb_status atb_moe_forward(const atb_moe *m, void *y, int64_t ldy, in
     q.group = m->group;
     q.act = m->act;
     q.renormalize = m->renormalize;
+    q.few = atb::moe_is_few(m->M, m->experts, m->top_k, m->F);
     q.logits = reinterpret_cast<double *>(work);
     q.plan = reinterpret_cast<atb::MoePlan *>(work + room.logits);
     q.h = reinterpret_cast<uint16_t *>(work + room.logits + room.plan);

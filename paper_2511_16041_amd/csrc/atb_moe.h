@@ -57,65 +57,109 @@ ATB_DEV void moe_weights(const MoeParams &p, const double (&mine)[PER], const in
     for (int i = 0; i < PER; ++i) weight[i] /= sum;
 }
 
-// The choice of a single token, by every workgroup of its gate and up products for itself, without a launch for it (which took 6 us, 5 more than this, of one token through 8 of 64 experts of 2048 x 1536 in 4 bits: 30 / 25.3 in all):
-// the experts ahead of each are counted by all 256 threads.  Returns this workgroup's segment; those of the first columns write their part of the plan.  `lds`: 12 bytes for each of kMoeExperts.
-ATB_DEV MoeSegment moe_choose_one(const MoeParams &p, char *lds)
+// A segment of up to 8 tokens, which are the bits of `tokens`
+struct MoeFew { MoeSegment segment; unsigned tokens; };
+
+// The choice of few tokens (moe_is_few), by every workgroup of their gate and up products for itself, without a launch for it, which took 6 us, 5 more than this does of one token over 64 experts (one token
+// through 8 of them, 2048 x 1536 in 4 bits, 30 / 25.3 in all): the experts ahead of each are counted by all 256 threads.  Workgroup y has the y-th of the chosen experts; the one of its first columns
+// writes its part of the plan.  rows 0: there is none.  `lds`: 12 bytes for each of 256 products.
+ATB_DEV MoeFew moe_choose_few(const MoeParams &p, char *lds)
 {
     double *l = reinterpret_cast<double *>(lds);
-    int *ahead = reinterpret_cast<int *>(l + kMoeExperts);
-    const int t = threadIdx.x, lane = t & 63, place = blockIdx.y;
-    const double mine = t < p.E ? p.logits[t] : -INFINITY;
+    int *ahead = reinterpret_cast<int *>(l + 256);
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, all = p.M * p.E;
+    const double mine = t < all ? p.logits[t] : -INFINITY;
     l[t] = mine == mine ? mine : -INFINITY;                        // NaN is behind all numbers
     ahead[t] = 0;
     __syncthreads();
-    const int width = p.E <= 64 ? 64 : p.E <= 128 ? 128 : 256, e = t & (width - 1), part = t / width, per = width * width / 256;
-    const double key = l[e];
-    int n = 0;
+    const int width = all <= 64 ? 64 : all <= 128 ? 128 : 256, o = t & (width - 1), per = (p.E * width + 255) / 256, from = t / width * per;
+    if (o < all) {
+        const int base = o / p.E * p.E;
+        const double key = l[o];
+        int n = 0;
 #pragma unroll 4
-    for (int j = part * per; j < (part + 1) * per; ++j) n += j < p.E && (l[j] > key || (l[j] == key && j < e));
-    atomicAdd(&ahead[e], n);
+        for (int j = base + from; j < base + min(from + per, p.E); ++j) n += l[j] > key || (l[j] == key && j < o);
+        atomicAdd(&ahead[o], n);
+    }
     __syncthreads();
-    // every wave finds the place-th of the chosen by itself
-    int expert = 0, before = 0, rank[4];
+    // every wave finds the chosen expert and its tokens by itself
+    unsigned chose[4];                                             // tokens of expert 64 i + lane
+    int expert = -1, experts = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        rank[i] = ahead[64 * i + lane];
-        const unsigned long long taken = __ballot(64 * i + lane < p.E && rank[i] < p.k), to = (taken >> lane & 1) == 0 ? 0 : __popcll(taken & ((1ull << lane) - 1)) + before == place;
-        const unsigned long long found = __ballot(to);
+        const int e = 64 * i + lane;
+        chose[i] = 0;
+        for (int m = 0; m < p.M; ++m) chose[i] |= e < p.E && ahead[min(m * p.E + e, 255)] < p.k ? 1u << m : 0;
+        const unsigned long long taken = __ballot(chose[i] != 0), found = __ballot(chose[i] != 0 && __popcll(taken & ((1ull << lane) - 1)) + experts == (int)blockIdx.y);
         if (found) expert = 64 * i + __ffsll(found) - 1;
-        before += __popcll(taken);
+        experts += __popcll(taken);
     }
-    if (blockIdx.x == 0 && t < 64) {
-        double raw[4];
-        float weight[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = 64 * i + lane < p.E ? p.logits[64 * i + lane] : -INFINITY;
-        moe_weights(p, raw, rank, weight);
+    MoeFew few = {{max(expert, 0), 0, 0}, 0};
+    if (expert >= 0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (64 * i + lane != expert) continue;
-            p.plan->expert[place] = expert;
-            p.plan->first[place] = place;
-            p.plan->rows[place] = 1;
-            p.plan->token[place] = 0;
-            p.plan->weight[place] = weight[i];
-            if (place == 0) p.plan->segments = p.k;
-            if (p.experts) p.experts[rank[i]] = expert;
-            if (p.weights) p.weights[rank[i]] = weight[i];
+            if (64 * i <= expert)
+                for (int m = 0; m < p.M; ++m) few.segment.first += __popcll(__ballot((chose[i] >> m & 1) != 0 && 64 * i + lane < expert));
+            if (expert >> 6 == i) few.tokens = __builtin_amdgcn_readlane(chose[i], expert & 63);
+        }
+        few.segment.rows = __popc(few.tokens);
+        if (blockIdx.x == 0) {
+            if (t == 0) {
+                p.plan->expert[blockIdx.y] = expert;
+                p.plan->first[blockIdx.y] = few.segment.first;
+                p.plan->rows[blockIdx.y] = few.segment.rows;
+                if (blockIdx.y == 0) p.plan->segments = experts;
+            }
+            int place = few.segment.first;
+            for (int m = 0; m < p.M; ++m) {
+                if ((few.tokens >> m & 1) == 0) continue;
+                if (place % 4 == wave) {
+                    double raw[4];
+                    float weight[4];
+                    int rank[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool live = 64 * i + lane < p.E;
+                        raw[i] = live ? p.logits[m * p.E + 64 * i + lane] : -INFINITY;
+                        rank[i] = live ? ahead[m * p.E + 64 * i + lane] : p.E;
+                    }
+                    moe_weights(p, raw, rank, weight);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (64 * i + lane != expert) continue;
+                        p.plan->token[place] = m;
+                        p.plan->weight[place] = weight[i];
+                        if (p.experts) p.experts[m * p.k + rank[i]] = expert;
+                        if (p.weights) p.weights[m * p.k + rank[i]] = weight[i];
+                    }
+                }
+                ++place;
+            }
         }
     }
     __syncthreads();                                               // `lds` is free again
-    return {expert, place, 1};
+    return few;
 }
 
-// Whether the workgroup has a segment, and which.  FEW: there may be one token alone
+// The workgroup's segment; rows 0: none.  FEW: moe_is_few
 template <bool FEW>
-ATB_DEV bool moe_open(const MoeParams &p, char *lds, MoeSegment &segment)
+ATB_DEV MoeFew moe_open(const MoeParams &p, char *lds)
 {
-    const bool one = FEW && p.M == 1;
-    if ((int)blockIdx.y >= (one ? p.k : p.plan->segments)) return false;
-    segment = one ? moe_choose_one(p, lds) : moe_segment(p.plan, blockIdx.y);
-    return true;
+    if constexpr (FEW) return moe_choose_few(p, lds);
+    if ((int)blockIdx.y >= p.plan->segments) return {};
+    return {moe_segment(p.plan, blockIdx.y), 0};
+}
+
+// The token of a segment's row
+template <bool FEW>
+ATB_DEV int moe_token(const MoeParams &p, const MoeFew &few, int row)
+{
+    if (!FEW) return p.plan->token[few.segment.first + row];
+    int token = 0;
+#pragma unroll
+    for (int m = 0; m < 8; ++m)
+        if (few.tokens >> m & 1 && row-- == 0) token = m;
+    return token;
 }
 
 // The product of a segment's gate and up weights, as finish_rows stores it: rows of h

@@ -2,8 +2,8 @@
 // Floor: the bytes of the chosen experts' weights.
 //
 // Four launches.  (1) The router's products in fp64, a wave for one expert and a few tokens: which experts are taken hangs on the order of the l, and in fp32 two that lie close could change places.
-// (2) One workgroup: every token's experts, their shares, and the plan, the choices sorted by expert; a single token's is
-// part of the products.  (3) Gate and up
+// (2) One workgroup: every token's experts, their shares, and the plan, the choices sorted by expert; that of few tokens is part
+// of the products.  (3) Gate and up
 // products of every expert and its tokens, as the kernel for few rows does them, with the rows of x gathered by the plan; h by place.  (4) The down product: a workgroup has 16 columns of y and
 // all experts in turn; its waves take the panels of all of them as one long reduction, and at an expert's end each adds its sums, times the tokens' shares, to its own part of y in LDS.  So every expert's weights
 // are read once (of more tokens than a segment's 16 or 32 again), those of no token not at all, the sum over a token's experts is in fp32, in the order of the experts, without atomics, and no token's values meet another's.
@@ -150,18 +150,18 @@ __global__ void __launch_bounds__(1024) moe_plan_kernel(const MoeParams p, int r
 
 // ---- the products
 
-template <class S>
+template <class S, bool FEW>
 __global__ void __launch_bounds__(S::W * 64) moe_gated_kernel(const MoeParams p)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS_BYTES];
-    static_assert(S::W == 4 && S::LDS_BYTES >= 12 * kMoeExperts, "moe_choose_one");
-    MoeSegment seg;
-    if (!moe_open<S::XQ == 1>(p, lds, seg)) return;
+    static_assert(S::W == 4 && S::LDS_BYTES >= 12 * 256, "moe_choose_few");
+    const MoeFew few = moe_open<FEW>(p, lds);
+    const MoeSegment &seg = few.segment;
+    if (seg.rows == 0) return;
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.F - n0, 16 * S::COLS);
     const int64_t at = ((int64_t)seg.expert * p.F + n0) * p.D;
     const StreamView view = {p.x, p.ldx, p.M, seg.rows, {static_cast<const uint16_t *>(p.gate.w) + at, static_cast<const uint16_t *>(p.up.w) + at}, {p.D, p.D}, cols, p.D};
-    const int *tokens = p.plan->token + seg.first;
-    Stream<S> s(view, (unsigned)reinterpret_cast<uintptr_t>(lds), [&](int row) { return S::XQ == 1 && p.M == 1 ? 0 : tokens[row]; });
+    Stream<S> s(view, (unsigned)reinterpret_cast<uintptr_t>(lds), [&](int row) { return moe_token<FEW>(p, few, row); });
     s.run();
     finish_rows<S::MB, S::NB, S::W, true>(moe_inner(p, seg), s.acc, reinterpret_cast<float *>(lds), 0, n0, cols);
 }
@@ -242,7 +242,9 @@ hipError_t launch_products(const MoeParams &p, hipStream_t stream)
     typedef StreamShape<MB, 2, XQ, 4, true> Gated;
     typedef StreamShape<MB, 1, XQ, 8, false> Down;
     const int segments = moe_segments(p.M, p.E, p.k, 16 * MB);
-    hipLaunchKernelGGL((moe_gated_kernel<Gated>), dim3((unsigned)((p.F + 15) / 16), (unsigned)segments), dim3(Gated::W * 64), 0, stream, p);
+    const dim3 grid((unsigned)((p.F + 15) / 16), (unsigned)segments);
+    if (XQ == 1 && p.few) hipLaunchKernelGGL((moe_gated_kernel<Gated, XQ == 1>), grid, dim3(Gated::W * 64), 0, stream, p);
+    else hipLaunchKernelGGL((moe_gated_kernel<Gated, false>), grid, dim3(Gated::W * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((moe_down_kernel<Down>), dim3((unsigned)((p.D + 15) / 16), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 16 * sizeof(float) + moe_copy_bytes(segments, p.M * p.k), stream, p, segments);
@@ -259,7 +261,7 @@ hipError_t launch_moe(const MoeParams &p, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int rows = p.group ? 16 : moe_rows(p.M, p.E, p.k);
-    if (p.M > 1) {                                                 // (a single token's choice: moe_choose_one)
+    if (!p.few) {
         if (p.E <= 64) hipLaunchKernelGGL(moe_plan_kernel<1>, dim3(1), dim3(1024), 0, stream, p, rows);
         else if (p.E <= 128) hipLaunchKernelGGL(moe_plan_kernel<2>, dim3(1), dim3(1024), 0, stream, p, rows);
         else hipLaunchKernelGGL(moe_plan_kernel<4>, dim3(1), dim3(1024), 0, stream, p, rows);

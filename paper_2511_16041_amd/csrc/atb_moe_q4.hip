@@ -5,19 +5,19 @@
 namespace atb {
 namespace {
 
-template <class S>
+template <class S, bool FEW>
 __global__ void __launch_bounds__(S::W * 64, S::NB > 2 ? 2 : 4) moe_q4_gated_kernel(const MoeParams p)
 {
     __shared__ __attribute__((aligned(16))) float lds[S::W * S::NB * 256];
-    static_assert(S::W == 4 && sizeof(lds) >= 12 * kMoeExperts, "moe_choose_one");
-    MoeSegment seg;
-    if (!moe_open<S::NB == 2>(p, reinterpret_cast<char *>(lds), seg)) return;
+    static_assert(S::W == 4 && sizeof(lds) >= 12 * 256, "moe_choose_few");
+    const MoeFew few = moe_open<FEW>(p, reinterpret_cast<char *>(lds));
+    const MoeSegment &seg = few.segment;
+    if (seg.rows == 0) return;
     const int n0 = blockIdx.x * 16 * S::COLS, cols = min(p.F - n0, 16 * S::COLS);
     const int64_t n = (int64_t)seg.expert * p.F + n0;
     const Q4View view = {p.x, p.ldx, p.M, seg.rows, {q4_columns(p.gate, n, p.D, S::G), q4_columns(p.up, n, p.D, S::G)}, cols, p.D};
-    const int *tokens = p.plan->token + seg.first;
     Q4Stream<S> s(view);
-    s.run([&] { s.open_rows(view, [&](int row) { return S::NB == 2 && p.M == 1 ? 0 : tokens[row]; }); });
+    s.run([&] { s.open_rows(view, [&](int row) { return moe_token<FEW>(p, few, row); }); });
     finish_rows<1, S::NB, S::W, true>(moe_inner(p, seg), s.acc, lds, 0, n0, cols);
 }
 
@@ -85,8 +85,10 @@ hipError_t launch_group(const MoeParams &p, hipStream_t stream)
     typedef Q4Shape<G, 4, 4, true, ZEROS> GatedWide;
     typedef Q4Shape<G, 2, 8, false, ZEROS> Down;
     const unsigned segments = (unsigned)moe_segments(p.M, p.E, p.k, 16);
-    if (p.M <= 8) hipLaunchKernelGGL((moe_q4_gated_kernel<Gated>), dim3((unsigned)((p.F + 15) / 16), segments), dim3(Gated::W * 64), 0, stream, p);
-    else hipLaunchKernelGGL((moe_q4_gated_kernel<GatedWide>), dim3((unsigned)((p.F + 31) / 32), segments), dim3(GatedWide::W * 64), 0, stream, p);
+    const dim3 narrow((unsigned)((p.F + 15) / 16), segments);
+    if (p.few) hipLaunchKernelGGL((moe_q4_gated_kernel<Gated, true>), narrow, dim3(Gated::W * 64), 0, stream, p);
+    else if (p.M <= 8) hipLaunchKernelGGL((moe_q4_gated_kernel<Gated, false>), narrow, dim3(Gated::W * 64), 0, stream, p);
+    else hipLaunchKernelGGL((moe_q4_gated_kernel<GatedWide, false>), dim3((unsigned)((p.F + 31) / 32), segments), dim3(GatedWide::W * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((moe_q4_down_kernel<Down>), dim3((unsigned)((p.D + 31) / 32), (unsigned)p.shares), dim3(Down::W * 64), (size_t)Down::W * p.M * 32 * sizeof(float) + moe_copy_bytes((int)segments, p.M * p.k), stream, p, (int)segments);
