@@ -84,6 +84,9 @@ constexpr int kResidualMaxGradRow = 2 * kResidualThreads * kResidualPerThread;  
 
 // ... and rows of less than a chunk with them
 static inline bool residual_is_long(int64_t D) { return D > kResidualMaxGradRow || D < kResidualPerThread; }
+// Rows of up to twice as many elements in 16 bits are held for dx and dz; there are no registers for the sums too, which stay a pass of their own.  us without the sums, held / read again: 4096 x 12000 159 / 225, 512 x 16384
+// 27 / 36, 9 x 11066 7.6 / 19.5.
+static inline bool residual_is_wide(int64_t D) { return D > kResidualMaxGradRow && D <= 2 * kResidualMaxGradRow; }
 
 // Threads per row: the power of two, 64 to 512, that holds it.
 static inline int residual_threads(int64_t D)

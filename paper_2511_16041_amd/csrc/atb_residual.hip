@@ -5,7 +5,7 @@
 //     g1 = t g w1,   dz = s1 (g1 - [mean(g1)] - xh1 mean(g1 xh1)),     [..] of layer norms only,
 //     dgate = w1 S1 + b1 S0,   dw1 = sum over groups g S1,   db1 = sum over groups g S0,   S1 = sum t xh1, S0 = sum t over the rows of a gate's group,
 //     dw2 = sum dh xh2,   db2 = sum dh,
-// so gate, w1 and b1 share two sums, and all parameters need four, of which two fall away without biases.  Rows of up to 8192 elements (forward 16384) are held in registers and read once; r is computed again in the
+// so gate, w1 and b1 share two sums, and all parameters need four, of which two fall away without biases.  Rows of up to 8192 elements (forward, and in 16 bits without the sums, 16384) are held in registers and read once; r is computed again in the
 // backward pass, which reads x in its place.  A workgroup of the backward pass walks rows of one group and keeps its share of the sums in registers; a second kernel adds them in order,
 // a third one the groups.  No atomics: the same bits every time.
 // Measured, bf16, root-mean-square norms on both sides: 8192 x 4096 forward 49.5 us, 5.4 TB/s (part of x and z in the memory-side cache), backward 79.3, 5.1 TB/s (waves waiting 44 %), sums 4.8; 2048 x 8192 with one norm 23.0;
@@ -302,13 +302,14 @@ struct RowStats {
 };
 
 // dx, dz and (SUMS) the workgroup's part of the sums over rows, [group][part][SUMS][D]: S1, dw2's, S0, db2's.  T threads per row with C chunks each.
+// rows: of rows whose sums residual_columns_kernel takes (C > 2), where their two means go, or null.
 template <class X, class Z, class P, int T, int C, int SUMS>
-__global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) residual_grad_kernel(const ResidualParams p, int parts, int rounds)
+__global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) residual_grad_kernel(const ResidualParams p, int parts, int rounds, float *rows)
 {
     constexpr int NT = T > kResidualThreads ? T : kResidualThreads, R = NT / T;
     // registers: the next row's operands (dr, which is used last, on its own) and the parameters are held unless they would not fit
     constexpr bool TIGHT = T > kResidualThreads && sizeof(X) == 4, LARGE = TIGHT && sizeof(Z) == 4;
-    constexpr bool AHEAD = C == 1 ? !LARGE : sizeof(X) == 2 && SUMS < 4, DR_AHEAD = AHEAD && !TIGHT, HOLD = C == 1 ? !TIGHT || sizeof(P) == 2 : sizeof(P) == 2;
+    constexpr bool AHEAD = C == 1 ? !LARGE : C == 2 && sizeof(X) == 2 && SUMS < 4, DR_AHEAD = AHEAD && !TIGHT, HOLD = C == 1 ? !TIGHT || sizeof(P) == 2 : C == 2 && sizeof(P) == 2;
     __shared__ float scratch[2][2 * NT / 64];
     RowSums<T, NT> sums(scratch);
     const int t = T >= kResidualThreads ? threadIdx.x : threadIdx.x % T, group = T >= kResidualThreads ? 0 : threadIdx.x / T, D = p.D;
@@ -398,6 +399,10 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
         }
         if (normed2) sums(s);
         const float m0 = s[0] * centre2, m1 = s[1] * inv;
+        if (C > 2 && rows && live && t == 0) {
+            rows[row] = m0;
+            rows[p.M + row] = m1;
+        }
         float q[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -812,12 +817,12 @@ hipError_t forward_of(const ResidualParams &p, hipStream_t stream)
 }
 
 template <class X, class Z, class P, int T, int C, int SUMS>
-hipError_t backward_of(const ResidualParams &p, hipStream_t stream)
+hipError_t backward_of(const ResidualParams &p, hipStream_t stream, float *rows = nullptr)
 {
     constexpr int NT = T > kResidualThreads ? T : kResidualThreads, R = NT / T;
     const int64_t per_gate = p.M / p.groups, turns = (per_gate + R - 1) / R;
     const int64_t parts = SUMS > 0 ? p.parts : std::min<int64_t>(turns, std::max<int64_t>(1, 2048 / p.groups));
-    hipLaunchKernelGGL((residual_grad_kernel<X, Z, P, T, C, SUMS>), dim3((unsigned)(p.groups * parts)), dim3(workgroup<T, C>(p.D, NT)), 0, stream, p, (int)parts, (int)((turns + parts - 1) / parts));
+    hipLaunchKernelGGL((residual_grad_kernel<X, Z, P, T, C, SUMS>), dim3((unsigned)(p.groups * parts)), dim3(workgroup<T, C>(p.D, NT)), 0, stream, p, (int)parts, (int)((turns + parts - 1) / parts), rows);
     return hipGetLastError();
 }
 
@@ -880,10 +885,17 @@ hipError_t backward(const ResidualParams &p, hipStream_t stream)
     const ResidualRoom room = residual_room(p.M, p.D, p.groups);
     float *totals = asked && p.groups > 1 ? p.workspace + room.sums : nullptr, *rows = asked && is_long ? p.workspace + room.sums + room.totals : nullptr;
     if (p.M > 0 && (asked || p.dx || p.dz)) {
-        hipError_t e;
+        hipError_t e = hipSuccess;
         if (is_long) {
-            hipLaunchKernelGGL((residual_grad_long_kernel<X, Z, P>), dim3((unsigned)std::min(p.M, kMostWorkgroups)), dim3(kResidualThreads), 0, stream, p, rows);
-            e = hipGetLastError();
+            bool held = false;
+            if constexpr (sizeof(X) == 2) {
+                held = residual_is_wide(p.D);
+                if (held) e = p.D <= 3 * kResidualThreads * E ? backward_of<X, Z, P, 512, 3, 0>(p, stream, rows) : backward_of<X, Z, P, 512, 4, 0>(p, stream, rows);
+            }
+            if (!held) {
+                hipLaunchKernelGGL((residual_grad_long_kernel<X, Z, P>), dim3((unsigned)std::min(p.M, kMostWorkgroups)), dim3(kResidualThreads), 0, stream, p, rows);
+                e = hipGetLastError();
+            }
         } else {
             e = sums == 0 ? backward_rows<X, Z, P, 0>(p, stream) : sums == 2 ? backward_rows<X, Z, P, 2>(p, stream) : backward_rows<X, Z, P, 4>(p, stream);
         }
