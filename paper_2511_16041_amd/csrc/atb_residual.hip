@@ -315,7 +315,8 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
     const int t = T >= kResidualThreads ? threadIdx.x : threadIdx.x % T, group = T >= kResidualThreads ? 0 : threadIdx.x / T, D = p.D;
     const int64_t per_gate = p.M / p.groups, gate_row = blockIdx.x / parts, part = blockIdx.x % parts;
     const bool normed1 = p.post.kind != ATB_NORM_NONE, normed2 = p.pre.kind != ATB_NORM_NONE;
-    const float inv = 1.0f / (float)D, centre1 = p.post.kind == ATB_NORM_LAYER ? inv : 0.0f, centre2 = p.pre.kind == ATB_NORM_LAYER ? inv : 0.0f;
+    const bool centred1 = p.post.kind == ATB_NORM_LAYER, centred2 = p.pre.kind == ATB_NORM_LAYER;
+    const float inv = 1.0f / (float)D;
     struct Params { Raw<P> w1, b1, w2, gate; };
     Params held[HOLD ? C : 1];
     auto params = [&](int c) {
@@ -398,7 +399,7 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
             if (DR_AHEAD) fetch_dr(next_row);
         }
         if (normed2) sums(s);
-        const float m0 = s[0] * centre2, m1 = s[1] * inv;
+        const float m0 = centred2 ? s[0] * inv : 0.0f, m1 = s[1] * inv;       // (selected: a sum that is not needed may be infinite, and times 0 NaN)
         if (C > 2 && rows && live && t == 0) {
             rows[row] = m0;
             rows[p.M + row] = m1;
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
         }
         if (normed1) {
             sums(q);
-            const float n0 = q[0] * centre1, n1 = q[1] * inv;
+            const float n0 = centred1 ? q[0] * inv : 0.0f, n1 = q[1] * inv;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -613,7 +614,8 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_long_kernel(co
     RowSums<kResidualThreads, kResidualThreads> sums(scratch);
     const int D = p.D;
     const bool normed1 = p.post.kind != ATB_NORM_NONE, normed2 = p.pre.kind != ATB_NORM_NONE;
-    const float inv = 1.0f / (float)D, centre1 = p.post.kind == ATB_NORM_LAYER ? inv : 0.0f, centre2 = p.pre.kind == ATB_NORM_LAYER ? inv : 0.0f;
+    const bool centred1 = p.post.kind == ATB_NORM_LAYER, centred2 = p.pre.kind == ATB_NORM_LAYER;
+    const float inv = 1.0f / (float)D;
     for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
         const int64_t gate_row = row / (p.M / p.groups);
         RowStats st;
@@ -631,7 +633,7 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_long_kernel(co
                 }
             });
             sums(s);
-            m0 = s[0] * centre2;
+            m0 = centred2 ? s[0] * inv : 0.0f;
             m1 = s[1] * inv;
         }
         if (rows && threadIdx.x == 0) {
@@ -665,7 +667,7 @@ __global__ void __launch_bounds__(kResidualThreads) residual_grad_long_kernel(co
                 }
             });
             sums(q);
-            n0 = q[0] * centre1;
+            n0 = centred1 ? q[0] * inv : 0.0f;
             n1 = q[1] * inv;
         }
         if (!p.dx && !p.dz) continue;

@@ -4,6 +4,7 @@ Tolerances.  fp32 sums along rows, in trees of at most 2^10 lanes and chains of 
 sums over the rows here, in chains of at most 16 to 90 additions, by less than F = 2^-17.  A value that errs is carried through what it enters.  A bf16 result adds its rounding, at most 2^-8 of its size."""
 import ctypes
 import itertools
+import math
 
 import pytest
 import torch
@@ -301,3 +302,53 @@ def test_gradients_against_differences():
             want = float((grad * (ends[0].double() - ends[1].double())).sum())
             # the results' errors, at most E of each; the third derivative: its share of the slope is the square of the relative move, 2^-12, times a few
             assert abs(slope - want) <= 2 * E * size * 0.1 + 2.0 ** -8 * abs(want), (post, pre, name, slope, want)
+
+
+# ------------------------------------------------------------------ gradients that are infinite or nearly so
+
+def limits_of(t):
+    """A result's infinities and NaNs: 1, -1, 2; of numbers 0"""
+    return torch.where(t.isnan(), 2.0, torch.where(t.isinf(), t.double().sign(), 0.0))
+
+
+@pytest.mark.parametrize("stream,block", [(BF16, BF16), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("post,pre,of_r", [("rms", "rms", False), ("rms", None, True), ("rms", "layer", True), (None, "rms", False)])
+@pytest.mark.parametrize("D", [64, 99, 700, 5000, 9000, 12500, 20000])
+def test_gradients_whose_sum_passes_fp32_through_root_mean_square_norms(D, post, pre, of_r, stream, block):
+    """These norms' formulas have sum(g xh) in them and not sum(g).  Gradients of 2^129 / D or more, all of one sign: the second is more than a float holds; the first, whose terms have either sign, is about 2^129 / sqrt(D)."""
+    a = inputs(6, D, stream, block, BF16, post, pre, seed=D, scale=1.0)
+    a["z"], a["x"] = (a["z"].double().sign() * (1 + a["z"].double().abs() % 1)).to(block), (0.5 * a["x"].double().sign()).to(stream)
+    large = torch.full((6, D), 2.0 ** (129 - int(math.log2(D))), device="cuda")
+    a["dr"] = (large if of_r else 0 * large).to(stream)
+    if pre:
+        a["dh"], a["pre"] = (0 * large if of_r else large).to(block), a["pre"]._replace(weight=torch.ones_like(a["pre"].weight))
+    if post:
+        a["post"] = a["post"]._replace(weight=torch.ones_like(a["post"].weight))
+    a["gate"] = torch.ones_like(a["gate"])
+    got = run(a)
+    close({k: got[k] for k in ("dx", "dz")}, reference(a))
+
+
+def rms_gradient(v, norm, dy):
+    """The gradient of a root-mean-square norm's row by its definition, rstd (g - xh mean(g xh)) with g = dy weight, in 64 bits"""
+    rstd = (v.square().mean(1, keepdim=True) + norm.eps).rsqrt()
+    g, hat = dy * norm.weight.double(), v * rstd
+    return rstd * (g - hat * (g * hat).mean(1, keepdim=True))
+
+
+@pytest.mark.parametrize("stream,block", [(BF16, BF16), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("D", [7, 64, 99, 700, 5000, 9000, 12500, 20000])
+def test_an_infinite_gradient_is_infinite_in_its_row(D, stream, block):
+    """dh or dr infinite at one place: through root-mean-square norms dx and dz have the signs that the formulas give, and no other row has any."""
+    for post, pre, name in ((None, "rms", "dh"), ("rms", None, "dr")):
+        a = inputs(6, D, stream, block, BF16, post, pre, seed=D + 1)
+        a[name] = a[name].clone()
+        a[name][2, D // 2], a[name][4, D - 1] = float("inf"), float("-inf")
+        x, z, gate, t = a["x"].double(), a["z"].double(), a["gate"].double(), a["dr"].double()
+        if pre:
+            t = t + rms_gradient(a["scale"] * x + gate * z, a["pre"], a["dh"].double())
+        want, got = {"dx": a["scale"] * t, "dz": rms_gradient(z, a["post"], t * gate) if post else t * gate}, run(a)
+        for k in ("dx", "dz"):
+            kinds = limits_of(got[k])
+            assert torch.equal(kinds, limits_of(want[k])), (name, k)
+            assert kinds[[2, 4]].any() and not kinds[[0, 1, 3, 5]].any(), (name, k)
