@@ -374,7 +374,8 @@ size_t atb_residual_norm_workspace(int64_t M, int64_t D, int64_t groups);
 
 /* dr: DEVICE, M x D of stream_type (pitch lddr), the gradient of r by all that follows but h, or NULL for 0; dh: of block_type (pitch lddh), with a norm `pre`.  x and z as in the forward pass (r is
  * computed again: rounded to bf16 it would cost the gradients digits, and x is no longer to read).  stats: of the forward pass.  workspace: DEVICE, 16-byte aligned.  The sums over rows are taken in an order
- * that M, D and groups alone decide. */
+ * that M, D and groups alone decide.  With t the whole gradient of r and v N1's normed row, dgate is summed as weight sum(t v) + bias sum(t), a term whose weight or bias is 0 left out: where t is infinite and both are not 0,
+ * it may be NaN in place of an infinity. */
 atb_status atb_residual_norm_backward(const atb_residual_norm *p, const float *stats, const void *dr, int64_t lddr, const void *dh, int64_t lddh,
                                       const atb_residual_norm_grads *grads, void *workspace, void *hip_stream);
 

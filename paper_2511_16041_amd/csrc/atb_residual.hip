@@ -771,7 +771,11 @@ __global__ void __launch_bounds__(1024) residual_params_kernel(const ResidualPar
     for (int i = 0; i < SUMS; ++i) s[i] = run[i];
     const bool normed1 = p.post.kind != ATB_NORM_NONE;
     auto value = [&](const void *w, int64_t at, float other) { return w ? (float)static_cast<const P *>(w)[at] : other; };
-    if (p.dgate) static_cast<P *>(p.dgate)[g * D + col] = (P)(value(normed1 ? p.post.weight : nullptr, col, 1.0f) * s[0] + value(normed1 ? p.post.bias : nullptr, col, 0.0f) * s[2]);
+    if (p.dgate) {
+        // (a factor of 0 takes its sum out: that may be infinite, and times 0 NaN, where sum t n1 is not)
+        const float w = value(normed1 ? p.post.weight : nullptr, col, 1.0f), b = value(normed1 ? p.post.bias : nullptr, col, 0.0f);
+        static_cast<P *>(p.dgate)[g * D + col] = (P)(b == 0.0f ? w * s[0] : w == 0.0f ? b * s[2] : w * s[0] + b * s[2]);
+    }
     const float gate = value(p.gate, g * D + col, 1.0f);
     s[0] *= gate;
     s[2] *= gate;

@@ -352,3 +352,20 @@ def test_an_infinite_gradient_is_infinite_in_its_row(D, stream, block):
             kinds = limits_of(got[k])
             assert torch.equal(kinds, limits_of(want[k])), (name, k)
             assert kinds[[2, 4]].any() and not kinds[[0, 1, 3, 5]].any(), (name, k)
+
+
+@pytest.mark.parametrize("groups", [1, 2, 3])
+@pytest.mark.parametrize("D", [7, 100, 5000, 9000, 20000])
+@pytest.mark.parametrize("post,weight,bias", [(None, None, None), ("rms", 1.0, None), ("rms", 1.0, 0.0), ("layer", None, 0.0), ("layer", 0.0, 0.5), ("rms", 0.0, 0.0)])
+def test_an_infinite_gradient_reaches_the_gate_as_it_is(post, weight, bias, D, groups):
+    """dr infinite at one place, with a norm `pre` that has a bias: sum t n1 is infinite of the sign of t n1, or NaN where n1 is 0, and nothing else of the gate's gradient is."""
+    a = inputs(6, D, F32, F32, F32, post, "layer", groups=groups, seed=D)
+    a["dr"], a["dh"] = a["dr"].clone(), 0 * a["dh"]
+    at = D // 2
+    a["dr"][4, at] = float("inf")
+    if post:
+        a["post"] = a["post"]._replace(**{k: torch.full_like(a["gate"].reshape(-1, D)[0], v) if v is not None else None for k, v in (("weight", weight), ("bias", bias))})
+    want, got = limits_of(reference(a)["dgate"][0]), limits_of(run(a)["dgate"]).reshape(groups, D)
+    kind = float(want[4 // (6 // groups), at])
+    assert kind == 2 if weight == bias == 0.0 else abs(kind) == 1
+    assert torch.equal(got, want)
