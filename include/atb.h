@@ -344,7 +344,7 @@ atb_status atb_linear_backward(const atb_linear *l, const void *slope, const voi
 typedef enum atb_norm_kind { ATB_NORM_NONE = 0, ATB_NORM_RMS = 1, ATB_NORM_LAYER = 2 } atb_norm_kind;
 typedef struct atb_norm {
     const void *weight, *bias;                  /* DEVICE, D elements of param_type, or NULL for 1 and 0 */
-    double eps;                                 /* >= 0 */
+    double eps;                                 /* >= 0, finite in fp32 and 0 there only if it is 0 */
     atb_norm_kind kind;                         /* ATB_NORM_NONE: the rest is not looked at */
 } atb_norm;
 typedef struct atb_residual_norm {

@@ -167,7 +167,9 @@ bool residual_lengths(int64_t M, int64_t D, int64_t groups)
 bool is_norm(const atb_norm &n, atb_type type)
 {
     if (n.kind == ATB_NORM_NONE) return true;
-    return (n.kind == ATB_NORM_RMS || n.kind == ATB_NORM_LAYER) && n.eps >= 0.0 && aligned(n.weight, size_of(type)) && aligned(n.bias, size_of(type));
+    // (the kernels take eps in fp32: one that becomes 0 there would make NaN of a row of zeros)
+    if (!(n.eps >= 0.0) || n.eps > std::numeric_limits<float>::max() || (n.eps > 0.0 && (float)n.eps == 0.0f)) return false;
+    return (n.kind == ATB_NORM_RMS || n.kind == ATB_NORM_LAYER) && aligned(n.weight, size_of(type)) && aligned(n.bias, size_of(type));
 }
 bool is_residual(const atb_residual_norm *p)
 {

@@ -126,6 +126,27 @@ def test_residual_norm_refuses():
         assert forward() == forward(pre=nothing, h=None) == forward(post=nothing, gate=None, groups=1) == forward(D=20000, ldx=20000, ldz=20000, ldr=20000, ldh=20000) == backward() == backward(dr=None) == 5
 
 
+@pytest.mark.parametrize("eps", [1e-50, 1e-46, 5e-324, 3.5e38, 1e300, float("inf")])
+@pytest.mark.parametrize("kind", [1, 2])
+def test_residual_norm_refuses_an_eps_that_fp32_does_not_hold(eps, kind):
+    """One that fp32 rounds to 0 would make 0 * inf of a row of zeros, one beyond its range 0 of every row."""
+    L = atb.lib()
+    keep, a = aligned_address()
+
+    def calls(eps, side):
+        norms = dict(post=atb.NormArgs(a, a, 1e-5, kind), pre=atb.NormArgs(a, a, 1e-5, kind))
+        norms[side].eps = eps
+        p = atb.ResidualNorm(a, a, 8, 8, norms["post"], norms["pre"], None, 1, 1.0, 0, 8, 0, 0, 0)
+        g = atb.ResidualNormGradArgs()
+        return (L.atb_residual_norm_forward(ctypes.byref(p), a, 8, a, 8, a, None), L.atb_residual_norm_backward(ctypes.byref(p), a, a, 8, a, 8, ctypes.byref(g), None, None))
+    for side in ("post", "pre"):
+        assert calls(eps, side) == (INVALID, INVALID)
+        for good in (0.0, 1e-45, 1e-40, 1e-5, 3.4e38):                          # (1e-45: the smallest that fp32 holds)
+            assert calls(good, side) == (0, 0), good
+        nothing = atb.NormArgs(None, None, eps, 0)                              # not looked at
+        assert L.atb_residual_norm_forward(ctypes.byref(atb.ResidualNorm(a, a, 8, 8, nothing, nothing, None, 1, 1.0, 0, 8, 0, 0, 0)), a, 8, None, 8, a, None) == 0
+
+
 def test_workspace_of_a_residual_norm():
     L = atb.lib()
     for M in (0, 6, 600, 60000, 2 ** 23 - 2 ** 23 % 6):
