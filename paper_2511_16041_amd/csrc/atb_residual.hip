@@ -372,22 +372,23 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
             const Params k = HOLD ? held[HOLD ? c : 0] : params(c);
             const Span own = span<T>(c, t, D);
             dr[c] = next_dr[c];
-            float dh[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) dh[e] = next_dh[c][e];
-            clear_before(dh, own.first);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
+                const float dh = next_dh[c][e];
                 xh1[c][e] = (next_z[c][e] - st.mean1) * st.rstd1;
                 const float r = p.scale * next_x[c][e] + k.gate[e] * (xh1[c][e] * k.w1[e] + k.b1[e]);
                 xh2[c][e] = (r - st.mean2) * st.rstd2;
                 if constexpr (SUMS > 0) {
                     if (live) {
-                        sum[1][c][e] += dh[e] * xh2[c][e];
-                        if constexpr (SUMS > 2) sum[SUMS - 1][c][e] += dh[e];
+                        sum[1][c][e] += dh * xh2[c][e];
+                        if constexpr (SUMS > 2) sum[SUMS - 1][c][e] += dh;
                     }
                 }
-                g[c][e] = dh[e] * k.w2[e];
+                g[c][e] = dh * k.w2[e];
+            }
+            clear_before(g[c], own.first);                    // (the products: a weight may be infinite)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
                 s[0] += g[c][e];
                 s[1] += g[c][e] * xh2[c][e];
             }
@@ -415,7 +416,6 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
                 d[e] = dr[c][e];
                 if (normed2) d[e] += st.rstd2 * (g[c][e] - m0 - xh2[c][e] * m1);
             }
-            clear_before(d, own.first);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if constexpr (SUMS > 0) {
@@ -426,6 +426,10 @@ __global__ void __launch_bounds__(T > kResidualThreads ? T : kResidualThreads) r
                 }
                 out[e] = p.scale * d[e];
                 g[c][e] = d[e] * k.gate[e] * k.w1[e];
+            }
+            clear_before(g[c], own.first);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
                 q[0] += g[c][e];
                 q[1] += g[c][e] * xh1[c][e];
             }

@@ -369,3 +369,22 @@ def test_an_infinite_gradient_reaches_the_gate_as_it_is(post, weight, bias, D, g
     kind = float(want[4 // (6 // groups), at])
     assert kind == 2 if weight == bias == 0.0 else abs(kind) == 1
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("stream,block", [(BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("D", [7, 8, 13, 96, 100, 515, 700, 5001, 8190, 9003, 12501, 20000])
+def test_an_infinite_weight_or_gate_gives_what_the_formulas_give(D, stream, block):
+    """Weight or gate of a root-mean-square norm infinite at the last elements of the row but one: the signs of dx and dz are the formulas', wherever the last chunks of a row lie."""
+    for post, pre, where in ((None, "rms", "pre"), ("rms", None, "post"), ("rms", None, "gate")):
+        a = inputs(5, D, stream, block, BF16, post, pre, seed=D + 3)
+        t = (a["gate"] if where == "gate" else a[where].weight).clone()
+        t[D - 2] = float("inf")
+        a = {**a, **({"gate": t} if where == "gate" else {where: a[where]._replace(weight=t)})}
+        x, z, gate, d = a["x"].double(), a["z"].double(), a["gate"].double(), a["dr"].double()
+        if pre:
+            d = d + rms_gradient(a["scale"] * x + gate * z, a["pre"], a["dh"].double())
+        want, got = {"dx": a["scale"] * d, "dz": rms_gradient(z, a["post"], d * gate) if post else d * gate}, run(a)
+        for k in ("dx", "dz"):
+            kinds = limits_of(got[k])
+            assert torch.equal(kinds, limits_of(want[k])), (where, k)
+            assert kinds.any() == (k == "dz" or where == "pre"), (where, k)
