@@ -382,7 +382,7 @@ atb_status atb_residual_norm_backward(const atb_residual_norm *p, const float *s
 /* A mixture of E experts, each a gated block, for few tokens: with l = x R^T, every token's k largest l (of equal ones the lowest expert), p = softmax(l) (renormalize != 0: of the chosen l alone),
  *     y = sum over the chosen experts e of p_e (act(x Wg_e^T) o (x Wu_e^T)) Wd_e^T,
  * weights in bf16 or all three in 4 bits.  l is summed in fp64, the products, p and the sum over the experts are fp32; the inner activations are rounded to bf16.  Only the chosen experts' weights are read, once for every 16 tokens
- * (32 where an expert has more than 12 on average; 4 bits: 16) that chose them.  A NaN among a token's l is behind all numbers, and its p as softmax gives it; 4-bit weights: see atb_q4_matvec. */
+ * (32 where an expert has more than 12 on average; 4 bits: 16) that chose them.  A NaN among a token's l is behind all others, -infinity too, and its p as softmax gives it; 4-bit weights: see atb_q4_matvec. */
 typedef struct atb_moe_weight {                 /* of all experts, one expert's rows after the other's, contiguous; DEVICE */
     const void *w;                              /* bf16, or codes as atb_q4's; 16-byte aligned */
     const void *scales, *zeros;                 /* 4 bits: as atb_q4's; all three weights with zero points or none */

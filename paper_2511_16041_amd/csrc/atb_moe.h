@@ -35,6 +35,9 @@ ATB_DEV MoeSegment moe_segment(const MoeCopy &c, int i)
     return {__builtin_amdgcn_readfirstlane(c.expert[i]), __builtin_amdgcn_readfirstlane(c.first[i]), __builtin_amdgcn_readfirstlane(c.rows[i])};
 }
 
+// What experts are ordered by: l, of -infinity less than all that sums of bf16 products can be (2^278), and NaN behind that
+ATB_DEV double moe_key(double l) { return l == l ? fmax(l, -0x1p1000) : -INFINITY; }
+
 // A token's router weights from its products, lane l's of the experts 64 i + l, and their ranks: exp(l - the largest l) over its sum over all experts or over the chosen ones.  A NaN or an infinity among the
 // summands gives what the formula gives.
 template <int PER>
@@ -69,7 +72,7 @@ ATB_DEV MoeFew moe_choose_few(const MoeParams &p, char *lds)
     int *ahead = reinterpret_cast<int *>(l + 256);
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, all = p.M * p.E;
     const double mine = t < all ? p.logits[t] : -INFINITY;
-    l[t] = mine == mine ? mine : -INFINITY;                        // NaN is behind all numbers
+    l[t] = moe_key(mine);
     ahead[t] = 0;
     __syncthreads();
     const int width = all <= 64 ? 64 : all <= 128 ? 128 : 256, o = t & (width - 1), per = (p.E * width + 255) / 256, from = t / width * per;

@@ -75,9 +75,9 @@ __global__ void __launch_bounds__(1024) moe_plan_kernel(const MoeParams p, int r
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             mine[i] = next[i];
-            left[i] = mine[i] == mine[i] ? mine[i] : -INFINITY;                // NaN is behind all numbers
             rank[i] = p.E;
             open[i] = 64 * i + lane < p.E;
+            left[i] = open[i] ? moe_key(mine[i]) : -INFINITY;
         }
         fetch(t + 16);
         // the greatest, of equal ones the first, k times (to count for every expert those ahead of it took 11 us of 21 tokens over 60 experts, this 6)

@@ -273,3 +273,31 @@ def test_through_the_c_entry_point():
     m = atb.Moe(args[0].data_ptr(), args[1].data_ptr(), D, D, *(atb.MoeWeight(w.data_ptr(), None, None) for w in args[2:]), M, D, F, E, k, 0, 0, 1, work.data_ptr())
     assert L.atb_moe_forward(ctypes.byref(m), y.data_ptr(), D + 3, None, None, stream) == 0
     assert torch.equal(y[:, :D], want) and bool((y[:, D:] == 7.0).all())
+
+
+@pytest.mark.parametrize("M", [1, 2, 8, 30])
+@pytest.mark.parametrize("E,group", [(12, 0), (12, 32), (70, 0), (200, 0)])
+def test_a_product_that_is_no_number_is_behind_minus_infinity(M, E, group):
+    """Experts with l = NaN, -infinity and numbers, by turns, NaN first: a token takes the numbers, then -infinity, whose share is 0, from the lowest index on, then NaN."""
+    x, router, *w = make(M, E, 96, 64, E + M, group)
+    x, router = x.abs(), router.clone()
+    numbers = [E - 1, 5, 2] + ([E // 2] if E > 12 else [])
+    for e in range(E):
+        if e not in numbers:
+            router[e, 7] = float("-inf") if e % 2 else float("nan")
+    x[:, 7] = 1.0
+    l = x.double() @ router.double().t()
+    low = [e for e in range(E) if e not in numbers and e % 2]
+    none = [e for e in range(E) if e not in numbers and e % 2 == 0]
+    assert l[:, low].isneginf().all() and l[:, none].isnan().all() and l[:, numbers].isfinite().all()
+    for k in (len(numbers) + 2, min(16, len(numbers) + len(low)), min(E, 16)):
+        y, chosen, shares = atb.moe_feed_forward(x, router, *w, k, routing=True)
+        n = len(numbers)
+        want = (low + none)[:k - n]
+        assert all(sorted(row[:n]) == sorted(numbers) and row[n:] == want for row in chosen.tolist()), (k, chosen[0].tolist())
+        if len(low) >= k - n:
+            assert not shares[:, n:].any()
+            finite = torch.where(router.isfinite(), router, torch.full_like(router, -2.0 ** 20))         # (the others' l far below, for the formula)
+            check((x, finite, *w), n, got=(y, chosen[:, :n], shares[:, :n]))
+        else:
+            assert shares.isnan().all() and y.isnan().all()
