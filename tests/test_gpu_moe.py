@@ -301,3 +301,16 @@ def test_a_product_that_is_no_number_is_behind_minus_infinity(M, E, group):
             check((x, finite, *w), n, got=(y, chosen[:, :n], shares[:, :n]))
         else:
             assert shares.isnan().all() and y.isnan().all()
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group,D,F", [(32, 67, 33), (32, 33, 67), (64, 33, 41), (64, 41, 33), (128, 17, 19), (128, 33, 17)])
+@pytest.mark.parametrize("M,E,k", [(8, 3, 2), (9, 3, 2), (17, 4, 1), (40, 3, 2), (64, 2, 1)])
+def test_weights_in_4_bits_over_many_panels(M, E, k, group, D, F, zeros):
+    """Reductions of 9 to 17 panels of 256, the last one cut, over four waves of the gate and up products and eight of the down product: a wave's second and third panel, and with more than 8 tokens the wide form.  Beside
+    the tolerance of every element, the 2-norm: the inner activations' rounding to bf16 and the result's, each at most 2^-8 / sqrt 3 of their size, are independent of each other and of the weights; all else is
+    2^-15 of it."""
+    args = make(M, E, D * group, F * group, M + D + F, group, zeros)
+    y, _, _ = check(args, k, "gelu_tanh", k == 2)
+    want = reference(*args, k, "gelu_tanh", k == 2)[0]
+    assert float((y.double() - want).norm()) <= 1.5 * R * float(want.norm())
