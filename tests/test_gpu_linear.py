@@ -282,3 +282,35 @@ def test_gradients_against_differences_along_themselves():
         # six deviations of y's roundings, independent; 2^-7 of the slope itself (its two roundings, in the 2-norm); the third derivative, below 2: 2 / 3 of an eighth cubed of |dy|
         limit = 6 * 2 ** 0.5 * R / 3 ** 0.5 * size + 2 * R * abs(want) + 2 / 3 * 0.125 ** 3 * float(dy.double().abs().sum())
         assert abs(losses[0] - losses[1] - want) <= limit, (grad, losses[0] - losses[1], want, limit)
+
+
+def difference(args, at, grad, dy, act, h, forward):
+    """Loss = sum of y dy: (its difference between the two ends of a move of operand `at` along its gradient, both ways by so much that no z moves by more than h; what the gradient makes of that; what they may be apart)"""
+    x, w = args[0].double(), args[1].double()
+    g = grad.double()
+
+    def z_of(v):
+        return v @ w.t() if at == 0 else x @ v.t() if at == 1 else v.expand(dy.shape)
+    v = g * (h / float(z_of(g).abs().max()))
+    ends = [(args[at].double() + s * v).to(args[at].dtype) for s in (1, -1)]                       # as they are after rounding
+    moved, shift = (z_of(t) for t in ((ends[0].double() - ends[1].double()) / 2, (ends[0].double() + ends[1].double()) / 2 - args[at].double()))
+    y = [forward(*args[:at], t, *args[at + 1:], act).double() for t in ends]
+    size = max(float((t * dy.double()).norm()) for t in y)
+    want, weight = float((g * (ends[0].double() - ends[1].double())).sum()), dy.double().abs()
+    # six deviations of y's roundings, independent of each other, of both ends; the gradient's own two roundings in the 2-norm; the third derivative, below 2, and the second, below 1.2, where rounding has moved the middle
+    limit = 6 * 2 ** 0.5 * R / 3 ** 0.5 * size + 2 * R * abs(want)
+    if act:
+        limit += 2 / 3 * float((weight * moved.abs() ** 3).sum()) + 2 * 1.2 * float((weight * moved.abs() * shift.abs()).sum())
+    return float((y[0] * dy.double()).sum() - (y[1] * dy.double()).sum()), want, limit
+
+
+@pytest.mark.parametrize("M,N,K", [(24, 136, 128), (64, 137, 128), (200, 264, 136)])
+@pytest.mark.parametrize("act", [None, "silu", "gelu", "gelu_tanh"])
+def test_gradients_against_differences_that_tell_them_from_wrong_ones(M, N, K, act):
+    """Along each gradient the loss moves by ten times what the difference may be off or more, so one that is zero, half as large or of the other sign is not taken."""
+    x, w, b, _, dy = make(M, N, K, 18, bias=F32, residual=False)
+    got = train(x, w, b, None, dy, act)
+    for name, at in (("dx", 0), ("dw", 1), ("db", 2)):
+        moved, want, limit = difference([x, w, b], at, got[name], dy, act, 0.125, atb.linear)
+        assert abs(moved - want) <= limit, (name, moved, want, limit)
+        assert abs(moved) > 10 * limit and abs(moved - 0.5 * want) > limit and abs(moved + want) > limit, (name, moved, want, limit)
