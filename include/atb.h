@@ -329,7 +329,8 @@ size_t atb_linear_workspace(int64_t M, int64_t N, int64_t K);
 size_t atb_linear_backward_workspace(int64_t M, int64_t N, int64_t K, atb_activation act);
 
 /* residual: DEVICE, M x N bf16 (pitch ldr), or NULL; may be y.  slope: DEVICE, M rows of round_up(N, 8) fp16, 16-byte aligned, of which N are written with act'(x W^T + bias)
- * for the backward pass, or NULL; with ATB_ACT_NONE there is none.  y: DEVICE, M x N bf16 (pitch ldy).  y and residual at any element.  Async on hip_stream. */
+ * for the backward pass, or NULL; with ATB_ACT_NONE there is none.  Beside fp32's errors it is off by 2^-11 of itself at most, or by 2^-25 where that is more: slopes below 2^-14 lose digits, and their part of the
+ * gradients with them.  y: DEVICE, M x N bf16 (pitch ldy).  y and residual at any element.  Async on hip_stream. */
 atb_status atb_linear_forward(const atb_linear *l, const void *residual, int64_t ldr, void *slope, void *y, int64_t ldy, void *hip_stream);
 
 /* Gradients of a loss with dy (M x N bf16, pitch lddy): with dz = dy o act'(z), rounded to bf16 for the products,

@@ -18,7 +18,7 @@ NO_ACTIVATION = len(ACTIVATIONS)       # ATB_ACT_NONE
 def linear(x, weight, bias=None, act: Optional[str] = None, residual=None, save: bool = False, stream=None):
     """act(x weight^T + bias) + residual in bf16: x M x K, weight N x K (as a linear layer's is kept), residual M x N; bias: N elements in bf16 or fp32.  K a multiple of 8, rows of x and weight
     16-byte aligned and a multiple of 8 elements apart; N any.  act: "silu", "gelu", "gelu_tanh" or None.  save: returns (y, slope), the activation's derivative in fp16 (M rows of
-    round_up(N, 8), of which N count; None without an activation), which linear_backward takes."""
+    round_up(N, 8), of which N count; None without an activation; off by 2^-11 of itself or by 2^-25, what is more), which linear_backward takes."""
     return _call("linear", "atb_linear_forward", stream, _address("atb_linear_forward"), _address("atb_linear_workspace"), x, weight, bias,
                  NO_ACTIVATION if act is None else _activation(act), residual, save)
 

@@ -314,3 +314,20 @@ def test_gradients_against_differences_that_tell_them_from_wrong_ones(M, N, K, a
         moved, want, limit = difference([x, w, b], at, got[name], dy, act, 0.125, atb.linear)
         assert abs(moved - want) <= limit, (name, moved, want, limit)
         assert abs(moved) > 10 * limit and abs(moved - 0.5 * want) > limit and abs(moved + want) > limit, (name, moved, want, limit)
+
+
+@pytest.mark.parametrize("M", [5, 33, 300])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_the_kept_slope_where_the_activation_is_flat(M, act):
+    """z from 5 to 40 on both sides: the slope is off by 2^-11 of itself or by 2^-25, what is more.  Beside it, 2^-15 of it for an exponential whose argument of up to 100 is rounded in fp32 (100 * 2^-24 * log2 e, and as
+    much of its result), and 2^-30 for the distribution function's polynomial, 1.6e-3 of 2.9e-7 at -5."""
+    N = 72
+    z = torch.cat((torch.linspace(-40, -5, M * N // 2 + 1), torch.linspace(5, 40, M * N // 2 + 1)))[:M * N].reshape(M, N).bfloat16().cuda()
+    x = torch.zeros((M, 8 * ((M + 7) // 8)), dtype=BF16, device="cuda")
+    x[torch.arange(M), torch.arange(M)] = 1.0                  # row m of x picks column m of w: z[m, n] = w[n, m], exactly
+    w = torch.zeros((N, x.shape[1]), dtype=BF16, device="cuda")
+    w[:, :M] = z.t()
+    slope = atb.linear(x, w, None, act, save=True)[1][:, :N].double()
+    want = activation(act, z.double())[1]
+    limit = torch.maximum(2.0 ** -11 * want.abs(), torch.tensor(2.0 ** -25, dtype=torch.float64, device="cuda")) + 2.0 ** -15 * want.abs() + 2.0 ** -30
+    assert bool(((slope - want).abs() <= limit).all()), float(((slope - want).abs() / limit).max())
