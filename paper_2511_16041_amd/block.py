@@ -24,7 +24,8 @@ def linear(x, weight, bias=None, act: Optional[str] = None, residual=None, save:
 
 
 def linear_backward(dy, x, weight, bias=None, slope=None, stream=None):
-    """(dx, dweight, dbias) of linear: in bf16, dbias in the bias's type and None without one; the residual's gradient is dy.  slope: what the forward call returned.  Inside, dy times
+    """(dx, dweight, dbias) of linear: in bf16, dbias in the bias's type and None without one; the residual's gradient is dy.  All three are
+    computed (the C entry point takes NULL for those that are not asked for).  slope: what the forward call returned.  Inside, dy times
     slope is rounded to bf16 for the two products.  Without a slope and with N a multiple of 8 the rows of dy are 16-byte aligned and a multiple of 8 elements apart."""
     return _call("linear_backward", "atb_linear_backward", stream, _address("atb_linear_backward"), _address("atb_linear_backward_workspace"), dy, x, weight, bias, slope)
 
@@ -70,7 +71,8 @@ def residual_norm(x, z, post: Optional[Norm] = None, gate=None, scale: float = 1
 
 
 def residual_norm_backward(dr, dh, x, z, stats, post: Optional[Norm] = None, gate=None, scale: float = 1.0, pre: Optional[Norm] = None, stream=None) -> ResidualNormGrads:
-    """The gradients of residual_norm from those of r (by all but h; None: 0) and of h (None without a norm `pre`), each in its operand's type.  The same inputs give the same bits."""
+    """The gradients of residual_norm from those of r (by all but h; None: 0) and of h (None without a norm `pre`), each in its operand's type; of everything that is there
+    (the C entry point takes NULL for those that are not asked for).  The same inputs give the same bits."""
     return ResidualNormGrads(*_call("residual_norm_backward", "atb_residual_norm_backward", stream, _address("atb_residual_norm_backward"), _address("atb_residual_norm_workspace"),
                                     dr, dh, x, z, stats, *_norm(post), gate, scale, *_norm(pre)))
 

@@ -84,8 +84,8 @@ constexpr int kResidualMaxGradRow = 2 * kResidualThreads * kResidualPerThread;  
 
 // ... and rows of less than a chunk with them
 static inline bool residual_is_long(int64_t D) { return D > kResidualMaxGradRow || D < kResidualPerThread; }
-// Rows of up to twice as many elements in 16 bits are held for dx and dz; there are no registers for the sums too, which stay a pass of their own.  us without the sums, held / read again: 4096 x 12000 159 / 225, 512 x 16384
-// 27 / 36, 9 x 11066 7.6 / 19.5.
+// Rows of up to twice as many elements in 16 bits are held for dx and dz; their sums are a pass of their own, as those of longer rows.  (The kernels have 123 to 199 of 256 registers: two sums, 48 or 64 more, would fit some of
+// them; not tried.)  us without the sums, held / read again: 4096 x 12000 138 / 225, 512 x 16384 28 / 36, 9 x 11066 7.6 / 19.5.  With x in fp32, whose rows are read again, 4096 x 12000 takes 294.
 static inline bool residual_is_wide(int64_t D) { return D > kResidualMaxGradRow && D <= 2 * kResidualMaxGradRow; }
 
 // Threads per row: the power of two, 64 to 512, that holds it.

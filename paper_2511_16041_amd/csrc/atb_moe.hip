@@ -7,9 +7,9 @@
 // products of every expert and its tokens, as the kernel for few rows does them, with the rows of x gathered by the plan; h by place.  (4) The down product: a workgroup has 16 columns of y and
 // all experts in turn; its waves take the panels of all of them as one long reduction, and at an expert's end each adds its sums, times the tokens' shares, to its own part of y in LDS.  So every expert's weights
 // are read once (of more tokens than a segment's 16 or 32 again), those of no token not at all, the sum over a token's experts is in fp32, in the order of the experts, without atomics, and no token's values meet another's.
-// Bound: the bytes of the weights; one token in 4 bits: launches, each of which waits for what the one before wrote.
-// Measured, gate and up / down, us: one token through 2 of 8 experts of 4096 x 14336 80.0 / 43.9, 5.9 and 5.3 TB/s; 21 tokens over 60 of 2056 x 1416 106 / 74, 6.6 and 4.7; in 4 bits one token through 8 of 64 of 2048 x 1536
-// 14.1 / 7.2, with the router 2.9 and the join 2.7, 32 tokens over 8 of 4096 x 14336 123 / 76, 4.0 and 3.2 TB/s (VALU busy 51 and 44 %; every 16 tokens of an expert decode its weights again).
+// Bound: the bytes of the weights; one token in 4 bits: latency, in the gate and up kernel that of what it waits for in a row (the router's products, the choice, weights, x), and four launches.
+// Measured, gate and up / down, us: one token through 2 of 8 experts of 4096 x 14336 80.0 / 43.9, 5.9 and 5.3 TB/s; 21 tokens over 60 of 2056 x 1416 106 / 74, 5.9 and 4.2 (of the 53.4 experts that they choose on average); in 4 bits one token through 8 of 64 of 2048 x 1536
+// 14.1 / 7.2, with the router 2.9 and the join 2.7, 32 tokens over 8 of 4096 x 14336 123 / 76, 3.9 and 3.2 TB/s (VALU busy 51 and 44 %; every 16 tokens of an expert decode its weights again).
 #include "atb_moe.h"
 #include "atb_stream_rows.h"
 
